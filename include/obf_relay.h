@@ -338,6 +338,85 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
                                        const int32_t* budgets_host, int32_t budget, int32_t max_budget, int32_t rank,
                                        void* K_out, void* V_out, int32_t* idx, int32_t* n_keep, void* stream);
 
+/* ---- reading and thinning out a relayed cache ------------------------------------------------------------------------
+ * The receiver of a message attends over it: headwise retention gives every (sample, KV head) a length of its own, the rows of
+ * a head stand in the order of its tokens, its newest n_queries rows are those of the queries themselves.
+ *
+ * obf_attend_t, one layer of a batch:
+ *   Q, O      element (s, i, t, c) at s * stride[0] + i * stride[1] + t * stride[2] + c; all three strides 0: contiguous
+ *             [n_samples][n_kv_heads*group][n_queries][head_dim].  Query head i belongs to KV head i / group.
+ *   K, V      row (s, h, j) at s * sample_stride + h * token_stride + j (in rows; sample_stride 0: n_kv_heads * token_stride),
+ *             so a layer of [n_samples][n_layers][n_kv_heads][token_stride][head_dim] is a call's cache as it lies
+ *   kv_len    rows per (sample, head), DEVICE int32, entry s * len_stride + h (len_stride 0: n_kv_heads); NULL: kv_len_all in
+ *             all.  A length below 0 or above token_stride (the -1 of obf_append_message) counts as a head without rows.
+ *   sink_len  first rows that stay visible, laid out as kv_len (the inherited message); NULL: `sink` in all
+ *   lse       nullable, float [n_samples][n_kv_heads*group][n_queries]: log of the sum of exp(logit) over the visible rows
+ *   mass      float, one per cache row with the row numbers of K: accumulated attention weight
+ * Logits are q . k / sqrt(head_dim), Q and K as given.  Of a head of n rows query t stands at position p = n - n_queries + t and
+ * sees the rows j < n with, if causal, j <= p and, if window > 0 (causal only), j > p - window or j < sink.  A query that sees
+ * nothing gets O = 0 and lse = -inf.  What a query does not see never reaches its result, not-a-number and infinities included;
+ * rows at and behind a head's length are not read.
+ * Sums and softmax statistics are single precision; O is rounded once to dtype.  With dtype OBF_BF16 the softmax weights enter
+ * the product with V as two bf16 parts, or as one where n_queries * group exceeds what is bound by the cache's bytes.
+ * Limits: head_dim 64 or 128; group <= 128; n_queries <= 2^20; strides of rows <= 2^24; n_samples*n_kv_heads <= 65535; at most
+ * 2^28 query rows and 2^36 cache rows; Q, K, V, O 16-byte aligned, strides of Q and O multiples of 16 bytes.  O may not overlap an input.  Results do
+ * not depend on what the workspace held, and are the same from call to call.  Two calls that may overlap in time (or two captured
+ * graphs) need a workspace each. */
+typedef struct {
+  int32_t n_samples;
+  int32_t n_kv_heads;
+  int32_t group;
+  int32_t head_dim;
+  int32_t n_queries;
+  int32_t token_stride;
+  int32_t dtype;          /* obf_dtype_t of Q, K, V, O */
+  int32_t causal;
+  int32_t window;         /* 0: none */
+  int32_t sink;
+  int32_t kv_len_all;
+  int32_t len_stride;
+  int64_t sample_stride;
+  int64_t q_stride[3];
+  int64_t o_stride[3];
+} obf_attend_t;
+
+/* Bytes of workspace of obf_attend (prefix_stride 0) or obf_attend_shared; 0 if the call is not supported.  Host function. */
+size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride);
+
+/* Attention of the queries over their own caches.  mass (nullable): the weight every visible row receives, summed over the
+ * head's group of query heads and the queries, is added to mass[row]; what it adds is the same from call to call. */
+obf_status_t obf_attend(const obf_attend_t* call, const void* Q, const void* K, const void* V, const int32_t* kv_len,
+                        const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, void* stream);
+
+/* The same for samples that share a message: before its own rows every query sees all rows of the message, prefix_K and
+ * prefix_V [n_kv_heads][prefix_stride][head_dim] with prefix_len[h] rows (DEVICE int32; NULL: prefix_len_all in all; a length
+ * outside [0, prefix_stride] counts as none).  One softmax runs over both; causal, window and sink are of the own rows, whose
+ * positions do not count the message. */
+obf_status_t obf_attend_shared(const obf_attend_t* call, const void* Q, const void* prefix_K, const void* prefix_V,
+                               const int32_t* prefix_len, int32_t prefix_len_all, int32_t prefix_stride, const void* K,
+                               const void* V, const int32_t* kv_len, const int32_t* sink_len, void* O, float* lse,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* The accumulated attention weight alone, from the lse that obf_attend or obf_attend_shared returned for the same queries:
+ * mass[row] += sum of exp(logit - lse) over the queries that see the row (a query of lse -inf counts 0). */
+obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void* K, const float* lse, const int32_t* kv_len,
+                             const int32_t* sink_len, float* mass, void* stream);
+
+/* Eviction by accumulated attention weight.  Of a head of n rows the first s (sink_len[h], DEVICE int32, or `sink`; they travel
+ * outside the budget, as in obf_window_t) and min(budget, n - s) of the others are kept: the newest `recent` ones and those of
+ * the largest mass, ties to the lowest index, by the order of the fp32 bit patterns (obf_select_topk's).  Kept rows keep their
+ * order and are copied bit for bit:
+ *   K, V [n_heads][in_stride][head_dim], mass [n_heads][in_stride], pos (nullable int32, the same)   ->
+ *   K_out, V_out [n_heads][out_stride][head_dim], mass_out, pos_out [n_heads][out_stride]; rows at and behind len_out[h] are
+ *   left as they were;  idx [n_heads][out_stride]: the rows kept, -1 behind them;  len_out [n_heads].
+ * kv_len (DEVICE int32 [n_heads]; NULL: kv_len_all).  A head whose length lies outside [0, in_stride], or whose kept rows exceed
+ * out_stride (possible with sink_len only), gets len_out = -1, idx -1 and no rows.  recent <= budget, min(budget + sink, in_stride) <= out_stride.
+ * Outputs may not overlap inputs (what the host can see of it is OBF_ERR_INVALID_ARG). */
+obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const void* K, const void* V, const float* mass,
+                       const int32_t* pos, const int32_t* kv_len, int32_t kv_len_all, int32_t in_stride, int32_t budget,
+                       int32_t recent, const int32_t* sink_len, int32_t sink, void* K_out, void* V_out, float* mass_out,
+                       int32_t* pos_out, int32_t* idx, int32_t* len_out, int32_t out_stride, void* stream);
+
 /* Profiling aid (tracing of the path's own kernels with HIP events on the caller's stream).
  * obf_profile_enable(stage) makes every later call on this thread bracket the launch of that
  * internal stage's kernel with a pair of events; stage -1 switches it off.  obf_profile_read

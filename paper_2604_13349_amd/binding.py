@@ -39,6 +39,14 @@ class _Variant(C.Structure):
                 ("subspace_iters", C.c_int32), ("per_token", C.c_int32)]
 
 
+class _Attend(C.Structure):
+    """obf_attend_t."""
+    _fields_ = [("n_samples", C.c_int32), ("n_kv_heads", C.c_int32), ("group", C.c_int32), ("head_dim", C.c_int32),
+                ("n_queries", C.c_int32), ("token_stride", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32),
+                ("window", C.c_int32), ("sink", C.c_int32), ("kv_len_all", C.c_int32), ("len_stride", C.c_int32),
+                ("sample_stride", C.c_int64), ("q_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3)]
+
+
 class _Window(C.Structure):
     """obf_window_t."""
     _fields_ = [("token_stride", C.c_int32), ("sink", C.c_int32)]
@@ -114,6 +122,17 @@ def load_library():
     lib.obf_compress_relay_static.argtypes = [sp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.obf_append_message.restype = C.c_int
     lib.obf_append_message.argtypes = [i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, i32, vp]
+    ap = C.POINTER(_Attend)
+    lib.obf_attend_workspace_bytes.restype = sz
+    lib.obf_attend_workspace_bytes.argtypes = [ap, i32]
+    lib.obf_attend.restype = C.c_int
+    lib.obf_attend.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.obf_attend_shared.restype = C.c_int
+    lib.obf_attend_shared.argtypes = [ap, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.obf_attend_mass.restype = C.c_int
+    lib.obf_attend_mass.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp]
+    lib.obf_evict.restype = C.c_int
+    lib.obf_evict.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp]
     lib.obf_profile_enable.restype = C.c_int
     lib.obf_profile_enable.argtypes = [i32]
     lib.obf_profile_read.restype = C.c_int
@@ -431,6 +450,189 @@ def append_message(prev_K, prev_V, prev_len, keep_K, keep_V, n_keep, gen_K, gen_
         _ptr(keep_K), _ptr(keep_V), _ptr(n_keep), rows(keep_K), _ptr(gen_K), _ptr(gen_V), rows(gen_K), rows(gen_K),
         _ptr(msg_K), _ptr(msg_V), _ptr(msg_len), msg_stride, _stream()))
     return msg_K, msg_V, msg_len
+
+
+def _on_device(ref: torch.Tensor, **tensors):
+    """Every tensor given (None: not given) lies on ref's GPU."""
+    if not ref.is_cuda:
+        raise ValueError("tensors must be on a GPU")
+    for name, t in tensors.items():
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+
+
+def _int32(name: str, t: Optional[torch.Tensor], shape):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be int32 {list(shape)}")
+    return t
+
+
+def _q_strides(name: str, t: torch.Tensor, d: int):
+    """Strides of a [samples, heads, queries, d] tensor; those of dimensions of one are made up."""
+    if t.shape[3] != 1 and t.stride(3) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return [t.stride(i) if t.shape[i] > 1 else d * max(1, t.shape[2]) for i in range(3)]
+
+
+def _attend_call(Q, K, kv_len, sink_len, causal, window, sink, V=None, mass=None, O=None):
+    """obf_attend_t of the call, with the tensors checked against each other; also kv_len and sink_len as they are handed over."""
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("Q must be [samples, query heads, queries, d], K [samples, heads, rows, d]")
+    S, Hq, T, d = Q.shape
+    Sk, H, rows, dk = K.shape
+    if Sk != S or dk != d or H < 1 or Hq % H != 0:
+        raise ValueError("Q does not match K")
+    if K.dtype not in (torch.float32, torch.bfloat16) or Q.dtype != K.dtype:
+        raise ValueError("Q and K must both be float32 or bfloat16")
+    if V is not None and (V.shape != K.shape or V.dtype != K.dtype):
+        raise ValueError("V does not match K")
+
+    def rows_between(name, t, width):
+        """Rows between the samples of a cache tensor whose heads are contiguous."""
+        if any(n > 1 and t.stride(i + 1) != w for i, (n, w) in enumerate(zip(t.shape[1:], (rows * width, width, 1)))):
+            raise ValueError(f"{name}: the heads of a sample must be contiguous")
+        if S == 1:
+            return H * rows
+        if t.stride(0) % width or t.stride(0) < H * rows * width:
+            raise ValueError(f"{name}: samples must be whole rows apart and not overlap")
+        return t.stride(0) // width
+
+    apart = rows_between("K", K, d)
+    if V is not None and rows_between("V", V, d) != apart:
+        raise ValueError("K and V must have the same strides")
+    if mass is not None:
+        if mass.dtype != torch.float32 or tuple(mass.shape) != (S, H, rows):
+            raise ValueError("mass must be float32 [samples, heads, rows]")
+        if H > 1 and mass.stride(1) != rows or rows > 1 and mass.stride(2) != 1 or S > 1 and mass.stride(0) != apart:
+            raise ValueError("mass must have the row strides of K")
+    kv_len, sink_len = _int32("kv_len", kv_len, (S, H)), _int32("sink_len", sink_len, (S, H))
+    lens = [t for t in (kv_len, sink_len) if t is not None]
+    if any(H > 1 and t.stride(1) != 1 or S > 1 and t.stride(0) < H for t in lens) or len({t.stride(0) for t in lens if S > 1}) > 1:
+        kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
+        lens = [t for t in (kv_len, sink_len) if t is not None]
+    c = _Attend(S, H, Hq // H, d, T, rows, OBF_F32 if K.dtype == torch.float32 else OBF_BF16, int(bool(causal)), int(window), int(sink), rows,
+                lens[0].stride(0) if lens and S > 1 else 0, apart)
+    c.q_stride = (C.c_int64 * 3)(*_q_strides("Q", Q, d))
+    if O is not None:
+        if O.shape != Q.shape or O.dtype != Q.dtype:
+            raise ValueError("O must have the shape and dtype of Q")
+        so = _q_strides("O", O, d)
+        if any(n > 1 and w < d for n, w in zip(O.shape[:3], so)):
+            raise ValueError("O: rows must not overlap")
+        c.o_stride = (C.c_int64 * 3)(*so)
+    return c, kv_len, sink_len
+
+
+def _at(t: Optional[torch.Tensor]):
+    """Address of a tensor whose strides travel beside it."""
+    return None if t is None else C.c_void_p(t.data_ptr())
+
+
+def _attend_out(out, Q):
+    """Output dict of an attention call: O, lse and the workspace, reused from `out` where they fit."""
+    o = out if out is not None else {}
+    if "O" not in o:
+        o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if "lse" not in o:
+        o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+    if o["lse"].dtype != torch.float32 or o["lse"].shape != Q.shape[:3] or not o["lse"].is_contiguous():
+        raise ValueError("lse must be contiguous float32 [samples, query heads, queries]")
+    return o
+
+
+def _attend_ws(o, c, prefix_stride, device):
+    lib = load_library()
+    need = int(lib.obf_attend_workspace_bytes(C.byref(c), prefix_stride))
+    if need == 0:
+        raise ObfError(2, lib.obf_last_error().decode())
+    if o.get("ws") is None or o["ws"].numel() < need:
+        o["ws"] = torch.empty(need, dtype=torch.uint8, device=device)
+    return o["ws"]
+
+
+def attend(Q, K, V, kv_len=None, causal=True, window=0, sink=0, sink_len=None, mass=None, out=None):
+    """obf_attend: Q [S,H*g,T,d] (any strides of 16 bytes, last dimension contiguous) over the caches K, V [S,H,rows,d] (samples any whole number of rows
+    apart) with kv_len int32 [S,H] rows per head (None: all).  sink_len int32 [S,H]: first rows that stay visible behind a window, per head, in place of
+    `sink`.  mass float32 [S,H,rows], in place: accumulated attention weight.  out: a dict returned by an earlier call of the same shape, whose buffers and
+    workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws."""
+    _on_device(Q, K=K, V=V, kv_len=kv_len, sink_len=sink_len, mass=mass, **(out or {}))
+    o = _attend_out(out, Q)
+    c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, V=V, mass=mass, O=o["O"])
+    with torch.cuda.device(Q.device):
+        ws = _attend_ws(o, c, 0, Q.device)
+        _check(load_library().obf_attend(C.byref(c), _at(Q), _at(K), _at(V), _at(kv_len), _at(sink_len), _at(o["O"]), _at(o["lse"]), _at(mass),
+                                         _ptr(ws), ws.numel(), _stream()))
+    return o
+
+
+def attend_shared(Q, prefix_K, prefix_V, K, V, prefix_len=None, kv_len=None, causal=True, window=0, sink=0, sink_len=None, out=None):
+    """obf_attend_shared: as attend, with the rows of a message prefix_K, prefix_V [H,prefix rows,d] that all samples see before their own;
+    prefix_len int32 [H] rows per head (None: all)."""
+    _on_device(Q, K=K, V=V, kv_len=kv_len, sink_len=sink_len, prefix_K=prefix_K, prefix_V=prefix_V, prefix_len=prefix_len,
+               **(out or {}))
+    o = _attend_out(out, Q)
+    c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, V=V, O=o["O"])
+    if prefix_K.dim() != 3 or prefix_K.shape[0] != c.n_kv_heads or prefix_K.shape[2] != c.head_dim or prefix_K.dtype != K.dtype:
+        raise ValueError("prefix_K must be [heads, rows, d] of K's dtype")
+    if prefix_V.shape != prefix_K.shape or prefix_V.dtype != K.dtype:
+        raise ValueError("prefix_V does not match prefix_K")
+    prefix_len = _int32("prefix_len", prefix_len, (c.n_kv_heads,))
+    rows = prefix_K.shape[1]
+    with torch.cuda.device(Q.device):
+        ws = _attend_ws(o, c, rows, Q.device)
+        _check(load_library().obf_attend_shared(C.byref(c), _at(Q), _ptr(prefix_K), _ptr(prefix_V), _ptr(prefix_len), rows, rows, _at(K), _at(V),
+                                                _at(kv_len), _at(sink_len), _at(o["O"]), _at(o["lse"]), _ptr(ws), ws.numel(), _stream()))
+    return o
+
+
+def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sink_len=None):
+    """obf_attend_mass: adds to mass float32 [S,H,rows], in place, the attention weight of the rows of K under the lse [S,H*g,T] of an earlier call."""
+    _on_device(Q, K=K, lse=lse, mass=mass, kv_len=kv_len, sink_len=sink_len)
+    c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, mass=mass)
+    if lse.dtype != torch.float32 or lse.shape != Q.shape[:3]:
+        raise ValueError("lse must be float32 [samples, query heads, queries]")
+    with torch.cuda.device(Q.device):
+        _check(load_library().obf_attend_mass(C.byref(c), _at(Q), _at(K), _ptr(lse), _at(kv_len), _at(sink_len), _at(mass), _stream()))
+    return mass
+
+
+def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, sink_len=None, pos=None, out=None, out_stride: Optional[int] = None):
+    """obf_evict on K, V [..., rows, d], mass float32 [..., rows] and pos (int32, optional) [..., rows]; leading dimensions = heads, kv_len and sink_len
+    int32 [...].  out: buffers to fill, K_out, V_out [..., out_stride, d], mass_out, pos_out, idx [..., out_stride], len_out [...]; those not given are
+    allocated with out_stride rows per head (default: sink + budget; needed with sink_len).  Rows behind len_out stay as they are."""
+    if K.dim() < 2 or V.shape != K.shape or V.dtype != K.dtype or K.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("K and V must be [..., rows, d], float32 or bfloat16")
+    lead, rows, d = tuple(K.shape[:-2]), K.shape[-2], K.shape[-1]
+    if mass.dtype != torch.float32 or tuple(mass.shape) != lead + (rows,):
+        raise ValueError("mass must be float32 [..., rows]")
+    pos, kv_len, sink_len = _int32("pos", pos, lead + (rows,)), _int32("kv_len", kv_len, lead), _int32("sink_len", sink_len, lead)
+    o = out if out is not None else {}
+    if out_stride is None:
+        if "K_out" in o:
+            out_stride = o["K_out"].shape[-2]
+        elif sink_len is not None:
+            raise ValueError("out_stride is needed with sink_len")
+        else:
+            out_stride = max(1, min(budget + sink, rows))
+    _on_device(K, V=V, mass=mass, pos=pos, kv_len=kv_len, sink_len=sink_len, **o)
+    want = {"K_out": (lead + (out_stride, d), K.dtype), "V_out": (lead + (out_stride, d), K.dtype), "mass_out": (lead + (out_stride,), torch.float32),
+            "idx": (lead + (out_stride,), torch.int32), "len_out": (lead, torch.int32)}
+    if pos is not None:
+        want["pos_out"] = (lead + (out_stride,), torch.int32)
+    for name, (shape, dtype) in want.items():
+        if name not in o:
+            o[name] = torch.empty(shape, dtype=dtype, device=K.device)
+        elif tuple(o[name].shape) != shape or o[name].dtype != dtype:
+            raise ValueError(f"{name} must be {dtype} {list(shape)}")
+    dt = OBF_BF16 if K.dtype == torch.bfloat16 else OBF_F32
+    with torch.cuda.device(K.device):
+        _check(load_library().obf_evict(
+            int(np.prod(lead)) if lead else 1, d, dt, _ptr(K), _ptr(V), _ptr(mass), _ptr(pos), _ptr(kv_len), rows, rows, budget, recent, _ptr(sink_len), sink,
+            _ptr(o["K_out"]), _ptr(o["V_out"]), _ptr(o["mass_out"]), _ptr(o["pos_out"]) if pos is not None else None, _ptr(o["idx"]), _ptr(o["len_out"]),
+            out_stride, _stream()))
+    return o
 
 
 def diag_to_numpy(diag: torch.Tensor) -> np.ndarray:

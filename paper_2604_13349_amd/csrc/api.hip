@@ -87,7 +87,8 @@ ProfScope::~ProfScope() {
 }
 
 static const char* kStageNames[ST_COUNT] = {"score_stats", "score_lse", "score_mass", "select", "refine", "gather",
-                                            "keep_cert", "keep_basis", "del_stats", "finalize", "basis_stats"};
+                                            "keep_cert", "keep_basis", "del_stats", "finalize", "basis_stats",
+                                            "attend", "attend_join", "attend_mass", "evict"};
 
 static obf_status_t check_shape(const obf_shape_t* s) {
   if (!s) { set_error("shape is NULL"); return OBF_ERR_INVALID_ARG; }
@@ -135,9 +136,6 @@ static obf_status_t run_score(const Dims& m, const Workspace& w, char* ws, const
 }  // namespace obf
 
 using namespace obf;
-
-#define OBF_TRY(expr) do { obf_status_t _s = (expr); if (_s != OBF_OK) return _s; } while (0)
-#define OBF_NONNULL(p) do { if (!(p)) { set_error(#p " is NULL"); return OBF_ERR_INVALID_ARG; } } while (0)
 
 extern "C" {
 

@@ -1,0 +1,103 @@
+// Attention over a relayed cache: what the kernels of attend_few.hip, attend_tile.hip, attend_mass.hip and the host side share.
+#pragma once
+#include "common.hpp"
+
+namespace obf {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+// A set of keys and the query rows that read it: the samples' own rows (one set per sample and KV head), or the rows of a message that all samples share.
+struct AttendKeys {
+  const void* K;
+  const void* V;
+  const int32_t* len;        // nullable: len_all rows in every head
+  const int32_t* sink_len;   // nullable: `sink` first rows in every head
+  int len_all, len_stride;   // len_stride: entries of len and sink_len between samples
+  int stride;                // rows between heads; a length above it is no length
+  long sample_rows;          // rows between samples
+  int sink, window, causal;
+  int samples;               // sets of keys per KV head: S, or 1 for a message
+  int row_samples;           // samples whose query rows read one set: 1, or S for a message
+  // the launch: a workgroup per (set, tile of query rows, range of keys)
+  int nsplit, split0;        // ranges, and the first one's place among the partial results
+  int row_tiles, blocks;
+};
+
+struct AttendArgs {
+  const void* Q;
+  void* O;
+  float* lse;                // nullable
+  long qs, qh, qt, os, oh, ot;   // elements between samples, query heads, queries
+  int S, H, g, T;
+  float scale2;              // log2(e) / sqrt(d)
+  long rows;                 // S * H * g * T query rows; a row's number is its place in lse, [S][H * g][T]
+  float* part_O;             // [ranges][rows][d] and [ranges][rows] (powers of two); used unless there is one range
+  float* part_lse;
+  int ranges;
+  AttendKeys keys[2];
+  int n_keys;
+};
+
+__device__ __forceinline__ float attend_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float attend_log2(float x) { return __builtin_amdgcn_logf(x); }
+
+// Rows of a head: a length that lies outside its storage (the -1 of a message that did not fit among them) counts as none.
+__device__ __forceinline__ int attend_len(const AttendKeys& k, const int sample, const int h) {
+  const int n = k.len ? k.len[(size_t)sample * k.len_stride + h] : k.len_all;
+  return n < 0 || n > k.stride ? 0 : n;
+}
+__device__ __forceinline__ int attend_sink(const AttendKeys& k, const int sample, const int h) {
+  return max(0, k.sink_len ? k.sink_len[(size_t)sample * k.len_stride + h] : k.sink);
+}
+
+// The keys that the query rows at positions pmin .. pmax of a head see: [0, a_end) and [b0, end), in na and nb tiles of TK.
+struct AttendSpan { int a_end, b0, end, na, nb; };
+template <int TK>
+__device__ __forceinline__ AttendSpan attend_span(const AttendKeys& k, const int n, const int sink, const int pmin, const int pmax) {
+  AttendSpan s;
+  s.end = k.causal ? min(n, pmax + 1) : n;
+  s.a_end = 0; s.b0 = 0;
+  if (k.window > 0) {
+    const int lo = pmin - k.window + 1;
+    const int first = min(sink, s.end);
+    if (lo > first) { s.a_end = first; s.b0 = lo; }
+  }
+  s.na = (s.a_end + TK - 1) / TK;
+  s.nb = s.end > s.b0 ? (s.end - s.b0 + TK - 1) / TK : 0;
+  return s;
+}
+
+// Whether the query at position p sees key j (below the head's length).
+__device__ __forceinline__ bool attend_sees(const int causal, const int window, const int sink, const int p, const int j) {
+  return !causal || (j <= p && (window <= 0 || j > p - window || j < sink));
+}
+
+// Query row r of the rows that read a set of keys: query head, query and sample, and the row's number.
+struct AttendRow { int s, gi, t; };
+__device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, const AttendKeys& k, const int set_sample, const int r) {
+  AttendRow w;
+  w.t = r / a.g;
+  w.gi = r - w.t * a.g;
+  w.s = set_sample;
+  if (k.row_samples > 1) { w.s = w.t / a.T; w.t -= w.s * a.T; }
+  return w;
+}
+__device__ __forceinline__ size_t attend_row_number(const AttendArgs& a, const int h, const AttendRow& w) {
+  return ((size_t)w.s * a.H * a.g + (size_t)h * a.g + w.gi) * a.T + w.t;
+}
+
+obf_status_t launch_attend_few(const AttendArgs& a, int d, int dtype, hipStream_t st);
+obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);
+obf_status_t launch_attend_mass(const AttendArgs& a, int d, int dtype, const float* lse, float* mass, hipStream_t st);
+int attend_few_rows(int d, int dtype, long rows_per_set);
+
+struct EvictArgs {
+  const void* K; const void* V; const float* mass; const int32_t* pos;
+  const int32_t* len; const int32_t* sink_len;
+  int heads, len_all, in_stride, budget, recent, sink, out_stride, row_vec;
+  void* K_out; void* V_out; float* mass_out; int32_t* pos_out; int32_t* idx; int32_t* len_out;
+};
+obf_status_t launch_evict(const EvictArgs& a, hipStream_t st);
+
+}  // namespace obf

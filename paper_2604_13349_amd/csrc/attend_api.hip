@@ -1,0 +1,213 @@
+// Entry points of the operators that read and thin out a relayed cache: argument checks, workspace, launches.
+#include "attend.hpp"
+
+namespace obf {
+
+constexpr int kAttendMaxStride = 1 << 24;     // rows between heads
+constexpr int kAttendMaxQueries = 1 << 20;
+constexpr int kAttendMaxGroup = 128;
+
+static bool attend_overlap(const void* a, size_t an, const void* b, size_t bn) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
+}
+
+static obf_status_t check_attend(const obf_attend_t* c) {
+  if (!c) { set_error("attend: descriptor is NULL"); return OBF_ERR_INVALID_ARG; }
+  if (c->n_samples < 1 || c->n_kv_heads < 1 || c->group < 1 || c->n_queries < 1 || c->token_stride < 1) {
+    set_error("attend: n_samples, n_kv_heads, group, n_queries, token_stride must all be >= 1");
+    return OBF_ERR_INVALID_ARG;
+  }
+  if (c->dtype != OBF_F32 && c->dtype != OBF_BF16) { set_error("attend: unknown dtype %d", c->dtype); return OBF_ERR_INVALID_ARG; }
+  if (c->window < 0 || c->sink < 0) { set_error("attend: window and sink must not be negative"); return OBF_ERR_INVALID_ARG; }
+  if (c->window > 0 && !c->causal) { set_error("attend: a window needs causal queries"); return OBF_ERR_INVALID_ARG; }
+  if (c->kv_len_all < 0 || c->kv_len_all > c->token_stride) { set_error("attend: kv_len_all outside [0, token_stride]"); return OBF_ERR_INVALID_ARG; }
+  if (c->len_stride < 0 || (c->len_stride > 0 && c->len_stride < c->n_kv_heads)) { set_error("attend: len_stride below n_kv_heads"); return OBF_ERR_INVALID_ARG; }
+  if (c->sample_stride < 0 || (c->sample_stride > 0 && c->sample_stride < (int64_t)c->n_kv_heads * c->token_stride)) {
+    set_error("attend: sample_stride below n_kv_heads * token_stride");
+    return OBF_ERR_INVALID_ARG;
+  }
+  const int unit = c->dtype == OBF_BF16 ? 8 : 4;
+  for (int i = 0; i < 3; ++i)
+    if (c->q_stride[i] < 0 || c->q_stride[i] % unit || c->o_stride[i] < 0 || c->o_stride[i] % unit) {
+      set_error("attend: strides of Q and O must be multiples of 16 bytes and not negative");
+      return OBF_ERR_INVALID_ARG;
+    }
+  if (c->head_dim != 64 && c->head_dim != 128) { set_error("head_dim %d unsupported (64 or 128)", c->head_dim); return OBF_ERR_UNSUPPORTED; }
+  if (c->token_stride > kAttendMaxStride) { set_error("attend: token_stride above the supported %d", kAttendMaxStride); return OBF_ERR_UNSUPPORTED; }
+  if (c->n_queries > kAttendMaxQueries) { set_error("attend: n_queries above the supported %d", kAttendMaxQueries); return OBF_ERR_UNSUPPORTED; }
+  if (c->group > kAttendMaxGroup) { set_error("attend: group above the supported %d", kAttendMaxGroup); return OBF_ERR_UNSUPPORTED; }
+  if ((int64_t)c->n_samples * c->n_kv_heads > 65535) { set_error("attend: more than 65535 heads in one call"); return OBF_ERR_UNSUPPORTED; }
+  if ((int64_t)c->n_samples * c->n_kv_heads * c->group * c->n_queries > ((int64_t)1 << 28)) {
+    set_error("attend: more than 2^28 query rows in one call");
+    return OBF_ERR_UNSUPPORTED;
+  }
+  if ((int64_t)c->n_samples * c->n_kv_heads * c->token_stride > ((int64_t)1 << 36)) {
+    set_error("attend: more than 2^36 cache rows in one call");
+    return OBF_ERR_UNSUPPORTED;
+  }
+  return OBF_OK;
+}
+
+static obf_status_t check_aligned(const char* name, const void* p) {
+  if (!p) { set_error("%s is NULL", name); return OBF_ERR_INVALID_ARG; }
+  if ((uintptr_t)p & 15) { set_error("%s must be 16-byte aligned", name); return OBF_ERR_INVALID_ARG; }
+  return OBF_OK;
+}
+
+// The launch of one call: sets of keys, tiles, ranges; and the workspace, in the order partial sums, partial normalisers, row normalisers.
+struct AttendPlan { AttendArgs a; size_t part_O, part_lse, lse, total; };
+
+static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
+  AttendPlan p;
+  AttendArgs& a = p.a;
+  a = AttendArgs();
+  a.S = c->n_samples; a.H = c->n_kv_heads; a.g = c->group; a.T = c->n_queries;
+  const long d = c->head_dim, hq = (long)a.H * a.g;
+  const bool qd = c->q_stride[0] || c->q_stride[1] || c->q_stride[2], od = c->o_stride[0] || c->o_stride[1] || c->o_stride[2];
+  a.qs = qd ? c->q_stride[0] : hq * a.T * d; a.qh = qd ? c->q_stride[1] : a.T * d; a.qt = qd ? c->q_stride[2] : d;
+  a.os = od ? c->o_stride[0] : hq * a.T * d; a.oh = od ? c->o_stride[1] : a.T * d; a.ot = od ? c->o_stride[2] : d;
+  a.scale2 = (float)(1.4426950408889634 / (d == 128 ? 11.313708498984761 : 8.0));
+  a.rows = (long)a.S * hq * a.T;
+  a.n_keys = 0;
+  if (prefix_stride > 0) {
+    AttendKeys& k = a.keys[a.n_keys++];
+    k = AttendKeys();
+    k.stride = prefix_stride; k.samples = 1; k.row_samples = a.S;
+  }
+  AttendKeys& k = a.keys[a.n_keys++];
+  k = AttendKeys();
+  k.len_all = c->kv_len_all; k.len_stride = c->len_stride ? c->len_stride : a.H;
+  k.stride = c->token_stride; k.sample_rows = c->sample_stride ? c->sample_stride : (long)a.H * c->token_stride;
+  k.sink = c->sink; k.window = c->window; k.causal = c->causal != 0;
+  k.samples = a.S; k.row_samples = 1;
+  long most = 0, base = 0;
+  for (int i = 0; i < a.n_keys; ++i) { const long r = (long)a.keys[i].row_samples * a.T * a.g; most = r > most ? r : most; }
+  const int tile = attend_few_rows(c->head_dim, c->dtype, most);
+  for (int i = 0; i < a.n_keys; ++i) {
+    AttendKeys& s = a.keys[i];
+    s.row_tiles = (int)(((long)s.row_samples * a.T * a.g + tile - 1) / tile);
+    base += (long)s.row_tiles * s.samples * a.H;
+  }
+  a.ranges = 0;
+  for (int i = 0; i < a.n_keys; ++i) {
+    AttendKeys& s = a.keys[i];
+    const long most_ranges = (s.stride + 255) / 256, want = (2 * kNumCU + base - 1) / base;
+    s.nsplit = (int)(want < most_ranges ? want : most_ranges);
+    s.split0 = a.ranges;
+    a.ranges += s.nsplit;
+    s.blocks = s.row_tiles * s.samples * a.H * s.nsplit;
+  }
+  size_t at = 0;
+  p.part_O = at;
+  if (a.ranges > 1) at += (size_t)a.ranges * a.rows * d * sizeof(float);
+  p.part_lse = at;
+  if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
+  p.lse = at;
+  at += ((size_t)a.rows * sizeof(float) + 255) & ~(size_t)255;
+  p.total = at;
+  return p;
+}
+
+static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
+                               int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
+                               const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, hipStream_t st) {
+  AttendPlan p = plan_attend(c, prefix_stride);
+  if (!ws) { set_error("workspace is NULL"); return OBF_ERR_INVALID_ARG; }
+  if (((uintptr_t)ws & 255) != 0) { set_error("workspace must be 256-byte aligned"); return OBF_ERR_INVALID_ARG; }
+  if (ws_bytes < p.total) { set_error("workspace too small: %zu bytes given, %zu needed", ws_bytes, p.total); return OBF_ERR_WORKSPACE_TOO_SMALL; }
+  AttendArgs& a = p.a;
+  char* base = (char*)ws;
+  if (mass && !lse) lse = (float*)(base + p.lse);
+  a.Q = Q; a.O = O; a.lse = lse;
+  a.part_O = (float*)(base + p.part_O);
+  a.part_lse = (float*)(base + p.part_lse);
+  AttendKeys& own = a.keys[a.n_keys - 1];
+  own.K = K; own.V = V; own.len = kv_len; own.sink_len = sink_len;
+  if (a.n_keys > 1) {
+    AttendKeys& m = a.keys[0];
+    m.K = prefix_K; m.V = prefix_V; m.len = prefix_len; m.len_all = prefix_len_all;
+  }
+  OBF_TRY(launch_attend_few(a, c->head_dim, c->dtype, st));
+  if (a.ranges > 1) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
+  return mass ? launch_attend_mass(a, c->head_dim, c->dtype, lse, mass, st) : OBF_OK;
+}
+
+}  // namespace obf
+
+using namespace obf;
+
+extern "C" {
+
+size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride) {
+  if (check_attend(call) != OBF_OK) return 0;
+  if (prefix_stride < 0 || prefix_stride > kAttendMaxStride) { set_error("attend: prefix_stride outside [0, %d]", kAttendMaxStride); return 0; }
+  return plan_attend(call, prefix_stride).total;
+}
+
+obf_status_t obf_attend(const obf_attend_t* call, const void* Q, const void* K, const void* V, const int32_t* kv_len, const int32_t* sink_len,
+                        void* O, float* lse, float* mass, void* ws, size_t ws_bytes, void* stream) {
+  OBF_TRY(check_attend(call));
+  OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("O", O));
+  return run_attend(call, Q, nullptr, nullptr, nullptr, 0, 0, K, V, kv_len, sink_len, O, lse, mass, ws, ws_bytes, (hipStream_t)stream);
+}
+
+obf_status_t obf_attend_shared(const obf_attend_t* call, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
+                               int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
+                               const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  OBF_TRY(check_attend(call));
+  if (prefix_stride < 1 || prefix_len_all < 0 || prefix_len_all > prefix_stride) {
+    set_error("attend: prefix_stride must be >= 1 and prefix_len_all lie in [0, prefix_stride]");
+    return OBF_ERR_INVALID_ARG;
+  }
+  if (prefix_stride > kAttendMaxStride) { set_error("attend: prefix_stride above the supported %d", kAttendMaxStride); return OBF_ERR_UNSUPPORTED; }
+  OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("prefix_K", prefix_K)); OBF_TRY(check_aligned("prefix_V", prefix_V));
+  OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("O", O));
+  return run_attend(call, Q, prefix_K, prefix_V, prefix_len, prefix_len_all, prefix_stride, K, V, kv_len, sink_len, O, lse, nullptr, ws, ws_bytes,
+                    (hipStream_t)stream);
+}
+
+obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void* K, const float* lse, const int32_t* kv_len,
+                             const int32_t* sink_len, float* mass, void* stream) {
+  OBF_TRY(check_attend(call));
+  OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_NONNULL(lse); OBF_NONNULL(mass);
+  AttendPlan p = plan_attend(call, 0);
+  p.a.Q = Q;
+  p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;
+  return launch_attend_mass(p.a, call->head_dim, call->dtype, lse, mass, (hipStream_t)stream);
+}
+
+obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const void* K, const void* V, const float* mass, const int32_t* pos,
+                       const int32_t* kv_len, int32_t kv_len_all, int32_t in_stride, int32_t budget, int32_t recent, const int32_t* sink_len,
+                       int32_t sink, void* K_out, void* V_out, float* mass_out, int32_t* pos_out, int32_t* idx, int32_t* len_out,
+                       int32_t out_stride, void* stream) {
+  if (n_heads < 1 || n_heads > 65535) { set_error("n_heads must lie in [1, 65535]"); return OBF_ERR_INVALID_ARG; }
+  if (dtype != OBF_F32 && dtype != OBF_BF16) { set_error("unknown dtype %d", dtype); return OBF_ERR_INVALID_ARG; }
+  if (head_dim != 64 && head_dim != 128) { set_error("head_dim %d unsupported (64 or 128)", head_dim); return OBF_ERR_UNSUPPORTED; }
+  if (in_stride < 1 || out_stride < 1) { set_error("in_stride and out_stride must be >= 1"); return OBF_ERR_INVALID_ARG; }
+  if (in_stride > kAttendMaxStride || out_stride > kAttendMaxStride) { set_error("in_stride or out_stride above the supported %d", kAttendMaxStride); return OBF_ERR_UNSUPPORTED; }
+  if (kv_len_all < 0 || kv_len_all > in_stride) { set_error("kv_len_all outside [0, in_stride]"); return OBF_ERR_INVALID_ARG; }
+  if (sink < 0 || recent < 0 || budget < 0) { set_error("budget, recent and sink must not be negative"); return OBF_ERR_INVALID_ARG; }
+  if (recent > budget) { set_error("recent %d above budget %d", recent, budget); return OBF_ERR_INVALID_ARG; }
+  const int64_t most = (int64_t)budget + (sink_len ? 0 : sink);
+  if ((most < in_stride ? most : in_stride) > out_stride) { set_error("budget and sink exceed out_stride %d", out_stride); return OBF_ERR_INVALID_ARG; }
+  OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("K_out", K_out)); OBF_TRY(check_aligned("V_out", V_out));
+  OBF_NONNULL(mass); OBF_NONNULL(mass_out); OBF_NONNULL(idx); OBF_NONNULL(len_out);
+  if (!pos != !pos_out) { set_error("pos and pos_out come together"); return OBF_ERR_INVALID_ARG; }
+  const size_t row = (size_t)head_dim * (dtype == OBF_BF16 ? 2 : 4);
+  const size_t in = (size_t)n_heads * in_stride, out = (size_t)n_heads * out_stride;
+  if (attend_overlap(K, in * row, K_out, out * row) || attend_overlap(K, in * row, V_out, out * row) || attend_overlap(V, in * row, K_out, out * row) ||
+      attend_overlap(V, in * row, V_out, out * row) || attend_overlap(K_out, out * row, V_out, out * row) ||
+      attend_overlap(mass, in * 4, mass_out, out * 4) || attend_overlap(pos, in * 4, pos_out, out * 4)) {
+    set_error("outputs must not overlap the caches they are taken from");
+    return OBF_ERR_INVALID_ARG;
+  }
+  if (kv_len && attend_overlap(kv_len, (size_t)n_heads * 4, len_out, (size_t)n_heads * 4)) { set_error("len_out must not overlap kv_len"); return OBF_ERR_INVALID_ARG; }
+  EvictArgs a;
+  a.K = K; a.V = V; a.mass = mass; a.pos = pos; a.len = kv_len; a.sink_len = sink_len;
+  a.heads = n_heads; a.len_all = kv_len_all; a.in_stride = in_stride; a.budget = budget; a.recent = recent; a.sink = sink; a.out_stride = out_stride;
+  a.row_vec = (int)(row / 16);
+  a.K_out = K_out; a.V_out = V_out; a.mass_out = mass_out; a.pos_out = pos_out; a.idx = idx; a.len_out = len_out;
+  return launch_evict(a, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,235 @@
+// Attention of few query rows per KV head (generation: the group's query heads, a handful of queries), and of any number for fp32 caches.
+//
+//   O_r = sum_j exp(x_rj - lse_r) V_j,  x_rj = q_r . k_j / sqrt(d) over the visible keys j,  lse_r = log sum_j exp(x_rj)
+//
+// One pass over K and V: every wave takes tiles of 32 keys, holds the running maximum m and sum l of its query rows and
+// O' = sum_j 2^(x_rj - m) V_j; the waves of a workgroup, and then the ranges of keys of a head, are joined by their maxima.
+// A tile's products are K Q^T (keys by rows, so that a lane holds four keys of one query row) and V^T P^T: the first one's result has the
+// lane layout of the second one's operand, and V, read row by row in full lines, becomes the other operand by byte permutes inside the lane.
+// Nothing passes through LDS before the end.  m follows the maximum only where that outgrows it by 2^8 (the sums have room for that), so that
+// most tiles need no exchange between lanes.
+// bf16: P is split into two bf16 parts, each with its own product, so that it keeps 16 bits; the matrix pipe has the room where the caches' bytes bound
+// the kernel.  fp32: all products by v_mfma_f32_16x16x4_f32.
+#include "attend_few.hpp"
+
+namespace obf {
+
+template <typename ET, int D, int NB, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
+  typedef FewTile<ET, D> Tile;
+  constexpr int DB = Tile::DB, ROWS = 16 * NB;
+  __shared__ __attribute__((aligned(16))) float sm_o[NW][ROWS][D];
+  __shared__ float sm_m[NW][ROWS], sm_l[NW][ROWS];
+  // which set of keys, tile of rows and range of keys
+  int block = blockIdx.x;
+  const bool second = block >= a.keys[0].blocks;
+  const AttendKeys& k = a.keys[second ? 1 : 0];
+  if (second) block -= a.keys[0].blocks;
+  const int split = block % k.nsplit;
+  block /= k.nsplit;
+  const int row_tile = block % k.row_tiles, set = block / k.row_tiles;
+  const int h = set % a.H, ks = set / a.H;
+  const int set_rows = k.row_samples * a.T * a.g;
+  const int row0 = row_tile * ROWS;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
+  const int n = attend_len(k, ks, h), sink = attend_sink(k, ks, h);
+  // (a message is not causal: its queries have no positions)
+  const int pmin = n - a.T + row0 / a.g, pmax = n - a.T + (min(row0 + ROWS, set_rows) - 1) / a.g;
+  const AttendSpan span = attend_span<32>(k, n, sink, pmin, pmax);
+  const int tiles = span.na + span.nb, per = max(NW, (tiles + k.nsplit - 1) / k.nsplit);   // (a short head does not use all its ranges)
+  const int first = split * per, behind = min(tiles, first + per);
+  const bool joined = a.ranges > 1;
+  const ET* K = (const ET*)k.K + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
+  const ET* V = (const ET*)k.V + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
+
+  typename Tile::Query q[NB];
+  int pos[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const AttendRow w = attend_row(a, k, ks, min(row0 + 16 * nb + (lane & 15), set_rows - 1));
+    Tile::load_query(q[nb], (const ET*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt, lane);
+    pos[nb] = n - a.T + w.t;
+  }
+  f32x4 o[NB][DB];
+  float m[NB], l[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    m[nb] = -INFINITY; l[nb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  for (int i = first + wave; i < behind; i += NW) {
+    const bool in_a = i < span.na;
+    const int base = in_a ? 32 * i : span.b0 + 32 * (i - span.na), end = in_a ? span.a_end : span.end;
+    typename Tile::Keys kf;
+    typename Tile::Vals vf;
+    Tile::load_keys(kf, K, base, end - 1, lane);
+    Tile::load_vals(vf, V, base, end - 1, lane);
+    // some row does not see some key of the tile
+    const bool cut = base + 32 > end || (k.causal && (base + 31 > pmin || (k.window > 0 && base <= pmax - k.window && base + 31 >= sink)));
+    float p[NB][2][4];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      f32x4 x[2];
+      Tile::scores(x, kf, q[nb]);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float v = x[b][r] * a.scale2;
+          const int j = base + 16 * b + 4 * quad + r;
+          if (cut && !(j < end && attend_sees(k.causal, k.window, sink, pos[nb], j))) v = -INFINITY;
+          x[b][r] = v;
+          mx = fmaxf(mx, v);
+        }
+      if (__any(mx > m[nb] + kAttendSlack)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float next = fmaxf(m[nb], mx);
+        const float f = next > -INFINITY ? attend_exp2(m[nb] - next) : 1.f;
+        m[nb] = next;
+        l[nb] *= f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[nb][db] *= f;
+      }
+      const float ref = m[nb] > -INFINITY ? m[nb] : 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { p[nb][b][r] = attend_exp2(x[b][r] - ref); l[nb] += p[nb][b][r]; }
+    }
+    // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
+    if (cut && k.causal && a.T > 1 && __any(Tile::not_finite(vf))) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            for (int qd = 0; qd < 4; ++qd) {
+              const int j = base + 16 * b + 4 * qd + r;
+              const float w = __shfl(p[nb][b][r], 16 * qd + (lane & 15));
+              if (j < end && attend_sees(k.causal, k.window, sink, pos[nb], j)) {
+                const ET* row = V + (size_t)j * D;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                  for (int c = 0; c < 4; ++c) o[nb][db][c] = fmaf(w, Tile::value(row, Tile::channel(quad, db, c)), o[nb][db][c]);
+              }
+            }
+    } else {
+      Tile::template values<NB>(o, vf, p);
+    }
+  }
+
+  // the waves' parts
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    l[nb] += __shfl_xor(l[nb], 16);
+    l[nb] += __shfl_xor(l[nb], 32);
+    const int r = 16 * nb + (lane & 15);
+    if (quad == 0) { sm_m[wave][r] = m[nb]; sm_l[wave][r] = l[nb]; }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sm_o[wave][r][Tile::channel(quad, db, c)] = o[nb][db][c];
+  }
+  __syncthreads();
+  constexpr int PIECES = D / 4;
+  for (int e = threadIdx.x; e < ROWS * PIECES; e += NW * 64) {
+    const int r = e / PIECES, c = (e % PIECES) * 4;
+    if (row0 + r >= set_rows) break;
+    float top = sm_m[0][r];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][r]);
+    const float ref = top > -INFINITY ? top : 0.f;
+    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = attend_exp2(sm_m[w][r] - ref);
+      sum = fmaf(f, sm_l[w][r], sum);
+      const float4 x = *(const float4*)&sm_o[w][r][c];
+      v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
+    }
+    const float inv = top > -INFINITY ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = top > -INFINITY ? v[i] * inv : 0.f;
+    const float lse2 = top > -INFINITY ? top + attend_log2(sum) : -INFINITY;
+    const AttendRow w = attend_row(a, k, ks, row0 + r);
+    const size_t number = attend_row_number(a, h, w);
+    if (joined) {
+      const size_t at = (size_t)(k.split0 + split) * a.rows + number;
+      if (c == 0) a.part_lse[at] = lse2;
+      if (top > -INFINITY) *(float4*)(a.part_O + at * D + c) = make_float4(v[0], v[1], v[2], v[3]);   // (nobody reads the others)
+    } else {
+      if (c == 0 && a.lse) a.lse[number] = lse2 * 0.69314718055994531f;
+      store4((ET*)a.O + (size_t)w.s * a.os + (size_t)(h * a.g + w.gi) * a.oh + (size_t)w.t * a.ot + c, v);
+    }
+  }
+}
+
+// Joins the ranges of a query row: O = sum_i 2^(lse_i - lse) O_i.  A lane has four channels; bound by the partial results' bytes.
+template <typename ET, int D>
+__global__ __launch_bounds__(256) void k_attend_join(const AttendArgs a) {
+  constexpr int PIECES = D / 4;
+  const size_t row = (size_t)blockIdx.x * (256 / PIECES) + threadIdx.x / PIECES;
+  const int c = (threadIdx.x % PIECES) * 4;
+  if (row >= (size_t)a.rows) return;
+  float top = -INFINITY;
+  for (int i = 0; i < a.ranges; ++i) top = fmaxf(top, a.part_lse[(size_t)i * a.rows + row]);
+  float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (top > -INFINITY) {
+    for (int i = 0; i < a.ranges; ++i) {
+      const size_t at = (size_t)i * a.rows + row;
+      const float part = a.part_lse[at];
+      if (!(part > -INFINITY)) continue;
+      const float f = attend_exp2(part - top);
+      const float4 x = *(const float4*)(a.part_O + at * D + c);
+      sum += f;
+      v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] /= sum;
+  }
+  const int t = (int)(row % a.T), hq = (int)(row / a.T % ((size_t)a.H * a.g)), s = (int)(row / a.T / ((size_t)a.H * a.g));
+  if (c == 0 && a.lse) a.lse[row] = top > -INFINITY ? (top + attend_log2(sum)) * 0.69314718055994531f : -INFINITY;
+  store4((ET*)a.O + (size_t)s * a.os + (size_t)hq * a.oh + (size_t)t * a.ot + c, v);
+}
+
+// Query rows of a workgroup's tile.
+int attend_few_rows(int d, int dtype, long rows_per_set) { (void)d; (void)dtype; return rows_per_set <= 16 ? 16 : 32; }
+
+template <typename ET, int D>
+static void few_launch(const AttendArgs& a, int rows, hipStream_t st) {
+  const int blocks = a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0);
+  if (rows == 16) hipLaunchKernelGGL((k_attend_few<ET, D, 1, 4>), dim3(blocks), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_attend_few<ET, D, 2, 2>), dim3(blocks), dim3(128), 0, st, a);
+}
+
+obf_status_t launch_attend_few(const AttendArgs& a, int d, int dtype, hipStream_t st) {
+  ProfScope prof(ST_ATTEND, st);
+  long most = 0;
+  for (int i = 0; i < a.n_keys; ++i) { const long r = (long)a.keys[i].row_samples * a.T * a.g; most = r > most ? r : most; }
+  const int rows = attend_few_rows(d, dtype, most);
+  if (dtype == OBF_BF16) { if (d == 128) few_launch<uint16_t, 128>(a, rows, st); else few_launch<uint16_t, 64>(a, rows, st); }
+  else { if (d == 128) few_launch<float, 128>(a, rows, st); else few_launch<float, 64>(a, rows, st); }
+  return check_launch("attend");
+}
+
+obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st) {
+  ProfScope prof(ST_ATTEND_JOIN, st);
+  const int per = 256 / (d / 4);
+  const dim3 grid((unsigned)((a.rows + per - 1) / per));
+  if (dtype == OBF_BF16) {
+    if (d == 128) hipLaunchKernelGGL((k_attend_join<uint16_t, 128>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_attend_join<uint16_t, 64>), grid, dim3(256), 0, st, a);
+  } else {
+    if (d == 128) hipLaunchKernelGGL((k_attend_join<float, 128>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_attend_join<float, 64>), grid, dim3(256), 0, st, a);
+  }
+  return check_launch("attend join");
+}
+
+}  // namespace obf

@@ -238,8 +238,12 @@ inline Workspace carve(const Dims& m, int max_budget, int rank) {
 
 enum Stage {
   ST_SCORE_STATS = 0, ST_SCORE_LSE, ST_SCORE_MASS, ST_SELECT, ST_REFINE, ST_GATHER, ST_KEEP_CERT, ST_KEEP_BASIS, ST_DEL_STATS,
-  ST_FINALIZE, ST_BASIS_STATS, ST_COUNT
+  ST_FINALIZE, ST_BASIS_STATS, ST_ATTEND, ST_ATTEND_JOIN, ST_ATTEND_MASS, ST_EVICT, ST_COUNT
 };
+
+// Entry points (inside namespace obf, or with it opened): leave with the status of a failed step; refuse a NULL argument.
+#define OBF_TRY(expr) do { obf_status_t _s = (expr); if (_s != OBF_OK) return _s; } while (0)
+#define OBF_NONNULL(p) do { if (!(p)) { set_error(#p " is NULL"); return OBF_ERR_INVALID_ARG; } } while (0)
 
 // Brackets one kernel launch with HIP events when profiling of that stage is enabled.
 struct ProfScope {

@@ -1,0 +1,133 @@
+// Eviction by accumulated attention weight: per head the first rows, the newest rows and the rows of the largest mass are kept, in their order.
+//
+// First launch, a workgroup per head: the mass of the last row that is kept, by histograms of an order-preserving integer image of the masses
+// (2048 bins over the range that can still hold it), then the list of kept rows by a prefix count.  All decisions are integer compares: exact, ties to
+// the lowest index.  Second launch: the kept rows of K and V in 16-byte pieces, their masses and positions.
+#include "attend.hpp"
+
+namespace obf {
+
+constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048;
+
+// larger float <=> larger key
+__device__ __forceinline__ uint32_t mass_key(const float f) {
+  const uint32_t u = __float_as_uint(f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+__global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) {
+  __shared__ int hist[EV_BINS];
+  __shared__ uint32_t wlo[EV_WAVES], whi[EV_WAVES];
+  __shared__ int wgt[EV_WAVES], weq[EV_WAVES];
+  __shared__ int s_bin, s_above;
+  const int head = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int32_t* out = a.idx + (size_t)head * a.out_stride;
+  const int n = a.len ? a.len[head] : a.len_all;
+  const int first = min(max(0, a.sink_len ? a.sink_len[head] : a.sink), max(n, 0));
+  const int kept = first + min(a.budget, n - first);
+  if (n < 0 || n > a.in_stride || kept > a.out_stride) {            // no length, or no room: flagged, nothing of the head is written
+    for (int i = tid; i < a.out_stride; i += EV_THREADS) out[i] = -1;
+    if (tid == 0) a.len_out[head] = -1;
+    return;
+  }
+  if (tid == 0) a.len_out[head] = kept;
+  for (int i = kept + tid; i < a.out_stride; i += EV_THREADS) out[i] = -1;
+  if (kept == n) {
+    for (int i = tid; i < n; i += EV_THREADS) out[i] = i;
+    return;
+  }
+  const int last = n - a.recent, want = a.budget - a.recent;        // of the rows first .. last - 1 the `want` of largest mass are kept
+  for (int i = tid; i < first; i += EV_THREADS) out[i] = i;
+  for (int i = tid; i < a.recent; i += EV_THREADS) out[first + want + i] = last + i;
+  if (want == 0) return;
+  const float* mass = a.mass + (size_t)head * a.in_stride;
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  for (int i = first + tid; i < last; i += EV_THREADS) { const uint32_t k = mass_key(mass[i]); lo = min(lo, k); hi = max(hi, k); }
+  for (int off = 32; off > 0; off >>= 1) { lo = min(lo, (uint32_t)__shfl_xor((int)lo, off)); hi = max(hi, (uint32_t)__shfl_xor((int)hi, off)); }
+  if (lane == 0) { wlo[wave] = lo; whi[wave] = hi; }
+  __syncthreads();
+  lo = 0xffffffffu; hi = 0u;
+  for (int w = 0; w < EV_WAVES; ++w) { lo = min(lo, wlo[w]); hi = max(hi, whi[w]); }
+  int need = want;                                                  // rank wanted among the keys of [lo, hi]
+  while (lo < hi) {                                                 // uniform
+    const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);      // (hi - lo) >> shift < EV_BINS
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
+    __syncthreads();
+    for (int i = first + tid; i < last; i += EV_THREADS) {
+      const uint32_t o = mass_key(mass[i]) - lo;                    // keys below the range wrap to above it
+      if (o <= hi - lo) atomicAdd(&hist[o >> shift], 1);
+    }
+    __syncthreads();
+    // from the top: this thread's bins are top and top - 1
+    const int top = EV_BINS - 1 - 2 * tid;
+    const int c0 = hist[top], c1 = hist[top - 1];
+    int inc = c0 + c1;
+    for (int off = 1; off < 64; off <<= 1) { const int x = __shfl_up(inc, off); if (lane >= off) inc += x; }
+    if (lane == 63) wgt[wave] = inc;
+    __syncthreads();
+    int before = inc - c0 - c1;
+    for (int w = 0; w < wave; ++w) before += wgt[w];
+    if (before < need && need <= before + c0) { s_bin = top; s_above = before; }
+    else if (before + c0 < need && need <= before + c0 + c1) { s_bin = top - 1; s_above = before + c0; }
+    __syncthreads();
+    need -= s_above;
+    const uint64_t bin_top = (uint64_t)lo + (((uint64_t)s_bin + 1u) << shift) - 1u;
+    if (bin_top < (uint64_t)hi) hi = (uint32_t)bin_top;
+    lo += (uint32_t)s_bin << shift;
+    __syncthreads();                                                // s_bin, hist and wgt are written again
+  }
+  // keys above lo are kept; of those equal to it the first `need`
+  int at = first, equal = 0;                                        // rows kept, and rows equal to lo, before this chunk
+  for (int c = first; c < last; c += EV_THREADS) {
+    const int i = c + tid;
+    const uint32_t k = i < last ? mass_key(mass[i]) : 0u;
+    const bool gt = i < last && k > lo, eq = i < last && k == lo;
+    const uint64_t bg = __ballot(gt), be = __ballot(eq), under = (1ull << lane) - 1ull;
+    if (lane == 0) { wgt[wave] = __popcll(bg); weq[wave] = __popcll(be); }
+    __syncthreads();
+    int g = __popcll(bg & under), e = equal + __popcll(be & under), tg = 0, te = 0;
+    for (int w = 0; w < EV_WAVES; ++w) { if (w < wave) { g += wgt[w]; e += weq[w]; } tg += wgt[w]; te += weq[w]; }
+    // kept rows before this one: the larger ones, and of the equal ones as many as were still needed
+    const int eq_before = min(e, need) - min(equal, need);
+    if (gt || (eq && e < need)) out[at + g + eq_before] = i;
+    at += tg + min(equal + te, need) - min(equal, need);
+    equal += te;
+    __syncthreads();
+  }
+}
+
+constexpr int EG_THREADS = 256, EG_UNROLL = 4;
+
+__global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictArgs a) {
+  const int head = blockIdx.y, per = EG_THREADS / a.row_vec, c = threadIdx.x % a.row_vec;
+  const int r0 = blockIdx.x * per * EG_UNROLL + threadIdx.x / a.row_vec;
+  const int n = a.len_out[head];
+  const uint4* K = (const uint4*)a.K;
+  const uint4* V = (const uint4*)a.V;
+  int j[EG_UNROLL];
+  uint4 kv[EG_UNROLL], vv[EG_UNROLL];
+#pragma unroll
+  for (int u = 0; u < EG_UNROLL; ++u) { const int r = r0 + u * per; j[u] = r < n ? a.idx[(size_t)head * a.out_stride + r] : -1; }
+#pragma unroll
+  for (int u = 0; u < EG_UNROLL; ++u)
+    if (j[u] >= 0) { const size_t s = ((size_t)head * a.in_stride + j[u]) * a.row_vec + c; kv[u] = K[s]; vv[u] = V[s]; }
+#pragma unroll
+  for (int u = 0; u < EG_UNROLL; ++u)
+    if (j[u] >= 0) {
+      const size_t row = (size_t)head * a.out_stride + r0 + u * per, from = (size_t)head * a.in_stride + j[u];
+      ((uint4*)a.K_out)[row * a.row_vec + c] = kv[u];
+      ((uint4*)a.V_out)[row * a.row_vec + c] = vv[u];
+      if (c == 0) a.mass_out[row] = a.mass[from];
+      if (c == 1 && a.pos) a.pos_out[row] = a.pos[from];
+    }
+}
+
+obf_status_t launch_evict(const EvictArgs& a, hipStream_t st) {
+  ProfScope prof(ST_EVICT, st);
+  hipLaunchKernelGGL(k_evict_select, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
+  const int per = EG_THREADS / a.row_vec * EG_UNROLL;
+  hipLaunchKernelGGL(k_evict_rows, dim3((a.out_stride + per - 1) / per, a.heads), dim3(EG_THREADS), 0, st, a);
+  return check_launch("evict");
+}
+
+}  // namespace obf
