@@ -37,10 +37,20 @@ struct AttendArgs {
   int ranges;
   AttendKeys keys[2];
   int n_keys;
+  int fused;                 // a workgroup goes over both sets (the message first): keys[1] describes the launch
 };
+
+constexpr float kAttendSlack = 8.f;      // powers of two by which a row's terms may pass its reference
 
 __device__ __forceinline__ float attend_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float attend_log2(float x) { return __builtin_amdgcn_logf(x); }
+
+// The same in every lane of the wave, in a scalar register.
+__device__ __forceinline__ int attend_uniform(const int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const void* attend_uniform(const void* p) {
+  const uint64_t u = (uint64_t)p;
+  return (const void*)((uint64_t)(uint32_t)attend_uniform((int)(uint32_t)u) | (uint64_t)(uint32_t)attend_uniform((int)(uint32_t)(u >> 32)) << 32);
+}
 
 // Rows of a head: a length that lies outside its storage (the -1 of a message that did not fit among them) counts as none.
 __device__ __forceinline__ int attend_len(const AttendKeys& k, const int sample, const int h) {
@@ -87,10 +97,12 @@ __device__ __forceinline__ size_t attend_row_number(const AttendArgs& a, const i
   return ((size_t)w.s * a.H * a.g + (size_t)h * a.g + w.gi) * a.T + w.t;
 }
 
-obf_status_t launch_attend_few(const AttendArgs& a, int d, int dtype, hipStream_t st);
+constexpr int kAttendFewRows = 32;    // query rows per set of keys up to which the waves read the keys straight into registers
+constexpr int kAttendTileRows = 128;
+obf_status_t launch_attend_few(const AttendArgs& a, int tile_rows, int d, int dtype, hipStream_t st);
+obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);
 obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);
 obf_status_t launch_attend_mass(const AttendArgs& a, int d, int dtype, const float* lse, float* mass, hipStream_t st);
-int attend_few_rows(int d, int dtype, long rows_per_set);
 
 struct EvictArgs {
   const void* K; const void* V; const float* mass; const int32_t* pos;

@@ -54,8 +54,13 @@ static obf_status_t check_aligned(const char* name, const void* p) {
   return OBF_OK;
 }
 
-// The launch of one call: sets of keys, tiles, ranges; and the workspace, in the order partial sums, partial normalisers, row normalisers.
-struct AttendPlan { AttendArgs a; size_t part_O, part_lse, lse, total; };
+// The launch of one call: which kernel goes over which set of keys, tiles, ranges; and the workspace, in the order partial sums, partial normalisers, row
+// normalisers.
+struct AttendPlan {
+  AttendArgs a;
+  int tile_rows[2];            // query rows of a workgroup's tile, by set of keys; kAttendTileRows: the kernel of many rows
+  size_t part_O, part_lse, lse, total;
+};
 
 static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   AttendPlan p;
@@ -80,22 +85,23 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   k.stride = c->token_stride; k.sample_rows = c->sample_stride ? c->sample_stride : (long)a.H * c->token_stride;
   k.sink = c->sink; k.window = c->window; k.causal = c->causal != 0;
   k.samples = a.S; k.row_samples = 1;
-  long most = 0, base = 0;
-  for (int i = 0; i < a.n_keys; ++i) { const long r = (long)a.keys[i].row_samples * a.T * a.g; most = r > most ? r : most; }
-  const int tile = attend_few_rows(c->head_dim, c->dtype, most);
+  const long own_rows = (long)a.T * a.g;
+  // A sample's queries fill tiles of many rows by themselves: one pass over the message and the own rows, no partial results of the message.
+  a.fused = a.n_keys > 1 && c->dtype == OBF_BF16 && own_rows > kAttendFewRows;
   for (int i = 0; i < a.n_keys; ++i) {
-    AttendKeys& s = a.keys[i];
-    s.row_tiles = (int)(((long)s.row_samples * a.T * a.g + tile - 1) / tile);
-    base += (long)s.row_tiles * s.samples * a.H;
+    const long r = a.keys[i].row_samples * own_rows;
+    p.tile_rows[i] = c->dtype == OBF_BF16 && r > kAttendFewRows ? kAttendTileRows : r > 16 ? 32 : 16;
   }
   a.ranges = 0;
-  for (int i = 0; i < a.n_keys; ++i) {
+  for (int i = a.fused ? 1 : 0; i < a.n_keys; ++i) {
     AttendKeys& s = a.keys[i];
-    const long most_ranges = (s.stride + 255) / 256, want = (2 * kNumCU + base - 1) / base;
+    s.row_tiles = (int)((s.row_samples * own_rows + p.tile_rows[i] - 1) / p.tile_rows[i]);
+    const long blocks = (long)s.row_tiles * s.samples * a.H, rows = s.stride + (a.fused ? a.keys[0].stride : 0);
+    const long most_ranges = (rows + 255) / 256, want = (2 * kNumCU + blocks - 1) / blocks;
     s.nsplit = (int)(want < most_ranges ? want : most_ranges);
     s.split0 = a.ranges;
     a.ranges += s.nsplit;
-    s.blocks = s.row_tiles * s.samples * a.H * s.nsplit;
+    s.blocks = (int)(blocks * s.nsplit);
   }
   size_t at = 0;
   p.part_O = at;
@@ -106,6 +112,20 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   at += ((size_t)a.rows * sizeof(float) + 255) & ~(size_t)255;
   p.total = at;
   return p;
+}
+
+static obf_status_t launch_plan(const AttendPlan& p, int d, int dtype, hipStream_t st) {
+  if (p.a.fused) return launch_attend_tile(p.a, d, st);
+  if (p.a.n_keys == 1 || p.tile_rows[0] == p.tile_rows[1])
+    return p.tile_rows[0] == kAttendTileRows ? launch_attend_tile(p.a, d, st) : launch_attend_few(p.a, p.tile_rows[0], d, dtype, st);
+  for (int i = 0; i < 2; ++i) {
+    AttendArgs one = p.a;
+    one.n_keys = 1;
+    one.keys[0] = p.a.keys[i];
+    if (p.tile_rows[i] == kAttendTileRows) OBF_TRY(launch_attend_tile(one, d, st));
+    else OBF_TRY(launch_attend_few(one, p.tile_rows[i], d, dtype, st));
+  }
+  return OBF_OK;
 }
 
 static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
@@ -127,7 +147,7 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
     AttendKeys& m = a.keys[0];
     m.K = prefix_K; m.V = prefix_V; m.len = prefix_len; m.len_all = prefix_len_all;
   }
-  OBF_TRY(launch_attend_few(a, c->head_dim, c->dtype, st));
+  OBF_TRY(launch_plan(p, c->head_dim, c->dtype, st));
   if (a.ranges > 1) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
   return mass ? launch_attend_mass(a, c->head_dim, c->dtype, lse, mass, st) : OBF_OK;
 }

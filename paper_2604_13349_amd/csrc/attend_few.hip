@@ -198,9 +198,6 @@ __global__ __launch_bounds__(256) void k_attend_join(const AttendArgs a) {
   store4((ET*)a.O + (size_t)s * a.os + (size_t)hq * a.oh + (size_t)t * a.ot + c, v);
 }
 
-// Query rows of a workgroup's tile.
-int attend_few_rows(int d, int dtype, long rows_per_set) { (void)d; (void)dtype; return rows_per_set <= 16 ? 16 : 32; }
-
 template <typename ET, int D>
 static void few_launch(const AttendArgs& a, int rows, hipStream_t st) {
   const int blocks = a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0);
@@ -208,11 +205,9 @@ static void few_launch(const AttendArgs& a, int rows, hipStream_t st) {
   else hipLaunchKernelGGL((k_attend_few<ET, D, 2, 2>), dim3(blocks), dim3(128), 0, st, a);
 }
 
-obf_status_t launch_attend_few(const AttendArgs& a, int d, int dtype, hipStream_t st) {
+// rows: of a workgroup's tile, 16 or 32
+obf_status_t launch_attend_few(const AttendArgs& a, int rows, int d, int dtype, hipStream_t st) {
   ProfScope prof(ST_ATTEND, st);
-  long most = 0;
-  for (int i = 0; i < a.n_keys; ++i) { const long r = (long)a.keys[i].row_samples * a.T * a.g; most = r > most ? r : most; }
-  const int rows = attend_few_rows(d, dtype, most);
   if (dtype == OBF_BF16) { if (d == 128) few_launch<uint16_t, 128>(a, rows, st); else few_launch<uint16_t, 64>(a, rows, st); }
   else { if (d == 128) few_launch<float, 128>(a, rows, st); else few_launch<float, 64>(a, rows, st); }
   return check_launch("attend");

@@ -4,8 +4,6 @@
 
 namespace obf {
 
-constexpr float kAttendSlack = 8.f;      // powers of two by which a row's terms may pass its reference
-
 template <typename ET, int D> struct FewTile;
 
 // bf16: operands of v_mfma_f32_16x16x32_bf16, lane l: row l % 16, elements 8 (l / 16) .. + 7 of 32

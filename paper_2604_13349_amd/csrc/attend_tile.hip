@@ -1,0 +1,249 @@
+// Attention of many query rows per KV head, bf16: prompts, and the rows of all samples against a shared message.
+//
+//   O_r = sum_j exp(x_rj - lse_r) V_j,  x_rj = q_r . k_j / sqrt(d) over the visible keys j,  lse_r = log sum_j exp(x_rj)
+//
+// A workgroup has 128 query rows (queries by the query heads of the group, so that the heads share the keys), a wave 32 of them.  K and V pass through
+// LDS in tiles of 64 keys, two of them there: the loads of the next one, straight to LDS, run beside the products of the present one.  A wave takes
+// K Q^T (keys by rows: a lane holds half the keys of one query row, so that the running maximum and sum need no exchange between lanes), the terms
+// 2^(x - m), and V^T P^T, whose operand P^T is the first product's result as it lies in its lanes; V's operand is read from LDS transposed
+// (ds_read_b64_tr_b16).  m follows the row's maximum only where that outgrows it by 2^8.
+// Pieces of 16 bytes (K) and 64 bytes (V) of a row lie in LDS permuted by the row's number, so that the operand reads use all banks.
+// P is rounded to bf16, 2^-9 of a weight at most: at this many rows the matrix pipe bounds the kernel, and the result is rounded as coarsely.
+#include "attend.hpp"
+#include "lds_load.hpp"
+
+namespace obf {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+
+constexpr int AT_WAVES = 4, AT_THREADS = AT_WAVES * 64, AT_ROWS = AT_WAVES * 32, AT_KEYS = 64;
+static_assert(AT_ROWS == kAttendTileRows, "rows of a workgroup's tile");
+
+union TileFrag { uint4 u; bf16x8 v; s16x4 h[2]; uint32_t w[4]; };
+
+// Places in a tile of rows of 2 D bytes.
+template <int D> __device__ __forceinline__ int place_k(const int row, const int piece) {       // 16-byte pieces
+  return row * 2 * D + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
+}
+template <int D> __device__ __forceinline__ int swap_v(const int row) { return D == 128 ? row & 3 : (row >> 1) & 1; }   // of 64-byte pieces
+
+// 64 rows of K (or V) from Kt on (rows past `last` repeat it) to LDS.
+template <int D, bool VALUES>
+__device__ __forceinline__ void tile_fill(const uint32_t lds, const uint16_t* Kt, const int last, const int wave, const int lane) {
+  constexpr int PIECES = D / 8, LOADS = AT_KEYS * PIECES / AT_THREADS, ROWS = AT_THREADS / PIECES;   // rows per load of the workgroup
+  uint32_t off[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int at = wave * 64 + lane, row = i * ROWS + at / PIECES, place = at % PIECES;
+    const int piece = VALUES ? place ^ (swap_v<D>(row) << 2) : place ^ (D == 128 ? row & 15 : (row >> 1) & 7);
+    off[i] = (uint32_t)(min(row, last) * 2 * D + piece * 16);
+  }
+  load_to_lds(lds + wave * 1024, off, attend_uniform(Kt));
+}
+
+template <int D>
+__global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs a) {
+  constexpr int KK = D / 16, DB = D / 32, TILE = AT_KEYS * D * 2;
+  __shared__ __attribute__((aligned(1024))) char sm[4 * TILE];          // K, K, V, V
+  // set of keys, tile of rows and range of keys; the sets go round the dies, the rows with the most keys first
+  int block = blockIdx.x;
+  const bool second = a.fused || block >= a.keys[0].blocks;
+  const AttendKeys& k = a.keys[second ? 1 : 0];
+  if (second && !a.fused) block -= a.keys[0].blocks;
+  const int sets = k.samples * a.H, round = sets & 7 ? sets & -sets : 8, per_set = k.row_tiles * k.nsplit;
+  const int set = block % round + round * (block / (round * per_set));
+  const int within = block / round % per_set;
+  const int split = within % k.nsplit, row_tile = k.row_tiles - 1 - within / k.nsplit;
+  const int h = set % a.H, ks = set / a.H;
+  const int set_rows = k.row_samples * a.T * a.g;
+  const int row0 = row_tile * AT_ROWS;
+  const int lane = threadIdx.x & 63, wave = attend_uniform(threadIdx.x >> 6), half = lane >> 5;
+  const int n = attend_uniform(attend_len(k, ks, h)), sink = attend_uniform(attend_sink(k, ks, h));
+  const int pmin = n - a.T + row0 / a.g, pmax = n - a.T + (min(row0 + AT_ROWS, set_rows) - 1) / a.g;
+  const AttendSpan span = attend_span<AT_KEYS>(k, n, sink, pmin, pmax);
+  const int front = a.fused ? attend_uniform(attend_len(a.keys[0], 0, h)) : 0, front_tiles = (front + AT_KEYS - 1) / AT_KEYS;
+  const int tiles = front_tiles + span.na + span.nb, per = (tiles + k.nsplit - 1) / k.nsplit;
+  const int first = split * per, behind = min(tiles, first + per);
+  const uint16_t* K = (const uint16_t*)k.K + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
+  const uint16_t* V = (const uint16_t*)k.V + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
+  const uint16_t* FK = a.fused ? (const uint16_t*)a.keys[0].K + (size_t)h * a.keys[0].stride * D : K;
+  const uint16_t* FV = a.fused ? (const uint16_t*)a.keys[0].V + (size_t)h * a.keys[0].stride * D : V;
+
+  const int r = row0 + wave * 32 + (lane & 31);
+  const AttendRow w = attend_row(a, k, ks, min(r, set_rows - 1));
+  const uint16_t* qrow = (const uint16_t*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt;
+  const int pos = n - a.T + w.t;
+  // the wave's own rows
+  const int wmin = n - a.T + min(row0 + wave * 32, set_rows - 1) / a.g, wmax = n - a.T + min(row0 + wave * 32 + 31, set_rows - 1) / a.g;
+  TileFrag q[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const uint4*)(qrow + 16 * kk + 8 * half);
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)sm;
+  const auto fill = [&](const int i, const int buf) {
+    const bool f = i < front_tiles;
+    const int j = i - front_tiles;
+    const bool in_a = j < span.na;
+    const int base = f ? i * AT_KEYS : in_a ? j * AT_KEYS : span.b0 + (j - span.na) * AT_KEYS, end = f ? front : in_a ? span.a_end : span.end;
+    tile_fill<D, false>(lds + buf * TILE, (f ? FK : K) + (size_t)base * D, end - 1 - base, wave, lane);
+    tile_fill<D, true>(lds + (2 + buf) * TILE, (f ? FV : V) + (size_t)base * D, end - 1 - base, wave, lane);
+  };
+  // lane's places
+  int at_k[KK], at_v[DB];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) at_k[kk] = place_k<D>(lane & 31, 2 * kk + half);
+  const int vrow = 4 * half + ((lane & 15) >> 2);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) at_v[db] = vrow * 2 * D + ((db ^ swap_v<D>(vrow)) << 6) + ((lane & 16) << 1) + ((lane & 3) << 3);
+
+  if (first < behind) fill(first, 0);
+  for (int i = first; i < behind; ++i) {
+    const int buf = (i - first) & 1;
+    wait_loads<0>();
+    __syncthreads();                                   // the tile is there, and nobody reads the other one any more
+    if (i + 1 < behind) fill(i + 1, buf ^ 1);
+    const bool f = i < front_tiles;
+    const int j0 = i - front_tiles;
+    const bool in_a = j0 < span.na;
+    const int base = f ? i * AT_KEYS : in_a ? j0 * AT_KEYS : span.b0 + (j0 - span.na) * AT_KEYS, end = f ? front : in_a ? span.a_end : span.end;
+    // some row of the wave does not see some key of the tile; none sees any
+    const bool causal = k.causal && !f;
+    const bool cut = base + AT_KEYS > end || (causal && (base + AT_KEYS - 1 > wmin || (k.window > 0 && base <= wmax - k.window && base + AT_KEYS - 1 >= sink)));
+    if (causal && (base > wmax || (k.window > 0 && base + AT_KEYS - 1 <= wmin - k.window && base >= sink))) continue;
+    const char* tk = sm + buf * TILE;
+    const char* tv = sm + (2 + buf) * TILE;
+    f32x16 x[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      TileFrag kf[KK];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) kf[kk].u = *(const uint4*)(tk + b * 32 * 2 * D + at_k[kk]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk].v, q[kk].v, x[b], 0, 0, 0);
+    }
+    if (cut) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = base + 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
+          if (!(j < end && attend_sees(causal, k.window, sink, pos, j))) x[b][e] = -INFINITY;
+        }
+    }
+    float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, fmaxf(x[0][e], x[1][e]));
+    mx *= a.scale2;
+    if (__any(mx > m + kAttendSlack)) {
+      const float next = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
+      const float scale = next > -INFINITY ? attend_exp2(m - next) : 1.f;
+      m = next;
+      l *= scale;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[db][e] *= scale;
+    }
+    const float ref = m > -INFINITY ? m : 0.f;
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      x[0][e] = attend_exp2(fmaf(x[0][e], a.scale2, -ref));
+      x[1][e] = attend_exp2(fmaf(x[1][e], a.scale2, -ref));
+      s0 += x[0][e]; s1 += x[1][e];
+    }
+    l += s0 + s1;
+    // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
+    if (cut && causal) {
+      bool bad = false;
+      for (int e = lane; e < TILE / 16; e += 64) {
+        const uint4 u = *(const uint4*)(tv + e * 16);
+        const uint32_t y[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) bad |= ((y[c] & 0x7f80u) == 0x7f80u) | ((y[c] & 0x7f800000u) == 0x7f800000u);
+      }
+      if (__any(bad)) {
+#pragma unroll 1
+        for (int j = base; j < min(end, base + AT_KEYS); ++j) {
+          const uint16_t* krow = K + (size_t)j * D;
+          const uint16_t* row = V + (size_t)j * D;
+          float dot = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < D; ++c) dot = fmaf(__uint_as_float((uint32_t)krow[c] << 16), __uint_as_float((uint32_t)qrow[c] << 16), dot);
+          if (attend_sees(causal, k.window, sink, pos, j)) {
+            const float wt = attend_exp2(fmaf(dot, a.scale2, -ref));
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                o[db][e] = fmaf(wt, __uint_as_float((uint32_t)row[32 * db + 8 * (e >> 2) + 4 * half + (e & 3)] << 16), o[db][e]);
+          }
+        }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      TileFrag p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p.v[e] = (__bf16)x[t >> 1][8 * (t & 1) + e];
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        TileFrag v;
+        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tv + at_v[db] + t * 16 * 2 * D));
+        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tv + at_v[db] + (t * 16 + 8) * 2 * D));
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p.v, o[db], 0, 0, 0);
+      }
+    }
+  }
+
+  l += __shfl_xor(l, 32);
+  if (r >= set_rows) return;
+  const bool any = m > -INFINITY;
+  const float inv = any ? 1.f / l : 0.f;
+  const float lse2 = any ? m + attend_log2(l) : -INFINITY;
+  const size_t number = attend_row_number(a, h, w);
+  if (a.ranges > 1) {
+    const size_t at = (size_t)(k.split0 + split) * a.rows + number;
+    if (half == 0) a.part_lse[at] = lse2;
+    if (!any) return;                                  // (nobody reads the others)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        *(float4*)(a.part_O + at * D + 32 * db + 8 * c + 4 * half) =
+            make_float4(o[db][4 * c] * inv, o[db][4 * c + 1] * inv, o[db][4 * c + 2] * inv, o[db][4 * c + 3] * inv);
+  } else {
+    if (half == 0 && a.lse) a.lse[number] = lse2 * 0.69314718055994531f;
+    uint16_t* out = (uint16_t*)a.O + (size_t)w.s * a.os + (size_t)(h * a.g + w.gi) * a.oh + (size_t)w.t * a.ot;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        union { __bf16 b[4]; uint2 u; } y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y.b[e] = (__bf16)(any ? o[db][4 * c + e] * inv : 0.f);
+        *(uint2*)(out + 32 * db + 8 * c + 4 * half) = y.u;
+      }
+  }
+}
+
+obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st) {
+  ProfScope prof(ST_ATTEND, st);
+  const int blocks = a.fused ? a.keys[1].blocks : a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0);
+  if (d == 128) hipLaunchKernelGGL(k_attend_tile<128>, dim3(blocks), dim3(AT_THREADS), 0, st, a);
+  else hipLaunchKernelGGL(k_attend_tile<64>, dim3(blocks), dim3(AT_THREADS), 0, st, a);
+  return check_launch("attend");
+}
+
+}  // namespace obf

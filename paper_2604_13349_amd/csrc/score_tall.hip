@@ -19,6 +19,7 @@
 // (most tiles of a cache with outlier tokens outgrow it in some lane), 320 rows this way (160 operand registers a lane) slower.
 // Errors against 64 bits, six draws of each of eleven shapes of 161 to 512 rows, with and without tokens of eight times the size: rms of scores 0.95 and of
 // normalisers 0.83 of the pairs' (geometric means; 0.85 to 0.99 and 0.52 to 0.93), largest errors 0.98 and 0.91 (0.83 to 1.20 and 0.72 to 1.11).
+#include "lds_load.hpp"
 #include "score_parts.hpp"
 #include "wave_ops.hpp"
 
@@ -41,20 +42,6 @@ struct TallPart {
   long TT;       // heads * SH
   long kstride;  // elements between consecutive heads of K
 };
-
-// Four times 16 bytes per lane from base + off to LDS at `lds` + 16 lane and 4096 further each time, without registers between; complete when vmcnt says
-// so.  (The builtin would have the compiler wait for the youngest of these loads before every read of LDS.)  m0 is left as it was: the compiler reserves
-// it and would not be told by a clobber.
-__device__ __forceinline__ void load_to_lds(const uint32_t lds, const uint32_t (&off)[4], const void* base) {
-  uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %6\n\t"
-               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %6\n\t"
-               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %6\n\t"
-               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base) : "memory", "scc");
-}
-template <int N>
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // The 64 tokens from Kt on (rows past `last` repeat it) to a step of the ring: token r's piece c goes to place c ^ (r % 16).  Keys off a 16-byte boundary
 // go through registers.
