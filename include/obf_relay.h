@@ -380,7 +380,7 @@ typedef struct {
   int64_t o_stride[3];
 } obf_attend_t;
 
-/* Bytes of workspace of obf_attend (prefix_stride 0) or obf_attend_shared; 0 if the call is not supported.  Host function. */
+/* Bytes of workspace of obf_attend and obf_attend_mass (prefix_stride 0) or obf_attend_shared; 0 if the call is not supported.  Host function. */
 size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride);
 
 /* Attention of the queries over their own caches.  mass (nullable): the weight every visible row receives, summed over the
@@ -400,7 +400,7 @@ obf_status_t obf_attend_shared(const obf_attend_t* call, const void* Q, const vo
 /* The accumulated attention weight alone, from the lse that obf_attend or obf_attend_shared returned for the same queries:
  * mass[row] += sum of exp(logit - lse) over the queries that see the row (a query of lse -inf counts 0). */
 obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void* K, const float* lse, const int32_t* kv_len,
-                             const int32_t* sink_len, float* mass, void* stream);
+                             const int32_t* sink_len, float* mass, void* ws, size_t ws_bytes, void* stream);
 
 /* Eviction by accumulated attention weight.  Of a head of n rows the first s (sink_len[h], DEVICE int32, or `sink`; they travel
  * outside the budget, as in obf_window_t) and min(budget, n - s) of the others are kept: the newest `recent` ones and those of

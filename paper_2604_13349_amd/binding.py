@@ -130,7 +130,7 @@ def load_library():
     lib.obf_attend_shared.restype = C.c_int
     lib.obf_attend_shared.argtypes = [ap, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.obf_attend_mass.restype = C.c_int
-    lib.obf_attend_mass.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp]
+    lib.obf_attend_mass.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.obf_evict.restype = C.c_int
     lib.obf_evict.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp]
     lib.obf_profile_enable.restype = C.c_int
@@ -587,14 +587,15 @@ def attend_shared(Q, prefix_K, prefix_V, K, V, prefix_len=None, kv_len=None, cau
     return o
 
 
-def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sink_len=None):
+def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sink_len=None, ws=None):
     """obf_attend_mass: adds to mass float32 [S,H,rows], in place, the attention weight of the rows of K under the lse [S,H*g,T] of an earlier call."""
     _on_device(Q, K=K, lse=lse, mass=mass, kv_len=kv_len, sink_len=sink_len)
     c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, mass=mass)
     if lse.dtype != torch.float32 or lse.shape != Q.shape[:3]:
         raise ValueError("lse must be float32 [samples, query heads, queries]")
     with torch.cuda.device(Q.device):
-        _check(load_library().obf_attend_mass(C.byref(c), _at(Q), _at(K), _ptr(lse), _at(kv_len), _at(sink_len), _at(mass), _stream()))
+        ws = _attend_ws({"ws": ws}, c, 0, Q.device)
+        _check(load_library().obf_attend_mass(C.byref(c), _at(Q), _at(K), _ptr(lse), _at(kv_len), _at(sink_len), _at(mass), _ptr(ws), ws.numel(), _stream()))
     return mass
 
 

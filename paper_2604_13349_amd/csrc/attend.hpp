@@ -102,7 +102,11 @@ constexpr int kAttendTileRows = 128;
 obf_status_t launch_attend_few(const AttendArgs& a, int tile_rows, int d, int dtype, hipStream_t st);
 obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);
 obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);
-obf_status_t launch_attend_mass(const AttendArgs& a, int d, int dtype, const float* lse, float* mass, hipStream_t st);
+
+// Accumulated weights of the own rows; part: a sum per range of query rows (unless there is one) and row of a dense cache.
+struct AttendMass { float* mass; float* part; int nsplit, tiles; };
+int attend_mass_ranges(const AttendArgs& a, int dtype);
+obf_status_t launch_attend_mass(const AttendArgs& a, int d, int dtype, const float* lse, const AttendMass& mass, hipStream_t st);
 
 struct EvictArgs {
   const void* K; const void* V; const float* mass; const int32_t* pos;

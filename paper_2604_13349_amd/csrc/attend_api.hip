@@ -55,11 +55,12 @@ static obf_status_t check_aligned(const char* name, const void* p) {
 }
 
 // The launch of one call: which kernel goes over which set of keys, tiles, ranges; and the workspace, in the order partial sums, partial normalisers, row
-// normalisers.
+// normalisers, partial weights.
 struct AttendPlan {
   AttendArgs a;
   int tile_rows[2];            // query rows of a workgroup's tile, by set of keys; kAttendTileRows: the kernel of many rows
-  size_t part_O, part_lse, lse, total;
+  int mass_ranges;
+  size_t part_O, part_lse, lse, mass, total;
 };
 
 static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
@@ -110,6 +111,9 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
   p.lse = at;
   at += ((size_t)a.rows * sizeof(float) + 255) & ~(size_t)255;
+  p.mass_ranges = attend_mass_ranges(a, c->dtype);
+  p.mass = at;
+  if (p.mass_ranges > 1) at += ((size_t)p.mass_ranges * a.S * a.H * c->token_stride * sizeof(float) + 255) & ~(size_t)255;
   p.total = at;
   return p;
 }
@@ -128,13 +132,18 @@ static obf_status_t launch_plan(const AttendPlan& p, int d, int dtype, hipStream
   return OBF_OK;
 }
 
+static obf_status_t check_attend_ws(const AttendPlan& p, const void* ws, size_t ws_bytes) {
+  if (!ws) { set_error("workspace is NULL"); return OBF_ERR_INVALID_ARG; }
+  if (((uintptr_t)ws & 255) != 0) { set_error("workspace must be 256-byte aligned"); return OBF_ERR_INVALID_ARG; }
+  if (ws_bytes < p.total) { set_error("workspace too small: %zu bytes given, %zu needed", ws_bytes, p.total); return OBF_ERR_WORKSPACE_TOO_SMALL; }
+  return OBF_OK;
+}
+
 static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
                                int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
                                const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, hipStream_t st) {
   AttendPlan p = plan_attend(c, prefix_stride);
-  if (!ws) { set_error("workspace is NULL"); return OBF_ERR_INVALID_ARG; }
-  if (((uintptr_t)ws & 255) != 0) { set_error("workspace must be 256-byte aligned"); return OBF_ERR_INVALID_ARG; }
-  if (ws_bytes < p.total) { set_error("workspace too small: %zu bytes given, %zu needed", ws_bytes, p.total); return OBF_ERR_WORKSPACE_TOO_SMALL; }
+  OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   AttendArgs& a = p.a;
   char* base = (char*)ws;
   if (mass && !lse) lse = (float*)(base + p.lse);
@@ -149,7 +158,7 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
   }
   OBF_TRY(launch_plan(p, c->head_dim, c->dtype, st));
   if (a.ranges > 1) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
-  return mass ? launch_attend_mass(a, c->head_dim, c->dtype, lse, mass, st) : OBF_OK;
+  return mass ? launch_attend_mass(a, c->head_dim, c->dtype, lse, AttendMass{mass, (float*)(base + p.mass), p.mass_ranges, 0}, st) : OBF_OK;
 }
 
 }  // namespace obf
@@ -187,13 +196,14 @@ obf_status_t obf_attend_shared(const obf_attend_t* call, const void* Q, const vo
 }
 
 obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void* K, const float* lse, const int32_t* kv_len,
-                             const int32_t* sink_len, float* mass, void* stream) {
+                             const int32_t* sink_len, float* mass, void* ws, size_t ws_bytes, void* stream) {
   OBF_TRY(check_attend(call));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_NONNULL(lse); OBF_NONNULL(mass);
   AttendPlan p = plan_attend(call, 0);
+  OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   p.a.Q = Q;
   p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;
-  return launch_attend_mass(p.a, call->head_dim, call->dtype, lse, mass, (hipStream_t)stream);
+  return launch_attend_mass(p.a, call->head_dim, call->dtype, lse, AttendMass{mass, (float*)((char*)ws + p.mass), p.mass_ranges, 0}, (hipStream_t)stream);
 }
 
 obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const void* K, const void* V, const float* mass, const int32_t* pos,

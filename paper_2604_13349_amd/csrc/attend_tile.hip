@@ -9,24 +9,13 @@
 // (ds_read_b64_tr_b16).  m follows the row's maximum only where that outgrows it by 2^8.
 // Pieces of 16 bytes (K) and 64 bytes (V) of a row lie in LDS permuted by the row's number, so that the operand reads use all banks.
 // P is rounded to bf16, 2^-9 of a weight at most: at this many rows the matrix pipe bounds the kernel, and the result is rounded as coarsely.
-#include "attend.hpp"
+#include "attend_tile.hpp"
 #include "lds_load.hpp"
 
 namespace obf {
 
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
-typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
-
 constexpr int AT_WAVES = 4, AT_THREADS = AT_WAVES * 64, AT_ROWS = AT_WAVES * 32, AT_KEYS = 64;
 static_assert(AT_ROWS == kAttendTileRows, "rows of a workgroup's tile");
-
-union TileFrag { uint4 u; bf16x8 v; s16x4 h[2]; uint32_t w[4]; };
-
-// Places in a tile of rows of 2 D bytes.
-template <int D> __device__ __forceinline__ int place_k(const int row, const int piece) {       // 16-byte pieces
-  return row * 2 * D + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
-}
-template <int D> __device__ __forceinline__ int swap_v(const int row) { return D == 128 ? row & 3 : (row >> 1) & 1; }   // of 64-byte pieces
 
 // 64 rows of K (or V) from Kt on (rows past `last` repeat it) to LDS.
 template <int D, bool VALUES>

@@ -52,7 +52,7 @@ def test_refused_descriptors(lib, change, status, word):
     assert rc == status and word in msg
     assert lib.obf_attend_workspace_bytes(C.byref(c), 0) == 0
     assert lib.obf_attend_shared(C.byref(c), FAKE, FAKE, FAKE, None, 10, 10, FAKE, FAKE, None, None, FAKE, None, FAKE, 1 << 40, None) == status
-    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, None) == status
+    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, FAKE, 1 << 40, None) == status
 
 
 def test_refused_pointers_and_workspaces(lib):
@@ -76,8 +76,10 @@ def test_refused_pointers_and_workspaces(lib):
     assert shared(pk=None) == 1 and shared(pv=None) == 1 and shared(n=11) == 1 and shared(n=-1) == 1 and shared(stride=0, n=0) == 1
     assert shared(n=1, stride=(1 << 24) + 1) == 2
     assert shared(n=4000, stride=4000) == 3
-    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, None, None, None, FAKE, None) == 1
-    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, None, None) == 1
+    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, None, None, None, FAKE, FAKE, need, None) == 1
+    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, None, FAKE, need, None) == 1
+    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, None, need, None) == 1
+    assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, FAKE, need - 1, None) == 3
 
 
 def test_refused_evictions(lib):
