@@ -30,6 +30,7 @@ struct AttendArgs {
   float* lse;                // nullable
   long qs, qh, qt, os, oh, ot;   // elements between samples, query heads, queries
   int S, H, g, T;
+  uint32_t g_inv;            // ceil(2^23 / g)
   float scale2;              // log2(e) / sqrt(d)
   long rows;                 // S * H * g * T query rows; a row's number is its place in lse, [S][H * g][T]
   float* part_O;             // [ranges][rows][d] and [ranges][rows] (powers of two); used unless there is one range
@@ -78,10 +79,13 @@ __device__ __forceinline__ AttendSpan attend_span(const AttendKeys& k, const int
   return s;
 }
 
-// Whether the query at position p sees key j (below the head's length).
-__device__ __forceinline__ bool attend_sees(const int causal, const int window, const int sink, const int p, const int j) {
-  return !causal || (j <= p && (window <= 0 || j > p - window || j < sink));
+// The keys below `end` that the query at position p sees: j <= hi and (j > lo or j < first); numbers relative to `from`, so that a tile's keys are constants.
+struct AttendView { int hi, lo, first; };
+__device__ __forceinline__ AttendView attend_view(const int causal, const int window, const int sink, const int p, const int end, const int from = 0) {
+  return {(causal ? min(p, end - 1) : end - 1) - from, (causal && window > 0 ? p - window : -1) - from, sink - from};
 }
+__device__ __forceinline__ AttendView attend_from(const AttendView v, const int from) { return {v.hi - from, v.lo - from, v.first - from}; }
+__device__ __forceinline__ bool attend_sees(const AttendView v, const int j) { return (j <= v.hi) & ((j > v.lo) | (j < v.first)); }
 
 // Query row r of the rows that read a set of keys: query head, query and sample, and the row's number.
 struct AttendRow { int s, gi, t; };
@@ -92,6 +96,13 @@ __device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, const Atten
   w.s = set_sample;
   if (k.row_samples > 1) { w.s = w.t / a.T; w.t -= w.s * a.T; }
   return w;
+}
+// Row first + i (i < 128) of a sample's own rows, from the query and query head of row `first`: small numbers, so that a product with a reciprocal divides.
+struct AttendStep { int t, gi; };
+__device__ __forceinline__ AttendStep attend_step(const AttendArgs& a, const int first) { return {first / a.g, first % a.g}; }
+__device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, const AttendStep first, const int s, const int i) {
+  const uint32_t n = (uint32_t)(first.gi + i), q = (n * a.g_inv) >> 23;        // exact for n < 512 and g <= 128
+  return {s, (int)(n - q * a.g), first.t + (int)q};
 }
 __device__ __forceinline__ size_t attend_row_number(const AttendArgs& a, const int h, const AttendRow& w) {
   return ((size_t)w.s * a.H * a.g + (size_t)h * a.g + w.gi) * a.T + w.t;

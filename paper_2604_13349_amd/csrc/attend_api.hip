@@ -68,6 +68,7 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   AttendArgs& a = p.a;
   a = AttendArgs();
   a.S = c->n_samples; a.H = c->n_kv_heads; a.g = c->group; a.T = c->n_queries;
+  a.g_inv = ((1u << 23) + a.g - 1) / a.g;
   const long d = c->head_dim, hq = (long)a.H * a.g;
   const bool qd = c->q_stride[0] || c->q_stride[1] || c->q_stride[2], od = c->o_stride[0] || c->o_stride[1] || c->o_stride[2];
   a.qs = qd ? c->q_stride[0] : hq * a.T * d; a.qh = qd ? c->q_stride[1] : a.T * d; a.qt = qd ? c->q_stride[2] : d;
@@ -84,7 +85,9 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   k = AttendKeys();
   k.len_all = c->kv_len_all; k.len_stride = c->len_stride ? c->len_stride : a.H;
   k.stride = c->token_stride; k.sample_rows = c->sample_stride ? c->sample_stride : (long)a.H * c->token_stride;
-  k.sink = c->sink; k.window = c->window; k.causal = c->causal != 0;
+  k.sink = c->sink;
+  k.window = c->window < c->token_stride ? c->window : 0;      // (positions lie below the stride: the others hide nothing)
+  k.causal = c->causal != 0;
   k.samples = a.S; k.row_samples = 1;
   const long own_rows = (long)a.T * a.g;
   // A sample's queries fill tiles of many rows by themselves: one pass over the message and the own rows, no partial results of the message.

@@ -23,8 +23,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
   // which set of keys, tile of rows and range of keys
   int block = blockIdx.x;
   const bool second = block >= a.keys[0].blocks;
-  const AttendKeys& k = a.keys[second ? 1 : 0];
-  if (second) block -= a.keys[0].blocks;
+  AttendKeys k = a.keys[0];
+  if (second) { k = a.keys[1]; block -= a.keys[0].blocks; }
   const int split = block % k.nsplit;
   block /= k.nsplit;
   const int row_tile = block % k.row_tiles, set = block / k.row_tiles;
@@ -73,14 +73,14 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
     for (int nb = 0; nb < NB; ++nb) {
       f32x4 x[2];
       Tile::scores(x, kf, q[nb]);
+      const AttendView view = attend_view(k.causal, k.window, sink, pos[nb], end, base + 4 * quad);
       float mx = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float v = x[b][r] * a.scale2;
-          const int j = base + 16 * b + 4 * quad + r;
-          if (cut && !(j < end && attend_sees(k.causal, k.window, sink, pos[nb], j))) v = -INFINITY;
+          if (cut) v = attend_sees(view, 16 * b + r) ? v : -INFINITY;
           x[b][r] = v;
           mx = fmaxf(mx, v);
         }
@@ -102,23 +102,26 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
     }
     // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
     if (cut && k.causal && a.T > 1 && __any(Tile::not_finite(vf))) {
+#pragma unroll 1
+      for (int j = base; j < min(end, base + 32); ++j) {
+        const ET* krow = K + (size_t)j * D;
+        const ET* row = V + (size_t)j * D;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) {
+          const AttendRow w = attend_row(a, k, ks, min(row0 + 16 * nb + (lane & 15), set_rows - 1));
+          const ET* qrow = (const ET*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt;
+          float dot = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < D; ++c) dot = fmaf(Tile::value(krow, c), Tile::value(qrow, c), dot);
+          if (attend_sees(attend_view(k.causal, k.window, sink, pos[nb], end), j)) {
+            const float wt = attend_exp2(fmaf(dot, a.scale2, -(m[nb] > -INFINITY ? m[nb] : 0.f)));
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            for (int qd = 0; qd < 4; ++qd) {
-              const int j = base + 16 * b + 4 * qd + r;
-              const float w = __shfl(p[nb][b][r], 16 * qd + (lane & 15));
-              if (j < end && attend_sees(k.causal, k.window, sink, pos[nb], j)) {
-                const ET* row = V + (size_t)j * D;
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                  for (int c = 0; c < 4; ++c) o[nb][db][c] = fmaf(w, Tile::value(row, Tile::channel(quad, db, c)), o[nb][db][c]);
-              }
-            }
+              for (int c = 0; c < 4; ++c) o[nb][db][c] = fmaf(wt, Tile::value(row, Tile::channel(quad, db, c)), o[nb][db][c]);
+          }
+        }
+      }
     } else {
       Tile::template values<NB>(o, vf, p);
     }

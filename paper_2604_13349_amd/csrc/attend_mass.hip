@@ -34,7 +34,7 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
   const int behind = t1 * a.g;
   for (int r0 = t0 * a.g; r0 < behind; r0 += 16) {
     const int r = r0 + (lane & 15);
-    const AttendRow w = attend_row(a, k, s, min(r, behind - 1));
+    const AttendRow w = attend_row(a, attend_step(a, r0), s, min(lane & 15, behind - 1 - r0));
     typename Tile::Query q;
     Tile::load_query(q, (const ET*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt, lane);
     const float row_lse = lse[attend_row_number(a, h, w)];
@@ -42,13 +42,14 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
     const bool counts = r < behind && !(row_lse == -INFINITY);       // (a row that sees nothing has weights of 0)
     f32x4 x[2];
     Tile::scores(x, kf, q);
+    AttendView view = attend_view(k.causal, k.window, sink, p0 + w.t, n, base + 4 * quad);
+    if (!counts) view.hi = -1;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const int j = base + 16 * b + 4 * quad + c;
-        const bool sees = counts && attend_sees(k.causal, k.window, sink, p0 + w.t, j);
-        sum[b][c] += sees ? attend_exp2(fmaf(x[b][c], a.scale2, -ref)) : 0.f;
+        const float v = attend_exp2(fmaf(x[b][c], a.scale2, -ref));
+        sum[b][c] += attend_sees(view, 16 * b + c) ? v : 0.f;
       }
   }
 #pragma unroll
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
   constexpr int KK = D / 16, PIECES = D / 8, LOADS = MT_ROWS * PIECES / MT_THREADS;
   __shared__ __attribute__((aligned(16))) char sm_q[2][MT_ROWS * 2 * D];
   __shared__ float sm_ref[2][MT_ROWS];
-  __shared__ int sm_pos[2][MT_ROWS];
+  __shared__ AttendView sm_view[2][MT_ROWS];
   const AttendKeys& k = a.keys[0];
   const int lane = threadIdx.x & 63, wave = attend_uniform(threadIdx.x >> 6), half = lane >> 5;
   const int split = blockIdx.x % ms.nsplit, tile = blockIdx.x / ms.nsplit % ms.tiles, set = blockIdx.x / ms.nsplit / ms.tiles, h = set % a.H, s = set / a.H;
@@ -100,29 +101,33 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
 #pragma unroll
     for (int e = 0; e < 16; ++e) sum[b][e] = 0.f;
 
-  uint4 next[LOADS];
+  // 64 rows from r0 on, to registers and from there to LDS; a thread fetches LOADS pieces, and the first 64 threads a row's normaliser and view
+  TilePiece next[LOADS];
   float next_ref = 0.f;
-  int next_pos = 0;
+  AttendView next_view = {-1, -1, 0};
+  const uint16_t* Q = (const uint16_t*)a.Q + (size_t)s * a.qs + (size_t)h * a.g * a.qh + 8 * (threadIdx.x % PIECES);
   const auto fetch = [&](const int r0) {
+    const AttendStep at = attend_step(a, r0);
+    const int most = behind - 1 - r0;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const AttendRow w = attend_row(a, k, s, min(r0 + (int)(i * (MT_THREADS / PIECES) + threadIdx.x / PIECES), behind - 1));
-      next[i] = *(const uint4*)((const uint16_t*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt + 8 * (threadIdx.x % PIECES));
+      const AttendRow w = attend_row(a, at, s, min((int)(i * (MT_THREADS / PIECES) + threadIdx.x / PIECES), most));
+      next[i] = *(const TilePiece*)(Q + (size_t)w.gi * a.qh + (size_t)w.t * a.qt);
     }
-    if (threadIdx.x < MT_ROWS) {
-      const int r = r0 + threadIdx.x;
-      const AttendRow w = attend_row(a, k, s, min(r, behind - 1));
-      const float v = lse[attend_row_number(a, h, w)];
-      // (a row that sees nothing has weights of 0, and so has one behind the range)
-      next_ref = r < behind && v != -INFINITY ? v * 1.44269504088896341f : INFINITY;
-      next_pos = p0 + w.t;
-    }
+    const int i = (int)(threadIdx.x % MT_ROWS);
+    const AttendRow w = attend_row(a, at, s, min(i, most));
+    const float v = lse[attend_row_number(a, h, w)];
+    next_view = attend_view(k.causal, k.window, sink, p0 + w.t, n);
+    // (a row that sees nothing has weights of 0, and so has one behind the range)
+    const bool counts = i <= most && !(v == -INFINITY);
+    next_ref = counts ? v * 1.44269504088896341f : INFINITY;
+    if (!counts) next_view.hi = -1;
   };
   const auto put = [&](const int buf) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
-      *(uint4*)(sm_q[buf] + place_k<D>(i * (MT_THREADS / PIECES) + threadIdx.x / PIECES, threadIdx.x % PIECES)) = next[i];
-    if (threadIdx.x < MT_ROWS) { sm_ref[buf][threadIdx.x] = next_ref; sm_pos[buf][threadIdx.x] = next_pos; }
+      *(TilePiece*)(sm_q[buf] + place_k<D>(i * (MT_THREADS / PIECES) + threadIdx.x / PIECES, threadIdx.x % PIECES)) = next[i];
+    if (threadIdx.x < MT_ROWS) { sm_ref[buf][threadIdx.x] = next_ref; sm_view[buf][threadIdx.x] = next_view; }
   };
   if (first < behind) { fetch(first); put(0); }
   __syncthreads();
@@ -142,7 +147,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const uint4*)(sm_q[buf] + place_k<D>(row, 2 * kk + half));
         const float ref = sm_ref[buf][row];
-        const int pos = sm_pos[buf][row];
+        const AttendView view = attend_from(sm_view[buf][row], base + 4 * half);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           f32x16 x;
@@ -153,8 +158,8 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
           if (cut) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const bool sees = !(ref == INFINITY) && attend_sees(k.causal, k.window, sink, pos, base + 32 * b + 8 * (e >> 2) + 4 * half + (e & 3));
-              sum[b][e] += sees ? attend_exp2(fmaf(x[e], a.scale2, -ref)) : 0.f;
+              const float v = attend_exp2(fmaf(x[e], a.scale2, -ref));
+              sum[b][e] += attend_sees(view, 32 * b + 8 * (e >> 2) + (e & 3)) ? v : 0.f;
             }
           } else {
 #pragma unroll

@@ -38,8 +38,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   // set of keys, tile of rows and range of keys; the sets go round the dies, the rows with the most keys first
   int block = blockIdx.x;
   const bool second = a.fused || block >= a.keys[0].blocks;
-  const AttendKeys& k = a.keys[second ? 1 : 0];
-  if (second && !a.fused) block -= a.keys[0].blocks;
+  AttendKeys k = a.keys[0];
+  if (second) { k = a.keys[1]; if (!a.fused) block -= a.keys[0].blocks; }
   const int sets = k.samples * a.H, round = sets & 7 ? sets & -sets : 8, per_set = k.row_tiles * k.nsplit;
   const int set = block % round + round * (block / (round * per_set));
   const int within = block / round % per_set;
@@ -120,14 +120,12 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk].v, q[kk].v, x[b], 0, 0, 0);
     }
+    const AttendView view = attend_view(causal, k.window, sink, pos, end, base + 4 * half);
     if (cut) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = base + 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
-          if (!(j < end && attend_sees(causal, k.window, sink, pos, j))) x[b][e] = -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e) x[b][e] = attend_sees(view, 32 * b + 8 * (e >> 2) + (e & 3)) ? x[b][e] : -INFINITY;
     }
     float mx = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
@@ -169,7 +167,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
           float dot = 0.f;
 #pragma unroll 1
           for (int c = 0; c < D; ++c) dot = fmaf(__uint_as_float((uint32_t)krow[c] << 16), __uint_as_float((uint32_t)qrow[c] << 16), dot);
-          if (attend_sees(causal, k.window, sink, pos, j)) {
+          if (attend_sees(view, j - base - 4 * half)) {
             const float wt = attend_exp2(fmaf(dot, a.scale2, -ref));
 #pragma unroll
             for (int db = 0; db < DB; ++db)
