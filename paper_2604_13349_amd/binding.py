@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -452,104 +453,153 @@ def append_message(prev_K, prev_V, prev_len, keep_K, keep_V, n_keep, gen_K, gen_
     return msg_K, msg_V, msg_len
 
 
-def _on_device(ref: torch.Tensor, **tensors):
-    """Every tensor given (None: not given) lies on ref's GPU."""
-    if not ref.is_cuda:
+def _meta(t: Optional[torch.Tensor]):
+    """What a call is checked and laid out by; never a tensor's address."""
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
+
+
+def _same_device(metas):
+    device = metas[0][1][3]
+    if device.type != "cuda":
         raise ValueError("tensors must be on a GPU")
-    for name, t in tensors.items():
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+    for name, m in metas:
+        if m is not None and m[3] != device:
+            raise ValueError(f"{name} is on {m[3]}, not on {device}")
+    return device
 
 
-def _int32(name: str, t: Optional[torch.Tensor], shape):
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be int32 {list(shape)}")
-    return t
+def _contiguous(shape, stride) -> bool:
+    want = 1
+    for n, w in zip(reversed(shape), reversed(stride)):
+        if n > 1 and w != want:
+            return False
+        want *= n
+    return True
 
 
-def _q_strides(name: str, t: torch.Tensor, d: int):
+def _want(name: str, m, shape, dtype, contiguous=True):
+    """A tensor, if given, has this shape and dtype."""
+    if m is not None and (m[2] != dtype or tuple(m[0]) != tuple(shape) or contiguous and not _contiguous(m[0], m[1])):
+        raise ValueError(f"{name} must be {'contiguous ' if contiguous else ''}{dtype} {list(shape)}")
+
+
+def _row_strides(name: str, m, d: int):
     """Strides of a [samples, heads, queries, d] tensor; those of dimensions of one are made up."""
-    if t.shape[3] != 1 and t.stride(3) != 1:
+    shape, stride = m[0], m[1]
+    if stride[3] != 1 and shape[3] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return [t.stride(i) if t.shape[i] > 1 else d * max(1, t.shape[2]) for i in range(3)]
+    return [stride[i] if shape[i] > 1 else d * max(1, shape[2]) for i in range(3)]
 
 
-def _attend_call(Q, K, kv_len, sink_len, causal, window, sink, V=None, mass=None, O=None):
-    """obf_attend_t of the call, with the tensors checked against each other; also kv_len and sink_len as they are handed over."""
-    if Q.dim() != 4 or K.dim() != 4:
+@functools.lru_cache(maxsize=1024)
+def _attend_plan(Q, K, V, O, lse, mass, kv_len, sink_len, prefix_K, prefix_V, prefix_len, causal, window, sink):
+    """The descriptor of an attention call and what goes with it, from the tensors' metadata, which is checked: (obf_attend_t, bytes of workspace, rows of the
+    message, whether the lengths have to be made contiguous)."""
+    _same_device((("Q", Q), ("K", K), ("V", V), ("O", O), ("lse", lse), ("mass", mass), ("kv_len", kv_len), ("sink_len", sink_len), ("prefix_K", prefix_K),
+                  ("prefix_V", prefix_V), ("prefix_len", prefix_len)))
+    if len(Q[0]) != 4 or len(K[0]) != 4:
         raise ValueError("Q must be [samples, query heads, queries, d], K [samples, heads, rows, d]")
-    S, Hq, T, d = Q.shape
-    Sk, H, rows, dk = K.shape
+    S, Hq, T, d = Q[0]
+    Sk, H, rows, dk = K[0]
+    dtype = K[2]
     if Sk != S or dk != d or H < 1 or Hq % H != 0:
         raise ValueError("Q does not match K")
-    if K.dtype not in (torch.float32, torch.bfloat16) or Q.dtype != K.dtype:
+    if dtype not in (torch.float32, torch.bfloat16) or Q[2] != dtype:
         raise ValueError("Q and K must both be float32 or bfloat16")
-    if V is not None and (V.shape != K.shape or V.dtype != K.dtype):
-        raise ValueError("V does not match K")
+    _want("V", V, K[0], dtype, contiguous=False)
 
-    def rows_between(name, t, width):
-        """Rows between the samples of a cache tensor whose heads are contiguous."""
-        if any(n > 1 and t.stride(i + 1) != w for i, (n, w) in enumerate(zip(t.shape[1:], (rows * width, width, 1)))):
+    def apart(name, m):
+        """Rows between the samples of a cache, whose heads are contiguous."""
+        if any(n > 1 and w != x for n, w, x in zip(m[0][1:], m[1][1:], (rows * d, d, 1))):
             raise ValueError(f"{name}: the heads of a sample must be contiguous")
         if S == 1:
             return H * rows
-        if t.stride(0) % width or t.stride(0) < H * rows * width:
+        if m[1][0] % d or m[1][0] < H * rows * d:
             raise ValueError(f"{name}: samples must be whole rows apart and not overlap")
-        return t.stride(0) // width
+        return m[1][0] // d
 
-    apart = rows_between("K", K, d)
-    if V is not None and rows_between("V", V, d) != apart:
+    between = apart("K", K)
+    if V is not None and apart("V", V) != between:
         raise ValueError("K and V must have the same strides")
     if mass is not None:
-        if mass.dtype != torch.float32 or tuple(mass.shape) != (S, H, rows):
-            raise ValueError("mass must be float32 [samples, heads, rows]")
-        if H > 1 and mass.stride(1) != rows or rows > 1 and mass.stride(2) != 1 or S > 1 and mass.stride(0) != apart:
+        _want("mass", mass, (S, H, rows), torch.float32, contiguous=False)
+        if H > 1 and mass[1][1] != rows or rows > 1 and mass[1][2] != 1 or S > 1 and mass[1][0] != between:
             raise ValueError("mass must have the row strides of K")
-    kv_len, sink_len = _int32("kv_len", kv_len, (S, H)), _int32("sink_len", sink_len, (S, H))
-    lens = [t for t in (kv_len, sink_len) if t is not None]
-    if any(H > 1 and t.stride(1) != 1 or S > 1 and t.stride(0) < H for t in lens) or len({t.stride(0) for t in lens if S > 1}) > 1:
-        kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
-        lens = [t for t in (kv_len, sink_len) if t is not None]
-    c = _Attend(S, H, Hq // H, d, T, rows, OBF_F32 if K.dtype == torch.float32 else OBF_BF16, int(bool(causal)), int(window), int(sink), rows,
-                lens[0].stride(0) if lens and S > 1 else 0, apart)
-    c.q_stride = (C.c_int64 * 3)(*_q_strides("Q", Q, d))
+    lens = [m for m in (kv_len, sink_len) if m is not None]
+    _want("kv_len", kv_len, (S, H), torch.int32, contiguous=False)
+    _want("sink_len", sink_len, (S, H), torch.int32, contiguous=False)
+    copy_lens = any(H > 1 and m[1][1] != 1 or S > 1 and m[1][0] < H for m in lens) or len({m[1][0] for m in lens if S > 1}) > 1
+    c = _Attend(S, H, Hq // H, d, T, rows, OBF_F32 if dtype == torch.float32 else OBF_BF16, int(bool(causal)), int(window), int(sink), rows,
+                lens[0][1][0] if lens and S > 1 and not copy_lens else 0, between)
+    c.q_stride = (C.c_int64 * 3)(*_row_strides("Q", Q, d))
     if O is not None:
-        if O.shape != Q.shape or O.dtype != Q.dtype:
-            raise ValueError("O must have the shape and dtype of Q")
-        so = _q_strides("O", O, d)
-        if any(n > 1 and w < d for n, w in zip(O.shape[:3], so)):
+        _want("O", O, Q[0], dtype, contiguous=False)
+        so = _row_strides("O", O, d)
+        if any(n > 1 and w < d for n, w in zip(O[0][:3], so)):
             raise ValueError("O: rows must not overlap")
         c.o_stride = (C.c_int64 * 3)(*so)
-    return c, kv_len, sink_len
+    _want("lse", lse, Q[0][:3], torch.float32)
+    front = 0
+    if prefix_K is not None:
+        if len(prefix_K[0]) != 3 or prefix_K[0][0] != H or prefix_K[0][2] != d or prefix_K[2] != dtype or prefix_V is None:
+            raise ValueError("prefix_K and prefix_V must be [heads, rows, d] of K's dtype")
+        _want("prefix_K", prefix_K, prefix_K[0], dtype)
+        _want("prefix_V", prefix_V, prefix_K[0], dtype)
+        _want("prefix_len", prefix_len, (H,), torch.int32)
+        front = prefix_K[0][1]
+    lib = load_library()
+    need = int(lib.obf_attend_workspace_bytes(C.byref(c), front))
+    if need == 0:
+        raise ObfError(2, lib.obf_last_error().decode())
+    return c, need, front, copy_lens
 
 
-def _at(t: Optional[torch.Tensor]):
+def _addr(t: Optional[torch.Tensor]):
     """Address of a tensor whose strides travel beside it."""
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
-def _attend_out(out, Q):
-    """Output dict of an attention call: O, lse and the workspace, reused from `out` where they fit."""
+class _on:
+    """The GPU of a call, and its current stream there."""
+    def __init__(self, device):
+        self.device = device if device.index != torch.cuda.current_device() else None
+        self.index = device
+
+    def __enter__(self):
+        if self.device is not None:
+            self.back = torch.cuda.device(self.device)
+            self.back.__enter__()
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.device is not None:
+            self.back.__exit__(*exc)
+
+
+def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, prefix=None):
     o = out if out is not None else {}
     if "O" not in o:
         o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
     if "lse" not in o:
         o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
-    if o["lse"].dtype != torch.float32 or o["lse"].shape != Q.shape[:3] or not o["lse"].is_contiguous():
-        raise ValueError("lse must be contiguous float32 [samples, query heads, queries]")
-    return o
-
-
-def _attend_ws(o, c, prefix_stride, device):
+    pk, pv, pl = prefix if prefix is not None else (None, None, None)
+    O, lse = o["O"], o["lse"]
+    c, need, front, copy_lens = _attend_plan(_meta(Q), _meta(K), _meta(V), _meta(O), _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), _meta(pk),
+                                             _meta(pv), _meta(pl), causal, window, sink)
     lib = load_library()
-    need = int(lib.obf_attend_workspace_bytes(C.byref(c), prefix_stride))
-    if need == 0:
-        raise ObfError(2, lib.obf_last_error().decode())
-    if o.get("ws") is None or o["ws"].numel() < need:
-        o["ws"] = torch.empty(need, dtype=torch.uint8, device=device)
-    return o["ws"]
+    with _on(Q.device) as stream:
+        ws = o.get("ws")
+        if ws is None or ws.numel() < need or ws.device != Q.device:
+            ws = o["ws"] = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        if copy_lens:
+            kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
+        if prefix is None:
+            _check(lib.obf_attend(C.byref(c), Q.data_ptr(), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(sink_len), O.data_ptr(), lse.data_ptr(),
+                                  _addr(mass), ws.data_ptr(), ws.numel(), stream))
+        else:
+            _check(lib.obf_attend_shared(C.byref(c), Q.data_ptr(), pk.data_ptr(), pv.data_ptr(), _addr(pl), front, front, K.data_ptr(), V.data_ptr(),
+                                         _addr(kv_len), _addr(sink_len), O.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream))
+    return o
 
 
 def attend(Q, K, V, kv_len=None, causal=True, window=0, sink=0, sink_len=None, mass=None, out=None):
@@ -557,82 +607,79 @@ def attend(Q, K, V, kv_len=None, causal=True, window=0, sink=0, sink_len=None, m
     apart) with kv_len int32 [S,H] rows per head (None: all).  sink_len int32 [S,H]: first rows that stay visible behind a window, per head, in place of
     `sink`.  mass float32 [S,H,rows], in place: accumulated attention weight.  out: a dict returned by an earlier call of the same shape, whose buffers and
     workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws."""
-    _on_device(Q, K=K, V=V, kv_len=kv_len, sink_len=sink_len, mass=mass, **(out or {}))
-    o = _attend_out(out, Q)
-    c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, V=V, mass=mass, O=o["O"])
-    with torch.cuda.device(Q.device):
-        ws = _attend_ws(o, c, 0, Q.device)
-        _check(load_library().obf_attend(C.byref(c), _at(Q), _at(K), _at(V), _at(kv_len), _at(sink_len), _at(o["O"]), _at(o["lse"]), _at(mass),
-                                         _ptr(ws), ws.numel(), _stream()))
-    return o
+    return _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out)
 
 
 def attend_shared(Q, prefix_K, prefix_V, K, V, prefix_len=None, kv_len=None, causal=True, window=0, sink=0, sink_len=None, out=None):
     """obf_attend_shared: as attend, with the rows of a message prefix_K, prefix_V [H,prefix rows,d] that all samples see before their own;
     prefix_len int32 [H] rows per head (None: all)."""
-    _on_device(Q, K=K, V=V, kv_len=kv_len, sink_len=sink_len, prefix_K=prefix_K, prefix_V=prefix_V, prefix_len=prefix_len,
-               **(out or {}))
-    o = _attend_out(out, Q)
-    c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, V=V, O=o["O"])
-    if prefix_K.dim() != 3 or prefix_K.shape[0] != c.n_kv_heads or prefix_K.shape[2] != c.head_dim or prefix_K.dtype != K.dtype:
-        raise ValueError("prefix_K must be [heads, rows, d] of K's dtype")
-    if prefix_V.shape != prefix_K.shape or prefix_V.dtype != K.dtype:
-        raise ValueError("prefix_V does not match prefix_K")
-    prefix_len = _int32("prefix_len", prefix_len, (c.n_kv_heads,))
-    rows = prefix_K.shape[1]
-    with torch.cuda.device(Q.device):
-        ws = _attend_ws(o, c, rows, Q.device)
-        _check(load_library().obf_attend_shared(C.byref(c), _at(Q), _ptr(prefix_K), _ptr(prefix_V), _ptr(prefix_len), rows, rows, _at(K), _at(V),
-                                                _at(kv_len), _at(sink_len), _at(o["O"]), _at(o["lse"]), _ptr(ws), ws.numel(), _stream()))
-    return o
+    return _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, None, out, prefix=(prefix_K, prefix_V, prefix_len))
 
 
 def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sink_len=None, ws=None):
-    """obf_attend_mass: adds to mass float32 [S,H,rows], in place, the attention weight of the rows of K under the lse [S,H*g,T] of an earlier call."""
-    _on_device(Q, K=K, lse=lse, mass=mass, kv_len=kv_len, sink_len=sink_len)
-    c, kv_len, sink_len = _attend_call(Q, K, kv_len, sink_len, causal, window, sink, mass=mass)
-    if lse.dtype != torch.float32 or lse.shape != Q.shape[:3]:
-        raise ValueError("lse must be float32 [samples, query heads, queries]")
-    with torch.cuda.device(Q.device):
-        ws = _attend_ws({"ws": ws}, c, 0, Q.device)
-        _check(load_library().obf_attend_mass(C.byref(c), _at(Q), _at(K), _ptr(lse), _at(kv_len), _at(sink_len), _at(mass), _ptr(ws), ws.numel(), _stream()))
+    """obf_attend_mass: adds to mass float32 [S,H,rows], in place, the attention weight of the rows of K under the lse [S,H*g,T] of an earlier call (whose
+    workspace may be handed over as ws)."""
+    c, need, _, copy_lens = _attend_plan(_meta(Q), _meta(K), None, None, _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), None, None, None, causal,
+                                         window, sink)
+    with _on(Q.device) as stream:
+        if ws is None or ws.numel() < need:
+            ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        if copy_lens:
+            kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
+        _check(load_library().obf_attend_mass(C.byref(c), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), _addr(kv_len), _addr(sink_len), mass.data_ptr(),
+                                              ws.data_ptr(), ws.numel(), stream))
     return mass
+
+
+_EVICT_OUT = ("K_out", "V_out", "mass_out", "pos_out", "idx", "len_out")
+
+
+@functools.lru_cache(maxsize=1024)
+def _evict_plan(K, V, mass, pos, kv_len, sink_len, budget, sink, out_stride, outs):
+    """Checks an eviction by the tensors' metadata.  Returns (heads, out_stride, shapes and dtypes of the outputs)."""
+    if len(K[0]) < 2 or K[2] not in (torch.float32, torch.bfloat16):
+        raise ValueError("K must be [..., rows, d], float32 or bfloat16")
+    _same_device((("K", K), ("V", V), ("mass", mass), ("pos", pos), ("kv_len", kv_len), ("sink_len", sink_len)) + outs)
+    lead, rows, d = tuple(K[0][:-2]), K[0][-2], K[0][-1]
+    _want("K", K, K[0], K[2])
+    _want("V", V, K[0], K[2])
+    _want("mass", mass, lead + (rows,), torch.float32)
+    _want("pos", pos, lead + (rows,), torch.int32)
+    _want("kv_len", kv_len, lead, torch.int32)
+    _want("sink_len", sink_len, lead, torch.int32)
+    given = dict(outs)
+    if out_stride is None:
+        if given.get("K_out") is not None:
+            out_stride = given["K_out"][0][-2]
+        elif sink_len is not None:
+            raise ValueError("out_stride is needed with sink_len")
+        else:
+            out_stride = max(1, min(budget + sink, rows))
+    want = {"K_out": (lead + (out_stride, d), K[2]), "V_out": (lead + (out_stride, d), K[2]), "mass_out": (lead + (out_stride,), torch.float32),
+            "idx": (lead + (out_stride,), torch.int32), "len_out": (lead, torch.int32)}
+    if pos is not None:
+        want["pos_out"] = (lead + (out_stride,), torch.int32)
+    for name, (shape, dtype) in want.items():
+        _want(name, given.get(name), shape, dtype)
+    return int(np.prod(lead)) if lead else 1, out_stride, want
 
 
 def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, sink_len=None, pos=None, out=None, out_stride: Optional[int] = None):
     """obf_evict on K, V [..., rows, d], mass float32 [..., rows] and pos (int32, optional) [..., rows]; leading dimensions = heads, kv_len and sink_len
     int32 [...].  out: buffers to fill, K_out, V_out [..., out_stride, d], mass_out, pos_out, idx [..., out_stride], len_out [...]; those not given are
     allocated with out_stride rows per head (default: sink + budget; needed with sink_len).  Rows behind len_out stay as they are."""
-    if K.dim() < 2 or V.shape != K.shape or V.dtype != K.dtype or K.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("K and V must be [..., rows, d], float32 or bfloat16")
-    lead, rows, d = tuple(K.shape[:-2]), K.shape[-2], K.shape[-1]
-    if mass.dtype != torch.float32 or tuple(mass.shape) != lead + (rows,):
-        raise ValueError("mass must be float32 [..., rows]")
-    pos, kv_len, sink_len = _int32("pos", pos, lead + (rows,)), _int32("kv_len", kv_len, lead), _int32("sink_len", sink_len, lead)
     o = out if out is not None else {}
-    if out_stride is None:
-        if "K_out" in o:
-            out_stride = o["K_out"].shape[-2]
-        elif sink_len is not None:
-            raise ValueError("out_stride is needed with sink_len")
-        else:
-            out_stride = max(1, min(budget + sink, rows))
-    _on_device(K, V=V, mass=mass, pos=pos, kv_len=kv_len, sink_len=sink_len, **o)
-    want = {"K_out": (lead + (out_stride, d), K.dtype), "V_out": (lead + (out_stride, d), K.dtype), "mass_out": (lead + (out_stride,), torch.float32),
-            "idx": (lead + (out_stride,), torch.int32), "len_out": (lead, torch.int32)}
-    if pos is not None:
-        want["pos_out"] = (lead + (out_stride,), torch.int32)
-    for name, (shape, dtype) in want.items():
+    heads, out_stride, want = _evict_plan(_meta(K), _meta(V), _meta(mass), _meta(pos), _meta(kv_len), _meta(sink_len), budget, sink, out_stride,
+                                          tuple((k, _meta(o[k])) for k in _EVICT_OUT if k in o))
+    for name in want:
         if name not in o:
-            o[name] = torch.empty(shape, dtype=dtype, device=K.device)
-        elif tuple(o[name].shape) != shape or o[name].dtype != dtype:
-            raise ValueError(f"{name} must be {dtype} {list(shape)}")
-    dt = OBF_BF16 if K.dtype == torch.bfloat16 else OBF_F32
-    with torch.cuda.device(K.device):
+            o[name] = torch.empty(want[name][0], dtype=want[name][1], device=K.device)
+    rows, d = K.shape[-2], K.shape[-1]
+    with _on(K.device) as stream:
         _check(load_library().obf_evict(
-            int(np.prod(lead)) if lead else 1, d, dt, _ptr(K), _ptr(V), _ptr(mass), _ptr(pos), _ptr(kv_len), rows, rows, budget, recent, _ptr(sink_len), sink,
-            _ptr(o["K_out"]), _ptr(o["V_out"]), _ptr(o["mass_out"]), _ptr(o["pos_out"]) if pos is not None else None, _ptr(o["idx"]), _ptr(o["len_out"]),
-            out_stride, _stream()))
+            heads, d, OBF_BF16 if K.dtype == torch.bfloat16 else OBF_F32, K.data_ptr(), V.data_ptr(), mass.data_ptr(), _addr(pos), _addr(kv_len), rows, rows,
+            budget, recent, _addr(sink_len), sink, o["K_out"].data_ptr(), o["V_out"].data_ptr(), o["mass_out"].data_ptr(),
+            o["pos_out"].data_ptr() if pos is not None else None, o["idx"].data_ptr(), o["len_out"].data_ptr(), out_stride, stream))
     return o
 
 
