@@ -36,6 +36,9 @@ struct AttendArgs {
   float* part_O;             // [ranges][rows][d] and [ranges][rows] (powers of two); used unless there is one range
   float* part_lse;
   int ranges;
+  float* logits;             // nullable: [set][tile of 32 keys][query row of the set][32], in powers of two, -inf where hidden (one tile of rows only)
+  float* mass;               // with logits: the weights go there
+  int logit_tiles;           // tiles of a set, the most that its span can have
   AttendKeys keys[2];
   int n_keys;
   int fused;                 // a workgroup goes over both sets (the message first): keys[1] describes the launch
@@ -112,7 +115,7 @@ constexpr int kAttendFewRows = 32;    // query rows per set of keys up to which 
 constexpr int kAttendTileRows = 128;
 obf_status_t launch_attend_few(const AttendArgs& a, int tile_rows, int d, int dtype, hipStream_t st);
 obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);
-obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);
+obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);   // joins the ranges; adds the logits' weights to the mass
 
 // Accumulated weights of the own rows; part: a sum per range of query rows (unless there is one) and row of a dense cache.
 struct AttendMass { float* mass; float* part; int nsplit, tiles; };

@@ -60,7 +60,8 @@ struct AttendPlan {
   AttendArgs a;
   int tile_rows[2];            // query rows of a workgroup's tile, by set of keys; kAttendTileRows: the kernel of many rows
   int mass_ranges;
-  size_t part_O, part_lse, lse, mass, total;
+  bool keep_logits;
+  size_t part_O, part_lse, lse, mass, logits, total;
 };
 
 static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
@@ -101,7 +102,7 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
     AttendKeys& s = a.keys[i];
     s.row_tiles = (int)((s.row_samples * own_rows + p.tile_rows[i] - 1) / p.tile_rows[i]);
     const long blocks = (long)s.row_tiles * s.samples * a.H, rows = s.stride + (a.fused ? a.keys[0].stride : 0);
-    const long most_ranges = (rows + 255) / 256, want = (2 * kNumCU + blocks - 1) / blocks;
+        const long most_ranges = rows <= 512 ? 1 : (rows + 255) / 256, want = (2 * kNumCU + blocks - 1) / blocks;
     s.nsplit = (int)(want < most_ranges ? want : most_ranges);
     s.split0 = a.ranges;
     a.ranges += s.nsplit;
@@ -117,7 +118,14 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   p.mass_ranges = attend_mass_ranges(a, c->dtype);
   p.mass = at;
   if (p.mass_ranges > 1) at += ((size_t)p.mass_ranges * a.S * a.H * c->token_stride * sizeof(float) + 255) & ~(size_t)255;
+  // Few query rows: the logits are kept and weighted at the end, 4 bytes a row and key written and read beside the 2 d or 4 d of a key, where a second pass
+  // would read the keys again.
+  const bool keep = a.n_keys == 1 && own_rows <= p.tile_rows[0] && own_rows <= kAttendFewRows;
+  p.logits = at;
+  a.logit_tiles = c->token_stride / 32 + 2;        // (the last tiles of a span's two parts are cut off)
+  if (keep) at += (size_t)a.rows * a.logit_tiles * 32 * sizeof(float);
   p.total = at;
+  p.keep_logits = keep;
   return p;
 }
 
@@ -159,9 +167,10 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
     AttendKeys& m = a.keys[0];
     m.K = prefix_K; m.V = prefix_V; m.len = prefix_len; m.len_all = prefix_len_all;
   }
+  if (mass && p.keep_logits) { a.logits = (float*)(base + p.logits); a.mass = mass; }
   OBF_TRY(launch_plan(p, c->head_dim, c->dtype, st));
-  if (a.ranges > 1) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
-  return mass ? launch_attend_mass(a, c->head_dim, c->dtype, lse, AttendMass{mass, (float*)(base + p.mass), p.mass_ranges, 0}, st) : OBF_OK;
+  if (a.ranges > 1 || a.logits) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
+  return mass && !a.logits ? launch_attend_mass(a, c->head_dim, c->dtype, lse, AttendMass{mass, (float*)(base + p.mass), p.mass_ranges, 0}, st) : OBF_OK;
 }
 
 }  // namespace obf

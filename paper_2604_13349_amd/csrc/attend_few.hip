@@ -59,13 +59,28 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
     for (int db = 0; db < DB; ++db) o[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  for (int i = first + wave; i < behind; i += NW) {
+  // A tile's logits are stored behind the next one's loads: the counter of outstanding accesses runs in order, and a wait for loads behind stores would wait
+  // for those too.  (A message's weights are not asked for.)
+  float* logits = a.logits && !second ? a.logits + ((size_t)set * a.logit_tiles * set_rows + (lane & 15)) * 32 + 4 * quad : nullptr;
+  f32x4 held[NB][2];
+  const auto keep = [&](const int i) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      if (16 * nb + (lane & 15) < set_rows) {
+        float* at = logits + ((size_t)i * set_rows + 16 * nb) * 32;
+        *(f32x4*)at = held[nb][0];
+        *(f32x4*)(at + 16) = held[nb][1];
+      }
+  };
+  int i = first + wave;
+  for (; i < behind; i += NW) {
     const bool in_a = i < span.na;
     const int base = in_a ? 32 * i : span.b0 + 32 * (i - span.na), end = in_a ? span.a_end : span.end;
     typename Tile::Keys kf;
     typename Tile::Vals vf;
     Tile::load_keys(kf, K, base, end - 1, lane);
     Tile::load_vals(vf, V, base, end - 1, lane);
+    if (logits && i > first + wave) keep(i - NW);
     // some row does not see some key of the tile
     const bool cut = base + 32 > end || (k.causal && (base + 31 > pmin || (k.window > 0 && base <= pmax - k.window && base + 31 >= sink)));
     float p[NB][2][4];
@@ -84,6 +99,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
           x[b][r] = v;
           mx = fmaxf(mx, v);
         }
+      held[nb][0] = x[0]; held[nb][1] = x[1];
       if (__any(mx > m[nb] + kAttendSlack)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -126,6 +142,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
       Tile::template values<NB>(o, vf, p);
     }
   }
+  if (logits && i > first + wave) keep(i - NW);
 
   // the waves' parts
 #pragma unroll
@@ -173,38 +190,122 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
   }
 }
 
-// Joins the ranges of a query row: O = sum_i 2^(lse_i - lse) O_i.  A lane has four channels; bound by the partial results' bytes.
-template <typename ET, int D>
-__global__ __launch_bounds__(256) void k_attend_join(const AttendArgs a) {
-  constexpr int PIECES = D / 4;
-  const size_t row = (size_t)blockIdx.x * (256 / PIECES) + threadIdx.x / PIECES;
-  const int c = (threadIdx.x % PIECES) * 4;
-  if (row >= (size_t)a.rows) return;
-  float top = -INFINITY;
-  for (int i = 0; i < a.ranges; ++i) top = fmaxf(top, a.part_lse[(size_t)i * a.rows + row]);
-  float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (top > -INFINITY) {
-    for (int i = 0; i < a.ranges; ++i) {
-      const size_t at = (size_t)i * a.rows + row;
-      const float part = a.part_lse[at];
-      if (!(part > -INFINITY)) continue;
-      const float f = attend_exp2(part - top);
-      const float4 x = *(const float4*)(a.part_O + at * D + c);
+// Joins the ranges of a query row, O = sum_i 2^(lse_i - lse) O_i, and turns the logits of the own keys into weights, mass_j += sum_r 2^(x_rj - lse_r).
+// GROUPS lanes share a row's ranges and a lane has four channels, so that the loads of many ranges are in flight; bound by the partial results' bytes, or
+// by its launch.  Workgroups behind those of the rows take 32 tiles of keys of a set each, for which they join the normalisers of its few rows themselves.
+constexpr int JN_THREADS = 256, JN_TILES = 32;
+
+template <typename ET, int D, int GROUPS>
+__global__ __launch_bounds__(JN_THREADS) void k_attend_join(const AttendArgs a, const int row_blocks) {
+  constexpr int PIECES = D / 4, PER_ROW = PIECES * GROUPS, PER_BLOCK = JN_THREADS / PER_ROW;
+  __shared__ float sm_sum[PER_BLOCK][GROUPS][PIECES];
+  __shared__ __attribute__((aligned(16))) float sm_o[PER_BLOCK][GROUPS][D];
+  __shared__ float sm_ref[32];
+  if ((int)blockIdx.x >= row_blocks) {
+    const AttendKeys& k = a.keys[0];
+    constexpr int OWN = 32 * JN_TILES / JN_THREADS, RUN = 8;       // keys of a thread, rows whose logits it has in flight
+    const int chunks = (a.logit_tiles + JN_TILES - 1) / JN_TILES, block = blockIdx.x - row_blocks, set = block / chunks, h = set % a.H, s = set / a.H;
+    const int n = attend_len(k, s, h), first = block % chunks * JN_TILES, set_rows = a.T * a.g;
+    const AttendSpan span = attend_span<32>(k, n, attend_sink(k, s, h), n - a.T, n - 1);
+    if (first >= span.na + span.nb) return;
+    const float* logits[OWN];
+    float* mass[OWN];
+    bool valid[OWN];
+    float x[OWN][RUN], sum[OWN];
+#pragma unroll
+    for (int e = 0; e < OWN; ++e) {
+      const int i = first + (int)threadIdx.x / 32 + e * (JN_THREADS / 32);
+      const bool in_a = i < span.na;
+      const int j = (in_a ? 32 * i : span.b0 + 32 * (i - span.na)) + (int)threadIdx.x % 32;
+      valid[e] = i < span.na + span.nb && j < (in_a ? span.a_end : span.end);
+      logits[e] = a.logits + ((size_t)set * a.logit_tiles + i) * set_rows * 32 + threadIdx.x % 32;
+      mass[e] = a.mass + (size_t)s * k.sample_rows + (size_t)h * k.stride + j;
+      sum[e] = valid[e] ? *mass[e] : 0.f;
+#pragma unroll
+      for (int r = 0; r < RUN; ++r) x[e][r] = valid[e] && r < set_rows ? logits[e][32 * r] : -INFINITY;
+    }
+    if ((int)threadIdx.x < set_rows) {
+      const size_t row = attend_row_number(a, h, attend_row(a, k, s, threadIdx.x));
+      float ref;
+      if (a.ranges > 1) {
+        float top = -INFINITY, sum = 0.f;
+        for (int i = 0; i < a.ranges; ++i) top = fmaxf(top, a.part_lse[(size_t)i * a.rows + row]);
+        for (int i = 0; i < a.ranges; ++i) { const float x = a.part_lse[(size_t)i * a.rows + row]; if (x > -INFINITY) sum += attend_exp2(x - top); }
+        ref = top > -INFINITY ? top + attend_log2(sum) : -INFINITY;
+      } else {
+        ref = a.lse[row] * 1.44269504088896341f;
+      }
+      sm_ref[threadIdx.x] = ref;
+    }
+    __syncthreads();
+    for (int r0 = 0;; r0 += RUN) {
+      float w[OWN] = {};
+#pragma unroll
+      for (int r = 0; r < RUN; ++r) {
+        const float ref = sm_ref[min(r0 + r, 31)];
+#pragma unroll
+        for (int e = 0; e < OWN; ++e) w[e] += x[e][r] == -INFINITY ? 0.f : attend_exp2(x[e][r] - ref);
+      }
+#pragma unroll
+      for (int e = 0; e < OWN; ++e) sum[e] += w[e];
+      if (r0 + RUN >= set_rows) break;
+#pragma unroll
+      for (int e = 0; e < OWN; ++e)
+#pragma unroll
+        for (int r = 0; r < RUN; ++r) x[e][r] = valid[e] && r0 + RUN + r < set_rows ? logits[e][32 * (r0 + RUN + r)] : -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < OWN; ++e) if (valid[e]) *mass[e] = sum[e];
+    return;
+  }
+  const int in_block = threadIdx.x / PER_ROW, group = threadIdx.x / PIECES % GROUPS, piece = threadIdx.x % PIECES, c = piece * 4;
+  const size_t row = (size_t)blockIdx.x * PER_BLOCK + in_block;
+  const bool valid = row < (size_t)a.rows;
+  float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (valid) {
+    const float* lse = a.part_lse + row;
+#pragma unroll 8
+    for (int i = 0; i < a.ranges; ++i) top = fmaxf(top, lse[(size_t)i * a.rows]);
+    const float ref = top > -INFINITY ? top : 0.f;
+#pragma unroll 4
+    for (int i = group; i < a.ranges; i += GROUPS) {
+      const float part = lse[(size_t)i * a.rows];
+      // (a range without visible keys has no O)
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (part != -INFINITY) x = *(const float4*)(a.part_O + ((size_t)i * a.rows + row) * D + c);
+      const float f = attend_exp2(part - ref);
       sum += f;
       v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] /= sum;
   }
+  if (GROUPS > 1) {
+    sm_sum[in_block][group][piece] = sum;
+    *(float4*)&sm_o[in_block][group][c] = make_float4(v[0], v[1], v[2], v[3]);
+    __syncthreads();
+    if (group != 0) return;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) {
+      const float4 x = *(const float4*)&sm_o[in_block][i][c];
+      sum += sm_sum[in_block][i][piece];
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    }
+  }
+  if (!valid) return;
+  const bool any = top != -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = any ? v[i] / sum : 0.f;
   const int t = (int)(row % a.T), hq = (int)(row / a.T % ((size_t)a.H * a.g)), s = (int)(row / a.T / ((size_t)a.H * a.g));
-  if (c == 0 && a.lse) a.lse[row] = top > -INFINITY ? (top + attend_log2(sum)) * 0.69314718055994531f : -INFINITY;
+  if (c == 0 && a.lse) a.lse[row] = any ? (top + attend_log2(sum)) * 0.69314718055994531f : -INFINITY;
   store4((ET*)a.O + (size_t)s * a.os + (size_t)hq * a.oh + (size_t)t * a.ot + c, v);
 }
 
+#ifndef FEW_NW
+#define FEW_NW 4
+#endif
 template <typename ET, int D>
 static void few_launch(const AttendArgs& a, int rows, hipStream_t st) {
   const int blocks = a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0);
-  if (rows == 16) hipLaunchKernelGGL((k_attend_few<ET, D, 1, 4>), dim3(blocks), dim3(256), 0, st, a);
+  if (rows == 16) hipLaunchKernelGGL((k_attend_few<ET, D, 1, FEW_NW>), dim3(blocks), dim3(FEW_NW * 64), 0, st, a);
   else hipLaunchKernelGGL((k_attend_few<ET, D, 2, 2>), dim3(blocks), dim3(128), 0, st, a);
 }
 
@@ -216,17 +317,22 @@ obf_status_t launch_attend_few(const AttendArgs& a, int rows, int d, int dtype, 
   return check_launch("attend");
 }
 
+template <typename ET, int D>
+static void join_launch(const AttendArgs& a, hipStream_t st) {
+  const int mass_blocks = a.logits ? (a.logit_tiles + JN_TILES - 1) / JN_TILES * a.S * a.H : 0;
+  if (a.ranges > 8) {
+    const int per = JN_THREADS / D, rows = (int)((a.rows + per - 1) / per);
+    hipLaunchKernelGGL((k_attend_join<ET, D, 4>), dim3(rows + mass_blocks), dim3(JN_THREADS), 0, st, a, rows);
+  } else {
+    const int per = JN_THREADS * 4 / D, rows = a.ranges > 1 ? (int)((a.rows + per - 1) / per) : 0;
+    hipLaunchKernelGGL((k_attend_join<ET, D, 1>), dim3(rows + mass_blocks), dim3(JN_THREADS), 0, st, a, rows);
+  }
+}
+
 obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st) {
   ProfScope prof(ST_ATTEND_JOIN, st);
-  const int per = 256 / (d / 4);
-  const dim3 grid((unsigned)((a.rows + per - 1) / per));
-  if (dtype == OBF_BF16) {
-    if (d == 128) hipLaunchKernelGGL((k_attend_join<uint16_t, 128>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<uint16_t, 64>), grid, dim3(256), 0, st, a);
-  } else {
-    if (d == 128) hipLaunchKernelGGL((k_attend_join<float, 128>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<float, 64>), grid, dim3(256), 0, st, a);
-  }
+  if (dtype == OBF_BF16) { if (d == 128) join_launch<uint16_t, 128>(a, st); else join_launch<uint16_t, 64>(a, st); }
+  else { if (d == 128) join_launch<float, 128>(a, st); else join_launch<float, 64>(a, st); }
   return check_launch("attend join");
 }
 
