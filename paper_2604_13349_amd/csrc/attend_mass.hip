@@ -94,7 +94,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
-      kf[b][kk].u = *(const uint4*)((const uint16_t*)k.K + (row_base + min(base + 32 * b + (lane & 31), n - 1)) * D + 16 * kk + 8 * half);
+      kf[b][kk].u = *(const TilePiece*)((const uint16_t*)k.K + (row_base + min(base + 32 * b + (lane & 31), n - 1)) * D + 16 * kk + 8 * half);
   float sum[2][16];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
         const int row = 32 * qb + (lane & 31);
         TileFrag q[KK];
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const uint4*)(sm_q[buf] + place_k<D>(row, 2 * kk + half));
+        for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const TilePiece*)(sm_q[buf] + place_k<D>(row, 2 * kk + half));
         const float ref = sm_ref[buf][row];
         const AttendView view = attend_from(sm_view[buf][row], base + 4 * half);
 #pragma unroll

@@ -31,6 +31,11 @@ __device__ __forceinline__ void tile_fill(const uint32_t lds, const uint16_t* Kt
   load_to_lds(lds + wave * 1024, off, attend_uniform(Kt));
 }
 
+template <bool CUT> struct TileCut { static constexpr bool value = CUT; };
+
+// The larger one; where one is no number, whatever (its row is none then).  One instruction: fmaxf would first make its operands quiet.
+__device__ __forceinline__ float tile_max(const float a, const float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
+
 template <int D>
 __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs a) {
   constexpr int KK = D / 16, DB = D / 32, TILE = AT_KEYS * D * 2;
@@ -63,11 +68,9 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   const AttendRow w = attend_row(a, k, ks, min(r, set_rows - 1));
   const uint16_t* qrow = (const uint16_t*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt;
   const int pos = n - a.T + w.t;
-  // the wave's own rows
-  const int wmin = n - a.T + min(row0 + wave * 32, set_rows - 1) / a.g, wmax = n - a.T + min(row0 + wave * 32 + 31, set_rows - 1) / a.g;
   TileFrag q[KK];
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const uint4*)(qrow + 16 * kk + 8 * half);
+  for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const TilePiece*)(qrow + 16 * kk + 8 * half);
 
   f32x16 o[DB];
 #pragma unroll
@@ -77,14 +80,6 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   float m = -INFINITY, l = 0.f;
 
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)sm;
-  const auto fill = [&](const int i, const int buf) {
-    const bool f = i < front_tiles;
-    const int j = i - front_tiles;
-    const bool in_a = j < span.na;
-    const int base = f ? i * AT_KEYS : in_a ? j * AT_KEYS : span.b0 + (j - span.na) * AT_KEYS, end = f ? front : in_a ? span.a_end : span.end;
-    tile_fill<D, false>(lds + buf * TILE, (f ? FK : K) + (size_t)base * D, end - 1 - base, wave, lane);
-    tile_fill<D, true>(lds + (2 + buf) * TILE, (f ? FV : V) + (size_t)base * D, end - 1 - base, wave, lane);
-  };
   // lane's places
   int at_k[KK], at_v[DB];
 #pragma unroll
@@ -93,44 +88,35 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
 #pragma unroll
   for (int db = 0; db < DB; ++db) at_v[db] = vrow * 2 * D + ((db ^ swap_v<D>(vrow)) << 6) + ((lane & 16) << 1) + ((lane & 3) << 3);
 
-  if (first < behind) fill(first, 0);
-  for (int i = first; i < behind; ++i) {
-    const int buf = (i - first) & 1;
-    wait_loads<0>();
-    __syncthreads();                                   // the tile is there, and nobody reads the other one any more
-    if (i + 1 < behind) fill(i + 1, buf ^ 1);
-    const bool f = i < front_tiles;
-    const int j0 = i - front_tiles;
-    const bool in_a = j0 < span.na;
-    const int base = f ? i * AT_KEYS : in_a ? j0 * AT_KEYS : span.b0 + (j0 - span.na) * AT_KEYS, end = f ? front : in_a ? span.a_end : span.end;
-    // some row of the wave does not see some key of the tile; none sees any
-    const bool causal = k.causal && !f;
-    const bool cut = base + AT_KEYS > end || (causal && (base + AT_KEYS - 1 > wmin || (k.window > 0 && base <= wmax - k.window && base + AT_KEYS - 1 >= sink)));
-    if (causal && (base > wmax || (k.window > 0 && base + AT_KEYS - 1 <= wmin - k.window && base >= sink))) continue;
-    const char* tk = sm + buf * TILE;
-    const char* tv = sm + (2 + buf) * TILE;
+  // One tile.  CUT: with the masks.
+  const auto take = [&](const auto tag, const char* tk, const char* tv, const int base, const int end, const int causal) {
+    constexpr bool CUT = decltype(tag)::value;
     f32x16 x[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       TileFrag kf[KK];
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kf[kk].u = *(const uint4*)(tk + b * 32 * 2 * D + at_k[kk]);
+      for (int kk = 0; kk < KK; ++kk) kf[kk].u = *(const TilePiece*)(tk + b * 32 * 2 * D + at_k[kk]);
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[b][e] = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk].v, q[kk].v, x[b], 0, 0, 0);
     }
     const AttendView view = attend_view(causal, k.window, sink, pos, end, base + 4 * half);
-    if (cut) {
+    if (CUT) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[b][e] = attend_sees(view, 32 * b + 8 * (e >> 2) + (e & 3)) ? x[b][e] : -INFINITY;
     }
-    float mx = fmaxf(x[0][0], x[1][0]);
+    float top[4];
 #pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, fmaxf(x[0][e], x[1][e]));
-    mx *= a.scale2;
+    for (int c = 0; c < 4; ++c) top[c] = x[c >> 1][8 * (c & 1)];
+#pragma unroll
+    for (int e = 1; e < 8; ++e)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) top[c] = tile_max(top[c], x[c >> 1][8 * (c & 1) + e]);
+    const float mx = tile_max(tile_max(top[0], top[1]), tile_max(top[2], top[3])) * a.scale2;
     if (__any(mx > m + kAttendSlack)) {
       const float next = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
       const float scale = next > -INFINITY ? attend_exp2(m - next) : 1.f;
@@ -150,12 +136,11 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
       s0 += x[0][e]; s1 += x[1][e];
     }
     l += s0 + s1;
-    // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
-    if (cut && causal) {
+    if (CUT && causal) {
+      // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
       bool bad = false;
       for (int e = lane; e < TILE / 16; e += 64) {
-        const uint4 u = *(const uint4*)(tv + e * 16);
-        const uint32_t y[4] = {u.x, u.y, u.z, u.w};
+        const TilePiece y = *(const TilePiece*)(tv + e * 16);
 #pragma unroll
         for (int c = 0; c < 4; ++c) bad |= ((y[c] & 0x7f80u) == 0x7f80u) | ((y[c] & 0x7f800000u) == 0x7f800000u);
       }
@@ -176,7 +161,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
                 o[db][e] = fmaf(wt, __uint_as_float((uint32_t)row[32 * db + 8 * (e >> 2) + 4 * half + (e & 3)] << 16), o[db][e]);
           }
         }
-        continue;
+        return;
       }
     }
 #pragma unroll
@@ -191,6 +176,46 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
         v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tv + at_v[db] + (t * 16 + 8) * 2 * D));
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p.v, o[db], 0, 0, 0);
       }
+    }
+  };
+
+  // Tile i: keys base .. end - 1 of the message (front) or of the own rows, 64 at most.  cut: some row of the workgroup does not see some key of it.
+  struct At { bool front, cut; int base, end; };
+  const auto locate = [&](const int i) {
+    const int j = i - front_tiles;
+    At t;
+    t.front = j < 0;
+    t.base = (t.front ? i : j) * AT_KEYS;
+    t.end = t.front ? front : span.a_end;
+    if (j >= span.na) { t.base = span.b0 + (j - span.na) * AT_KEYS; t.end = span.end; }
+    const bool causal = k.causal && !t.front;
+    t.cut = t.base + AT_KEYS > t.end || (causal && (t.base + AT_KEYS - 1 > pmin || (k.window > 0 && t.base <= pmax - k.window && t.base + AT_KEYS - 1 >= sink)));
+    return t;
+  };
+  const auto fill = [&](const int buf, const At& t) {
+    const uint16_t *from_k = K, *from_v = V;
+    if (t.front) { from_k = FK; from_v = FV; }
+    tile_fill<D, false>(lds + buf * TILE, from_k + (size_t)t.base * D, t.end - 1 - t.base, wave, lane);
+    tile_fill<D, true>(lds + (2 + buf) * TILE, from_v + (size_t)t.base * D, t.end - 1 - t.base, wave, lane);
+  };
+  At now = {false, false, 0, 0}, next = {false, false, 0, 0};
+  int i = first, buf = 0;
+  // Tile i is there, nobody reads the other one any more: the loads of tile i + 1.
+  const auto begin = [&]() {
+    wait_loads<0>();
+    __syncthreads();
+    if (i + 1 < behind) { next = locate(i + 1); fill(buf ^ 1, next); }
+  };
+  if (first < behind) { now = locate(first); fill(0, now); }
+  // (two loops, so that the common one has the registers to itself)
+  while (i < behind) {
+    for (; i < behind && !now.cut; ++i, buf ^= 1, now = next) {
+      begin();
+      take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, now.base, now.end, 0);
+    }
+    for (; i < behind && now.cut; ++i, buf ^= 1, now = next) {
+      begin();
+      take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, now.base, now.end, k.causal && !now.front);
     }
   }
 

@@ -9,7 +9,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t TilePiece;
 
-union TileFrag { uint4 u; bf16x8 v; s16x4 h[2]; uint32_t w[4]; };
+union TileFrag { TilePiece u; bf16x8 v; s16x4 h[2]; uint32_t w[4]; };
 
 // Places in a tile of rows of 2 D bytes.
 template <int D> __device__ __forceinline__ int place_k(const int row, const int piece) {       // 16-byte pieces
