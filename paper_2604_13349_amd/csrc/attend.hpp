@@ -65,30 +65,33 @@ __device__ __forceinline__ int attend_sink(const AttendKeys& k, const int sample
   return max(0, k.sink_len ? k.sink_len[(size_t)sample * k.len_stride + h] : k.sink);
 }
 
-// The keys that the query rows at positions pmin .. pmax of a head see: [0, a_end) and [b0, end), in na and nb tiles of TK.
-struct AttendSpan { int a_end, b0, end, na, nb; };
-template <int TK>
+// The keys that the query rows at positions pmin .. pmax of a head see, as one list of `count`: entry v is key v below `split` (the first rows, where the window
+// begins behind them) and key v + skip from there on.
+struct AttendSpan { int count, split, skip; };
 __device__ __forceinline__ AttendSpan attend_span(const AttendKeys& k, const int n, const int sink, const int pmin, const int pmax) {
-  AttendSpan s;
-  s.end = k.causal ? min(n, pmax + 1) : n;
-  s.a_end = 0; s.b0 = 0;
+  AttendSpan s = {max(0, k.causal ? min(n, pmax + 1) : n), 0, 0};
   if (k.window > 0) {
-    const int lo = pmin - k.window + 1;
-    const int first = min(sink, s.end);
-    if (lo > first) { s.a_end = first; s.b0 = lo; }
+    const int lo = pmin - k.window + 1, first = min(sink, s.count);
+    if (lo > first) { s.split = first; s.skip = lo - first; s.count = max(first, s.count - s.skip); }
   }
-  s.na = (s.a_end + TK - 1) / TK;
-  s.nb = s.end > s.b0 ? (s.end - s.b0 + TK - 1) / TK : 0;
   return s;
 }
+__device__ __forceinline__ int attend_key(const AttendSpan s, const int v) { return v < s.split ? v : v + s.skip; }
 
-// The keys below `end` that the query at position p sees: j <= hi and (j > lo or j < first); numbers relative to `from`, so that a tile's keys are constants.
+// The entries of a span that the query at position p sees: v <= hi and (v > lo or v < first); numbers relative to `from`, so that a tile's entries are
+// constants.  (Where the span skips rows, every query sees those in front.)
 struct AttendView { int hi, lo, first; };
-__device__ __forceinline__ AttendView attend_view(const int causal, const int window, const int sink, const int p, const int end, const int from = 0) {
-  return {(causal ? min(p, end - 1) : end - 1) - from, (causal && window > 0 ? p - window : -1) - from, sink - from};
+__device__ __forceinline__ AttendView attend_view(const AttendKeys& k, const AttendSpan s, const int sink, const int p, const int from = 0) {
+  return {(k.causal ? min(p - s.skip, s.count - 1) : s.count - 1) - from, (k.causal && k.window > 0 ? p - k.window - s.skip : -1) - from,
+          (s.skip > 0 ? s.split : sink) - from};
 }
 __device__ __forceinline__ AttendView attend_from(const AttendView v, const int from) { return {v.hi - from, v.lo - from, v.first - from}; }
 __device__ __forceinline__ bool attend_sees(const AttendView v, const int j) { return (j <= v.hi) & ((j > v.lo) | (j < v.first)); }
+// Whether some query at pmin .. pmax does not see some of the entries v .. v + width - 1.
+__device__ __forceinline__ bool attend_cut(const AttendKeys& k, const AttendSpan s, const int sink, const int pmin, const int pmax, const int v, const int width) {
+  const int last = v + width - 1;
+  return last >= s.count || (k.causal && (last > pmin - s.skip || (k.window > 0 && v <= pmax - k.window - s.skip && last >= (s.skip > 0 ? s.split : sink))));
+}
 
 // Query row r of the rows that read a set of keys: query head, query and sample, and the row's number.
 struct AttendRow { int s, gi, t; };

@@ -35,8 +35,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
   const int n = attend_len(k, ks, h), sink = attend_sink(k, ks, h);
   // (a message is not causal: its queries have no positions)
   const int pmin = n - a.T + row0 / a.g, pmax = n - a.T + (min(row0 + ROWS, set_rows) - 1) / a.g;
-  const AttendSpan span = attend_span<32>(k, n, sink, pmin, pmax);
-  const int tiles = span.na + span.nb, per = max(NW, (tiles + k.nsplit - 1) / k.nsplit);   // (a short head does not use all its ranges)
+  const AttendSpan span = attend_span(k, n, sink, pmin, pmax);
+  const int tiles = (span.count + 31) / 32, per = max(NW, (tiles + k.nsplit - 1) / k.nsplit);   // (a short head does not use all its ranges)
   const int first = split * per, behind = min(tiles, first + per);
   const bool joined = a.ranges > 1;
   const ET* K = (const ET*)k.K + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
@@ -74,21 +74,19 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
   };
   int i = first + wave;
   for (; i < behind; i += NW) {
-    const bool in_a = i < span.na;
-    const int base = in_a ? 32 * i : span.b0 + 32 * (i - span.na), end = in_a ? span.a_end : span.end;
+    const int base = 32 * i;
     typename Tile::Keys kf;
     typename Tile::Vals vf;
-    Tile::load_keys(kf, K, base, end - 1, lane);
-    Tile::load_vals(vf, V, base, end - 1, lane);
+    Tile::load_keys(kf, K, span, base, lane);
+    Tile::load_vals(vf, V, span, base, lane);
     if (logits && i > first + wave) keep(i - NW);
-    // some row does not see some key of the tile
-    const bool cut = base + 32 > end || (k.causal && (base + 31 > pmin || (k.window > 0 && base <= pmax - k.window && base + 31 >= sink)));
+    const bool cut = attend_cut(k, span, sink, pmin, pmax, base, 32);
     float p[NB][2][4];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       f32x4 x[2];
       Tile::scores(x, kf, q[nb]);
-      const AttendView view = attend_view(k.causal, k.window, sink, pos[nb], end, base + 4 * quad);
+      const AttendView view = attend_view(k, span, sink, pos[nb], base + 4 * quad);
       float mx = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -119,9 +117,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
     // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
     if (cut && k.causal && a.T > 1 && __any(Tile::not_finite(vf))) {
 #pragma unroll 1
-      for (int j = base; j < min(end, base + 32); ++j) {
-        const ET* krow = K + (size_t)j * D;
-        const ET* row = V + (size_t)j * D;
+      for (int v = base; v < min(span.count, base + 32); ++v) {
+        const ET* krow = K + few_row<D>(span, v);
+        const ET* row = V + few_row<D>(span, v);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const AttendRow w = attend_row(a, k, ks, min(row0 + 16 * nb + (lane & 15), set_rows - 1));
@@ -129,7 +127,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
           float dot = 0.f;
 #pragma unroll 1
           for (int c = 0; c < D; ++c) dot = fmaf(Tile::value(krow, c), Tile::value(qrow, c), dot);
-          if (attend_sees(attend_view(k.causal, k.window, sink, pos[nb], end), j)) {
+          if (attend_sees(attend_view(k, span, sink, pos[nb]), v)) {
             const float wt = attend_exp2(fmaf(dot, a.scale2, -(m[nb] > -INFINITY ? m[nb] : 0.f)));
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -206,8 +204,8 @@ __global__ __launch_bounds__(JN_THREADS) void k_attend_join(const AttendArgs a, 
     constexpr int OWN = 32 * JN_TILES / JN_THREADS, RUN = 8;       // keys of a thread, rows whose logits it has in flight
     const int chunks = (a.logit_tiles + JN_TILES - 1) / JN_TILES, block = blockIdx.x - row_blocks, set = block / chunks, h = set % a.H, s = set / a.H;
     const int n = attend_len(k, s, h), first = block % chunks * JN_TILES, set_rows = a.T * a.g;
-    const AttendSpan span = attend_span<32>(k, n, attend_sink(k, s, h), n - a.T, n - 1);
-    if (first >= span.na + span.nb) return;
+    const AttendSpan span = attend_span(k, n, attend_sink(k, s, h), n - a.T, n - 1);
+    if (32 * first >= span.count) return;
     const float* logits[OWN];
     float* mass[OWN];
     bool valid[OWN];
@@ -215,9 +213,8 @@ __global__ __launch_bounds__(JN_THREADS) void k_attend_join(const AttendArgs a, 
 #pragma unroll
     for (int e = 0; e < OWN; ++e) {
       const int i = first + (int)threadIdx.x / 32 + e * (JN_THREADS / 32);
-      const bool in_a = i < span.na;
-      const int j = (in_a ? 32 * i : span.b0 + 32 * (i - span.na)) + (int)threadIdx.x % 32;
-      valid[e] = i < span.na + span.nb && j < (in_a ? span.a_end : span.end);
+      const int v = 32 * i + (int)threadIdx.x % 32, j = attend_key(span, v);
+      valid[e] = v < span.count;
       logits[e] = a.logits + ((size_t)set * a.logit_tiles + i) * set_rows * 32 + threadIdx.x % 32;
       mass[e] = a.mass + (size_t)s * k.sample_rows + (size_t)h * k.stride + j;
       sum[e] = valid[e] ? *mass[e] : 0.f;

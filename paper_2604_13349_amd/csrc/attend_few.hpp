@@ -4,6 +4,9 @@
 
 namespace obf {
 
+// Place of entry v of a span; entries behind it repeat the last one.
+template <int D> __device__ __forceinline__ size_t few_row(const AttendSpan s, const int v) { return (size_t)attend_key(s, min(v, s.count - 1)) * D; }
+
 template <typename ET, int D> struct FewTile;
 
 // bf16: operands of v_mfma_f32_16x16x32_bf16, lane l: row l % 16, elements 8 (l / 16) .. + 7 of 32
@@ -21,20 +24,20 @@ template <int D> struct FewTile<uint16_t, D> {
 #pragma unroll
     for (int c = 0; c < KV; ++c) q.q[c].u = p[4 * c];
   }
-  static __device__ __forceinline__ void load_keys(Keys& f, const uint16_t* K, const int base, const int last, const int lane) {
+  static __device__ __forceinline__ void load_keys(Keys& f, const uint16_t* K, const AttendSpan span, const int base, const int lane) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const uint4* p = (const uint4*)(K + (size_t)min(base + 16 * b + (lane & 15), last) * D) + (lane >> 4);
+      const uint4* p = (const uint4*)(K + few_row<D>(span, base + 16 * b + (lane & 15))) + (lane >> 4);
 #pragma unroll
       for (int c = 0; c < KV; ++c) f.k[b][c].u = p[4 * c];
     }
   }
-  static __device__ __forceinline__ void load_vals(Vals& f, const uint16_t* V, const int base, const int last, const int lane) {
+  static __device__ __forceinline__ void load_vals(Vals& f, const uint16_t* V, const AttendSpan span, const int base, const int lane) {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        f.v[b][r] = *(const vrow*)(V + (size_t)min(base + 16 * b + 4 * (lane >> 4) + r, last) * D + DB * (lane & 15));
+        f.v[b][r] = *(const vrow*)(V + few_row<D>(span, base + 16 * b + 4 * (lane >> 4) + r) + DB * (lane & 15));
   }
   static __device__ __forceinline__ void scores(f32x4 (&x)[2], const Keys& k, const Query& q) {
 #pragma unroll
@@ -98,20 +101,20 @@ template <int D> struct FewTile<float, D> {
 #pragma unroll
     for (int c = 0; c < KV; ++c) q.q[c] = *(const f32x4*)(row + 16 * c + 4 * (lane >> 4));
   }
-  static __device__ __forceinline__ void load_keys(Keys& f, const float* K, const int base, const int last, const int lane) {
+  static __device__ __forceinline__ void load_keys(Keys& f, const float* K, const AttendSpan span, const int base, const int lane) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const float* p = K + (size_t)min(base + 16 * b + (lane & 15), last) * D + 4 * (lane >> 4);
+      const float* p = K + few_row<D>(span, base + 16 * b + (lane & 15)) + 4 * (lane >> 4);
 #pragma unroll
       for (int c = 0; c < KV; ++c) f.k[b][c] = *(const f32x4*)(p + 16 * c);
     }
   }
-  static __device__ __forceinline__ void load_vals(Vals& f, const float* V, const int base, const int last, const int lane) {
+  static __device__ __forceinline__ void load_vals(Vals& f, const float* V, const AttendSpan span, const int base, const int lane) {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float* p = V + (size_t)min(base + 16 * b + 4 * (lane >> 4) + r, last) * D + 4 * (lane & 15);
+        const float* p = V + few_row<D>(span, base + 16 * b + 4 * (lane >> 4) + r) + 4 * (lane & 15);
 #pragma unroll
         for (int c = 0; c < VV; ++c) f.v[b][r][c] = *(const f32x4*)(p + 64 * c);
       }

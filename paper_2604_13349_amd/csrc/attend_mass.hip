@@ -29,7 +29,8 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
   if (t0 >= t1) return;
   const size_t first_row = (size_t)s * k.sample_rows + (size_t)h * k.stride;
   typename Tile::Keys kf;
-  Tile::load_keys(kf, (const ET*)k.K + first_row * D, base, n - 1, lane);
+  const AttendSpan all = {n, 0, 0};
+  Tile::load_keys(kf, (const ET*)k.K + first_row * D, all, base, lane);
   float sum[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   const int behind = t1 * a.g;
   for (int r0 = t0 * a.g; r0 < behind; r0 += 16) {
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
     const bool counts = r < behind && !(row_lse == -INFINITY);       // (a row that sees nothing has weights of 0)
     f32x4 x[2];
     Tile::scores(x, kf, q);
-    AttendView view = attend_view(k.causal, k.window, sink, p0 + w.t, n, base + 4 * quad);
+    AttendView view = attend_view(k, all, sink, p0 + w.t, base + 4 * quad);
     if (!counts) view.hi = -1;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -89,6 +90,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
   const int steps = (int)(((long)max(0, t1 - t0) * a.g + MT_ROWS - 1) / MT_ROWS), per = (steps + ms.nsplit - 1) / ms.nsplit;
   const int first = t0 * a.g + split * per * MT_ROWS, behind = (int)min((long)t1 * a.g, (long)first + (long)per * MT_ROWS);
   const size_t row_base = (size_t)s * k.sample_rows + (size_t)h * k.stride;
+  const AttendSpan all = {n, 0, 0};
   TileFrag kf[2][KK];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
     const int i = (int)(threadIdx.x % MT_ROWS);
     const AttendRow w = attend_row(a, at, s, min(i, most));
     const float v = lse[attend_row_number(a, h, w)];
-    next_view = attend_view(k.causal, k.window, sink, p0 + w.t, n);
+    next_view = attend_view(k, all, sink, p0 + w.t);
     // (a row that sees nothing has weights of 0, and so has one behind the range)
     const bool counts = i <= most && !(v == -INFINITY);
     next_ref = counts ? v * 1.44269504088896341f : INFINITY;
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
     if (more) fetch(r0 + MT_ROWS);
     // some row of the step does not see some key of the wave; none sees any
     const int wmin = p0 + r0 / a.g, wmax = p0 + (min(r0 + MT_ROWS, behind) - 1) / a.g;
-    const bool cut = r0 + MT_ROWS > behind || (k.causal && (base + 63 > wmin || (k.window > 0 && base <= wmax - k.window && base + 63 >= sink)));
+    const bool cut = r0 + MT_ROWS > behind || attend_cut(k, all, sink, wmin, wmax, base, 64);
     const bool none = base >= n || (k.causal && (base > wmax || (k.window > 0 && base + 63 <= wmin - k.window && base >= sink)));
     if (!none) {
 #pragma unroll

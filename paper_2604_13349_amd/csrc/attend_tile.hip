@@ -17,18 +17,22 @@ namespace obf {
 constexpr int AT_WAVES = 4, AT_THREADS = AT_WAVES * 64, AT_ROWS = AT_WAVES * 32, AT_KEYS = 64;
 static_assert(AT_ROWS == kAttendTileRows, "rows of a workgroup's tile");
 
-// 64 rows of K (or V) from Kt on (rows past `last` repeat it) to LDS.
+// Entries v .. v + 63 of a span (those behind it repeat the last one) of K, or of V, to LDS.
 template <int D, bool VALUES>
-__device__ __forceinline__ void tile_fill(const uint32_t lds, const uint16_t* Kt, const int last, const int wave, const int lane) {
+__device__ __forceinline__ void tile_fill(const uint32_t lds, const uint16_t* X, const AttendSpan span, const int v, const int wave, const int lane) {
   constexpr int PIECES = D / 8, LOADS = AT_KEYS * PIECES / AT_THREADS, ROWS = AT_THREADS / PIECES;   // rows per load of the workgroup
+  // offsets from the first entry: 32 bits without a sign, what the rows of a head span
+  const int start = attend_uniform(attend_key(span, v)), jump = attend_uniform(v < span.split ? span.split - v : AT_KEYS), skip = attend_uniform(span.skip);
+  const int last = attend_uniform(span.count - 1 - v);
   uint32_t off[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
     const int at = wave * 64 + lane, row = i * ROWS + at / PIECES, place = at % PIECES;
     const int piece = VALUES ? place ^ (swap_v<D>(row) << 2) : place ^ (D == 128 ? row & 15 : (row >> 1) & 7);
-    off[i] = (uint32_t)(min(row, last) * 2 * D + piece * 16);
+    const int r = min(row, last);
+    off[i] = (uint32_t)(r + (r >= jump ? skip : 0)) * (2u * D) + piece * 16;
   }
-  load_to_lds(lds + wave * 1024, off, attend_uniform(Kt));
+  load_to_lds(lds + wave * 1024, off, attend_uniform(X + (size_t)start * D));
 }
 
 template <bool CUT> struct TileCut { static constexpr bool value = CUT; };
@@ -55,9 +59,9 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   const int lane = threadIdx.x & 63, wave = attend_uniform(threadIdx.x >> 6), half = lane >> 5;
   const int n = attend_uniform(attend_len(k, ks, h)), sink = attend_uniform(attend_sink(k, ks, h));
   const int pmin = n - a.T + row0 / a.g, pmax = n - a.T + (min(row0 + AT_ROWS, set_rows) - 1) / a.g;
-  const AttendSpan span = attend_span<AT_KEYS>(k, n, sink, pmin, pmax);
+  const AttendSpan span = attend_span(k, n, sink, pmin, pmax);
   const int front = a.fused ? attend_uniform(attend_len(a.keys[0], 0, h)) : 0, front_tiles = (front + AT_KEYS - 1) / AT_KEYS;
-  const int tiles = front_tiles + span.na + span.nb, per = (tiles + k.nsplit - 1) / k.nsplit;
+  const int tiles = front_tiles + (span.count + AT_KEYS - 1) / AT_KEYS, per = (tiles + k.nsplit - 1) / k.nsplit;
   const int first = split * per, behind = min(tiles, first + per);
   const uint16_t* K = (const uint16_t*)k.K + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
   const uint16_t* V = (const uint16_t*)k.V + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
@@ -89,7 +93,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   for (int db = 0; db < DB; ++db) at_v[db] = vrow * 2 * D + ((db ^ swap_v<D>(vrow)) << 6) + ((lane & 16) << 1) + ((lane & 3) << 3);
 
   // One tile.  CUT: with the masks.
-  const auto take = [&](const auto tag, const char* tk, const char* tv, const int base, const int end, const int causal) {
+  const auto take = [&](const auto tag, const char* tk, const char* tv, const AttendKeys& kt, const AttendSpan st, const int base) {
     constexpr bool CUT = decltype(tag)::value;
     f32x16 x[2];
 #pragma unroll
@@ -102,7 +106,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk].v, q[kk].v, x[b], 0, 0, 0);
     }
-    const AttendView view = attend_view(causal, k.window, sink, pos, end, base + 4 * half);
+    const AttendView view = attend_view(kt, st, sink, pos, base + 4 * half);
     if (CUT) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -136,7 +140,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
       s0 += x[0][e]; s1 += x[1][e];
     }
     l += s0 + s1;
-    if (CUT && causal) {
+    if (CUT && kt.causal) {
       // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
       bool bad = false;
       for (int e = lane; e < TILE / 16; e += 64) {
@@ -146,19 +150,19 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
       }
       if (__any(bad)) {
 #pragma unroll 1
-        for (int j = base; j < min(end, base + AT_KEYS); ++j) {
-          const uint16_t* krow = K + (size_t)j * D;
-          const uint16_t* row = V + (size_t)j * D;
+        for (int e = base; e < min(st.count, base + AT_KEYS); ++e) {
+          const uint16_t* krow = K + (size_t)attend_key(st, e) * D;
+          const uint16_t* row = V + (size_t)attend_key(st, e) * D;
           float dot = 0.f;
 #pragma unroll 1
           for (int c = 0; c < D; ++c) dot = fmaf(__uint_as_float((uint32_t)krow[c] << 16), __uint_as_float((uint32_t)qrow[c] << 16), dot);
-          if (attend_sees(view, j - base - 4 * half)) {
+          if (attend_sees(view, e - base - 4 * half)) {
             const float wt = attend_exp2(fmaf(dot, a.scale2, -ref));
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                o[db][e] = fmaf(wt, __uint_as_float((uint32_t)row[32 * db + 8 * (e >> 2) + 4 * half + (e & 3)] << 16), o[db][e]);
+              for (int c = 0; c < 16; ++c)
+                o[db][c] = fmaf(wt, __uint_as_float((uint32_t)row[32 * db + 8 * (c >> 2) + 4 * half + (c & 3)] << 16), o[db][c]);
           }
         }
         return;
@@ -179,26 +183,24 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
     }
   };
 
-  // Tile i: keys base .. end - 1 of the message (front) or of the own rows, 64 at most.  cut: some row of the workgroup does not see some key of it.
-  struct At { bool front, cut; int base, end; };
+  // Tile i: 64 entries of the message (front) or of the own span.  cut: some row of the workgroup does not see some of them.
+  const AttendSpan front_span = {front, 0, 0};
+  struct At { bool front, cut; int base; };
   const auto locate = [&](const int i) {
-    const int j = i - front_tiles;
     At t;
-    t.front = j < 0;
-    t.base = (t.front ? i : j) * AT_KEYS;
-    t.end = t.front ? front : span.a_end;
-    if (j >= span.na) { t.base = span.b0 + (j - span.na) * AT_KEYS; t.end = span.end; }
-    const bool causal = k.causal && !t.front;
-    t.cut = t.base + AT_KEYS > t.end || (causal && (t.base + AT_KEYS - 1 > pmin || (k.window > 0 && t.base <= pmax - k.window && t.base + AT_KEYS - 1 >= sink)));
+    t.front = i < front_tiles;
+    t.base = (t.front ? i : i - front_tiles) * AT_KEYS;
+    t.cut = t.front ? t.base + AT_KEYS > front : attend_cut(k, span, sink, pmin, pmax, t.base, AT_KEYS);
     return t;
   };
   const auto fill = [&](const int buf, const At& t) {
     const uint16_t *from_k = K, *from_v = V;
-    if (t.front) { from_k = FK; from_v = FV; }
-    tile_fill<D, false>(lds + buf * TILE, from_k + (size_t)t.base * D, t.end - 1 - t.base, wave, lane);
-    tile_fill<D, true>(lds + (2 + buf) * TILE, from_v + (size_t)t.base * D, t.end - 1 - t.base, wave, lane);
+    AttendSpan from = span;
+    if (t.front) { from_k = FK; from_v = FV; from = front_span; }
+    tile_fill<D, false>(lds + buf * TILE, from_k, from, t.base, wave, lane);
+    tile_fill<D, true>(lds + (2 + buf) * TILE, from_v, from, t.base, wave, lane);
   };
-  At now = {false, false, 0, 0}, next = {false, false, 0, 0};
+  At now = {false, false, 0}, next = {false, false, 0};
   int i = first, buf = 0;
   // Tile i is there, nobody reads the other one any more: the loads of tile i + 1.
   const auto begin = [&]() {
@@ -211,11 +213,14 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   while (i < behind) {
     for (; i < behind && !now.cut; ++i, buf ^= 1, now = next) {
       begin();
-      take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, now.base, now.end, 0);
+      take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, k, span, now.base);
     }
     for (; i < behind && now.cut; ++i, buf ^= 1, now = next) {
       begin();
-      take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, now.base, now.end, k.causal && !now.front);
+      AttendKeys kt = k;
+      AttendSpan st = span;
+      if (now.front) { kt.causal = 0; kt.window = 0; st = front_span; }
+      take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, kt, st, now.base);
     }
   }
 

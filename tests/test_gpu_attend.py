@@ -426,3 +426,44 @@ def test_a_relay_its_receivers_and_their_caches_cut():
         o = B.attend_shared(q.cuda(), msg_K, msg_V, e["K_out"], e["V_out"], prefix_len=msg_len, kv_len=n, **kw)
         _check("O", o["O"], O, tO)
         _check("lse", o["lse"], lse, tl)
+
+
+@pytest.mark.parametrize("T", [1, 60])
+def test_caches_whose_offsets_pass_32_bits(T):
+    """Two heads of 2^24 rows of storage: the second head, and the last rows of either, lie more than 2^32 bytes behind the start."""
+    B = _b()
+    H, g, d, rows = 2, 2, 128, 1 << 24
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    K, V = (torch.zeros((1, H, rows, d), dtype=BF, device="cuda") for _ in range(2))
+    Q, k, v = (x.cuda() for x in _make(61, BF, d, 1, H, g, T, 700))
+    n = torch.tensor([[rows, rows - 5]], dtype=torch.int32, device="cuda")
+    for h in range(H):
+        at = int(n[0, h])
+        K[0, h, :4], V[0, h, :4] = k[0, h, :4], v[0, h, :4]
+        K[0, h, at - 696:at], V[0, h, at - 696:at] = k[0, h, 4:], v[0, h, 4:]
+    kw = dict(window=500, sink=4)
+    o = B.attend(Q, K, V, kv_len=n, **kw)
+    small = B.attend(Q, k, v, **kw)
+    assert (o["lse"] - small["lse"]).abs().max() <= 1e-5 and (o["O"].float() - small["O"].float()).abs().max() <= 2.0 ** -7 * small["O"].float().abs().max()
+    if T > 1:
+        return
+    # without a window: the other rows' logits are 0, their values too; and the rows of largest weight of such a cache
+    K[0, :, 1 << 23], V[0, :, 1 << 23] = Q[0, ::g, 0] * 0.5, 1.0
+    o = B.attend(Q, K, V, kv_len=n, mass=(mass := torch.zeros((1, H, rows), device="cuda")))
+    for h in range(H):
+        at = int(n[0, h])
+        seen = torch.cat([torch.arange(4), torch.tensor([1 << 23]), torch.arange(at - 696, at)]).cuda()
+        x = (Q[0, h * g:(h + 1) * g, 0].double() @ K[0, h, seen].double().t()) / math.sqrt(d)
+        lse = torch.log(torch.exp(x).sum(dim=1) + (at - 701))
+        w = torch.exp(x - lse[:, None])
+        assert (o["lse"][0, h * g:(h + 1) * g, 0].double() - lse).abs().max() <= 2e-5
+        assert (o["O"][0, h * g:(h + 1) * g, 0].double() - w @ V[0, h, seen].double()).abs().max() <= 2.0 ** -7 * (w @ V[0, h, seen].double()).abs().max()
+        assert (mass[0, h, seen].double() - w.sum(dim=0)).abs().max() <= 1e-4 * w.sum(dim=0).max()
+    e = B.evict(K, V, mass, 300, kv_len=n, recent=50, sink=4)
+    for h in range(H):
+        at = int(n[0, h])
+        worth = mass[0, h, :at].clone()
+        worth[:4] = worth[at - 50:] = math.inf
+        keep = torch.sort(torch.sort(worth, descending=True, stable=True).indices[:304]).values
+        assert torch.equal(e["idx"][0, h].long(), keep) and torch.equal(e["K_out"][0, h], K[0, h, keep])
