@@ -22,17 +22,25 @@ template <int D, bool VALUES>
 __device__ __forceinline__ void tile_fill(const uint32_t lds, const uint16_t* X, const AttendSpan span, const int v, const int wave, const int lane) {
   constexpr int PIECES = D / 8, LOADS = AT_KEYS * PIECES / AT_THREADS, ROWS = AT_THREADS / PIECES;   // rows per load of the workgroup
   // offsets from the first entry: 32 bits without a sign, what the rows of a head span
-  const int start = attend_uniform(attend_key(span, v)), jump = attend_uniform(v < span.split ? span.split - v : AT_KEYS), skip = attend_uniform(span.skip);
+  const int start = attend_uniform(attend_key(span, v)), jump = attend_uniform(v < span.split ? span.split - v : AT_KEYS);
   const int last = attend_uniform(span.count - 1 - v);
+  const void* base = attend_uniform(X + (size_t)start * D);
   uint32_t off[LOADS];
+  int rows[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
     const int at = wave * 64 + lane, row = i * ROWS + at / PIECES, place = at % PIECES;
-    const int piece = VALUES ? place ^ (swap_v<D>(row) << 2) : place ^ (D == 128 ? row & 15 : (row >> 1) & 7);
-    const int r = min(row, last);
-    off[i] = (uint32_t)(r + (r >= jump ? skip : 0)) * (2u * D) + piece * 16;
+    off[i] = (VALUES ? place ^ (swap_v<D>(row) << 2) : place ^ (D == 128 ? row & 15 : (row >> 1) & 7)) * 16;
+    rows[i] = row;
   }
-  load_to_lds(lds + wave * 1024, off, attend_uniform(X + (size_t)start * D));
+  if (jump < AT_KEYS || last < AT_KEYS - 1) {
+    const int skip = attend_uniform(span.skip);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) { const int r = min(rows[i], last); rows[i] = r + (r >= jump ? skip : 0); }
+  }
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) off[i] += (uint32_t)rows[i] * (2u * D);
+  load_to_lds(lds + wave * 1024, off, base);
 }
 
 template <bool CUT> struct TileCut { static constexpr bool value = CUT; };
@@ -183,44 +191,46 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
     }
   };
 
-  // Tile i: 64 entries of the message (front) or of the own span.  cut: some row of the workgroup does not see some of them.
+  // Tile i: 64 entries of the message (the first front_tiles), then of the own span.  Every row of the workgroup sees all of the tiles from 0 to front_whole and
+  // from whole0 to whole1; the others are taken with their masks.
   const AttendSpan front_span = {front, 0, 0};
-  struct At { bool front, cut; int base; };
-  const auto locate = [&](const int i) {
-    At t;
-    t.front = i < front_tiles;
-    t.base = (t.front ? i : i - front_tiles) * AT_KEYS;
-    t.cut = t.front ? t.base + AT_KEYS > front : attend_cut(k, span, sink, pmin, pmax, t.base, AT_KEYS);
-    return t;
-  };
-  const auto fill = [&](const int buf, const At& t) {
+  const int front_whole = front / AT_KEYS;
+  int whole0 = front_tiles, whole1 = front_tiles + span.count / AT_KEYS;
+  if (k.causal) {
+    whole1 = min(whole1, front_tiles + max(0, pmin - span.skip + 1) / AT_KEYS);
+    if (k.window > 0) whole0 += max(0, pmax - k.window - span.skip + AT_KEYS) / AT_KEYS;
+  }
+  const auto fill = [&](const int buf, const int i) {
     const uint16_t *from_k = K, *from_v = V;
     AttendSpan from = span;
-    if (t.front) { from_k = FK; from_v = FV; from = front_span; }
-    tile_fill<D, false>(lds + buf * TILE, from_k, from, t.base, wave, lane);
-    tile_fill<D, true>(lds + (2 + buf) * TILE, from_v, from, t.base, wave, lane);
+    int v = (i - front_tiles) * AT_KEYS;
+    if (i < front_tiles) { from_k = FK; from_v = FV; from = front_span; v = i * AT_KEYS; }
+    tile_fill<D, false>(lds + buf * TILE, from_k, from, v, wave, lane);
+    tile_fill<D, true>(lds + (2 + buf) * TILE, from_v, from, v, wave, lane);
   };
-  At now = {false, false, 0}, next = {false, false, 0};
   int i = first, buf = 0;
   // Tile i is there, nobody reads the other one any more: the loads of tile i + 1.
   const auto begin = [&]() {
     wait_loads<0>();
     __syncthreads();
-    if (i + 1 < behind) { next = locate(i + 1); fill(buf ^ 1, next); }
+    if (i + 1 < behind) fill(buf ^ 1, i + 1);
   };
-  if (first < behind) { now = locate(first); fill(0, now); }
+  if (first < behind) fill(0, first);
   // (two loops, so that the common one has the registers to itself)
   while (i < behind) {
-    for (; i < behind && !now.cut; ++i, buf ^= 1, now = next) {
+    const int whole = min(behind, i < front_whole ? front_whole : i >= whole0 ? whole1 : i);
+    for (; i < whole; ++i, buf ^= 1) {
       begin();
-      take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, k, span, now.base);
+      take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, k, span, 0);
     }
-    for (; i < behind && now.cut; ++i, buf ^= 1, now = next) {
-      begin();
+    const int cut = min(behind, i < front_tiles ? front_tiles : i < whole0 ? whole0 : behind);
+    for (; i < cut; ++i, buf ^= 1) {
       AttendKeys kt = k;
       AttendSpan st = span;
-      if (now.front) { kt.causal = 0; kt.window = 0; st = front_span; }
-      take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, kt, st, now.base);
+      int v = (i - front_tiles) * AT_KEYS;
+      if (i < front_tiles) { kt.causal = 0; kt.window = 0; st = front_span; v = i * AT_KEYS; }
+      begin();
+      take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, kt, st, v);
     }
   }
 
