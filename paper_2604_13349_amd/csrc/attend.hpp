@@ -56,6 +56,14 @@ __device__ __forceinline__ const void* attend_uniform(const void* p) {
   return (const void*)((uint64_t)(uint32_t)attend_uniform((int)(uint32_t)u) | (uint64_t)(uint32_t)attend_uniform((int)(uint32_t)(u >> 32)) << 32);
 }
 
+// The set of keys of a workgroup, and its place `within` the set's workgroups: eight sets at a time go round the eight dies, so that a set's workgroups share a
+// second-level cache; the next eight one die further, since the heads of one number may all be longer than the others.
+__device__ __forceinline__ int attend_set(const int block, const int sets, const int per_set, int& within) {
+  const int round = sets & 7 ? sets & -sets : 8, group = block / (round * per_set);
+  within = block / round % per_set;
+  return group * round + (block + group) % round;
+}
+
 // Rows of a head: a length that lies outside its storage (the -1 of a message that did not fit among them) counts as none.
 __device__ __forceinline__ int attend_len(const AttendKeys& k, const int sample, const int h) {
   const int n = k.len ? k.len[(size_t)sample * k.len_stride + h] : k.len_all;
@@ -120,9 +128,10 @@ obf_status_t launch_attend_few(const AttendArgs& a, int tile_rows, int d, int dt
 obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);
 obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);   // joins the ranges; adds the logits' weights to the mass
 
-// Accumulated weights of the own rows; part: a sum per range of query rows (unless there is one) and row of a dense cache.
-struct AttendMass { float* mass; float* part; int nsplit, tiles; };
-int attend_mass_ranges(const AttendArgs& a, int dtype);
+// Accumulated weights of the own rows.  tiles > 0: by the kernel of many rows, per steps of query rows in each of nsplit ranges, whose sums (unless there is one
+// range) go to part, [range][set][stride].
+struct AttendMass { float* mass; float* part; int nsplit, tiles, per; };
+AttendMass plan_attend_mass(const AttendArgs& a, int dtype);
 obf_status_t launch_attend_mass(const AttendArgs& a, int d, int dtype, const float* lse, const AttendMass& mass, hipStream_t st);
 
 struct EvictArgs {

@@ -59,7 +59,7 @@ static obf_status_t check_aligned(const char* name, const void* p) {
 struct AttendPlan {
   AttendArgs a;
   int tile_rows[2];            // query rows of a workgroup's tile, by set of keys; kAttendTileRows: the kernel of many rows
-  int mass_ranges;
+  AttendMass ms;
   bool keep_logits;
   size_t part_O, part_lse, lse, mass, logits, total;
 };
@@ -115,9 +115,9 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
   p.lse = at;
   at += ((size_t)a.rows * sizeof(float) + 255) & ~(size_t)255;
-  p.mass_ranges = attend_mass_ranges(a, c->dtype);
+  p.ms = plan_attend_mass(a, c->dtype);
   p.mass = at;
-  if (p.mass_ranges > 1) at += ((size_t)p.mass_ranges * a.S * a.H * c->token_stride * sizeof(float) + 255) & ~(size_t)255;
+  if (p.ms.nsplit > 1) at += ((size_t)p.ms.nsplit * a.S * a.H * c->token_stride * sizeof(float) + 255) & ~(size_t)255;
   // Few query rows: the logits are kept and weighted at the end, 4 bytes a row and key written and read beside the 2 d or 4 d of a key, where a second pass
   // would read the keys again.
   const bool keep = a.n_keys == 1 && own_rows <= p.tile_rows[0] && own_rows <= kAttendFewRows;
@@ -170,7 +170,8 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
   if (mass && p.keep_logits) { a.logits = (float*)(base + p.logits); a.mass = mass; }
   OBF_TRY(launch_plan(p, c->head_dim, c->dtype, st));
   if (a.ranges > 1 || a.logits) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
-  return mass && !a.logits ? launch_attend_mass(a, c->head_dim, c->dtype, lse, AttendMass{mass, (float*)(base + p.mass), p.mass_ranges, 0}, st) : OBF_OK;
+  p.ms.mass = mass; p.ms.part = (float*)(base + p.mass);
+  return mass && !a.logits ? launch_attend_mass(a, c->head_dim, c->dtype, lse, p.ms, st) : OBF_OK;
 }
 
 }  // namespace obf
@@ -215,7 +216,8 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   p.a.Q = Q;
   p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;
-  return launch_attend_mass(p.a, call->head_dim, call->dtype, lse, AttendMass{mass, (float*)((char*)ws + p.mass), p.mass_ranges, 0}, (hipStream_t)stream);
+  p.ms.mass = mass; p.ms.part = (float*)((char*)ws + p.mass);
+  return launch_attend_mass(p.a, call->head_dim, call->dtype, lse, p.ms, (hipStream_t)stream);
 }
 
 obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const void* K, const void* V, const float* mass, const int32_t* pos,

@@ -5,6 +5,7 @@
 // arrival.
 #include "attend_few.hpp"
 #include "attend_tile.hpp"
+#include "lds_load.hpp"
 
 namespace obf {
 
@@ -65,154 +66,168 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
     }
 }
 
-// The same for many query rows, bf16: a wave holds the operands of 64 keys, a workgroup of 256; the query rows pass through LDS, 64 at a time, their normalisers
-// with them.  The rows are cut into ranges where the keys alone do not fill the chip; the ranges' sums are added in their order by k_attend_mass_add.
-constexpr int MT_KEYS = 256, MT_ROWS = 64, MT_THREADS = 256;
+// The same for many query rows, bf16: a wave holds the operands of 64 keys (two of 32), a workgroup of 256; the query rows that see any of them pass through LDS,
+// 64 at a time, loaded straight to it while the present ones' weights are taken (operands read from memory row by row cost a cache line per lane and load).
+// The rows are cut into ranges of ms.per steps, so that a head's early keys, which many queries see, take no longer than its late ones; the ranges' sums are
+// added in their order by k_attend_mass_add.
+// Bound by the vector work, a multiply-add, an exponential and an addition per weight, beside which the products of head_dim 128 take two thirds.
+constexpr int MT_WAVES = 4, MT_THREADS = MT_WAVES * 64, MT_KEYS = MT_WAVES * 64, MT_ROWS = 64;
+
+// query rows r0 .. r1 - 1 that see a key of the 256 from base on
+struct MassRows { int r0, r1; };
+__device__ __forceinline__ MassRows mass_rows(const AttendArgs& a, const AttendKeys& k, const int n, const int sink, const int base) {
+  int t0 = 0, t1 = a.T;
+  if (k.causal) {
+    t0 = max(0, base - (n - a.T));
+    if (k.window > 0 && base >= sink) t1 = (int)min((long)a.T, (long)base + MT_KEYS - 1 + k.window - (n - a.T));
+  }
+  return {t0 * a.g, max(t0, t1) * a.g};
+}
 
 template <int D>
 __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const AttendArgs a, const AttendMass ms, const float* __restrict__ lse) {
-  constexpr int KK = D / 16, PIECES = D / 8, LOADS = MT_ROWS * PIECES / MT_THREADS;
-  __shared__ __attribute__((aligned(16))) char sm_q[2][MT_ROWS * 2 * D];
-  __shared__ float sm_ref[2][MT_ROWS];
-  __shared__ AttendView sm_view[2][MT_ROWS];
+  constexpr int KK = D / 16, PIECES = D / 8, LOADS = MT_ROWS * PIECES / MT_THREADS, BYTES = MT_ROWS * D * 2;
+  __shared__ __attribute__((aligned(1024))) char sm[2 * BYTES];
   const AttendKeys& k = a.keys[0];
   const int lane = threadIdx.x & 63, wave = attend_uniform(threadIdx.x >> 6), half = lane >> 5;
-  const int split = blockIdx.x % ms.nsplit, tile = blockIdx.x / ms.nsplit % ms.tiles, set = blockIdx.x / ms.nsplit / ms.tiles, h = set % a.H, s = set / a.H;
+  // the sets go round the dies; where they do not fill the round the ranges, of which a late tile has fewer, are shifted from tile to tile
+  int within;
+  const int set = attend_set(blockIdx.x, a.S * a.H, ms.tiles * ms.nsplit, within);
+  const int tile = within / ms.nsplit, split = (within + tile) % ms.nsplit, h = set % a.H, s = set / a.H;
   const int n = attend_uniform(attend_len(k, s, h)), sink = attend_uniform(attend_sink(k, s, h));
   const int base0 = tile * MT_KEYS, base = base0 + wave * 64, p0 = n - a.T;
   if (base0 >= n) return;
-  // the queries that see a key of the workgroup
-  int t0 = 0, t1 = a.T;
-  if (k.causal) {
-    t0 = max(0, base0 - p0);
-    if (k.window > 0 && base0 >= sink) t1 = max(t0, (int)min((long)a.T, (long)base0 + MT_KEYS - 1 + k.window - p0));
-  }
-  const int steps = (int)(((long)max(0, t1 - t0) * a.g + MT_ROWS - 1) / MT_ROWS), per = (steps + ms.nsplit - 1) / ms.nsplit;
-  const int first = t0 * a.g + split * per * MT_ROWS, behind = (int)min((long)t1 * a.g, (long)first + (long)per * MT_ROWS);
+  const MassRows rows = mass_rows(a, k, n, sink, base0);
+  const int first = rows.r0 + split * ms.per * MT_ROWS, behind = (int)min((long)rows.r1, (long)first + (long)ms.per * MT_ROWS);
+  if (first >= behind) return;
   const size_t row_base = (size_t)s * k.sample_rows + (size_t)h * k.stride;
   const AttendSpan all = {n, 0, 0};
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)sm;
+  const uint16_t* Q = (const uint16_t*)a.Q + (size_t)s * a.qs + (size_t)h * a.g * a.qh;
+  const float* head_lse = lse + ((size_t)s * a.H + h) * a.g * a.T;
+  // 64 rows from r0 on to LDS (those behind the range repeat its last one), and of the lane's two its normaliser and query
+  struct Rows { float lse[2]; int t[2]; };
+  const auto fill = [&](Rows& x, const int buf, const int r0) {
+    const AttendStep at = attend_step(a, r0);
+    const int most = behind - 1 - r0;
+    const void* from[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = i * (MT_THREADS / PIECES) + (int)threadIdx.x / PIECES, place = threadIdx.x % PIECES;
+      const AttendRow w = attend_row(a, at, s, min(row, most));
+      from[i] = Q + (size_t)w.gi * a.qh + (size_t)w.t * a.qt + 8 * (place ^ (D == 128 ? row & 15 : (row >> 1) & 7));
+    }
+    load_to_lds(lds + buf * BYTES + wave * 1024, from);
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+      const AttendRow w = attend_row(a, at, s, min(32 * qb + (lane & 31), most));
+      x.lse[qb] = head_lse[(size_t)w.gi * a.T + w.t];
+      x.t[qb] = w.t;
+    }
+  };
+  Rows now, next = {};
+  fill(next, 0, first);
   TileFrag kf[2][KK];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
       kf[b][kk].u = *(const TilePiece*)((const uint16_t*)k.K + (row_base + min(base + 32 * b + (lane & 31), n - 1)) * D + 16 * kk + 8 * half);
-  float sum[2][16];
+  float sum[32];
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sum[b][e] = 0.f;
+  for (int e = 0; e < 32; ++e) sum[e] = 0.f;
 
-  // 64 rows from r0 on, to registers and from there to LDS; a thread fetches LOADS pieces, and the first 64 threads a row's normaliser and view
-  TilePiece next[LOADS];
-  float next_ref = 0.f;
-  AttendView next_view = {-1, -1, 0};
-  const uint16_t* Q = (const uint16_t*)a.Q + (size_t)s * a.qs + (size_t)h * a.g * a.qh + 8 * (threadIdx.x % PIECES);
-  const auto fetch = [&](const int r0) {
-    const AttendStep at = attend_step(a, r0);
-    const int most = behind - 1 - r0;
+  for (int r0 = first, buf = 0; r0 < behind; r0 += MT_ROWS, buf ^= 1) {
+    now = next;
+    wait_loads<0>();
+    __syncthreads();                                   // the rows are there, and nobody reads the other ones any more
+    if (r0 + MT_ROWS < behind) fill(next, buf ^ 1, r0 + MT_ROWS);
+    const int qmin = p0 + r0 / a.g, qmax = p0 + (min(r0 + MT_ROWS, behind) - 1) / a.g;
+    // none of the rows sees a key of the wave
+    if (base >= n || (k.causal && (base > qmax || (k.window > 0 && base + 63 <= qmin - k.window && base >= sink)))) continue;
+    const bool cut = r0 + MT_ROWS > behind || attend_cut(k, all, sink, qmin, qmax, base, 64);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const AttendRow w = attend_row(a, at, s, min((int)(i * (MT_THREADS / PIECES) + threadIdx.x / PIECES), most));
-      next[i] = *(const TilePiece*)(Q + (size_t)w.gi * a.qh + (size_t)w.t * a.qt);
-    }
-    const int i = (int)(threadIdx.x % MT_ROWS);
-    const AttendRow w = attend_row(a, at, s, min(i, most));
-    const float v = lse[attend_row_number(a, h, w)];
-    next_view = attend_view(k, all, sink, p0 + w.t);
-    // (a row that sees nothing has weights of 0, and so has one behind the range)
-    const bool counts = i <= most && !(v == -INFINITY);
-    next_ref = counts ? v * 1.44269504088896341f : INFINITY;
-    if (!counts) next_view.hi = -1;
-  };
-  const auto put = [&](const int buf) {
+    for (int qb = 0; qb < 2; ++qb) {
+      TileFrag q[KK];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i)
-      *(TilePiece*)(sm_q[buf] + place_k<D>(i * (MT_THREADS / PIECES) + threadIdx.x / PIECES, threadIdx.x % PIECES)) = next[i];
-    if (threadIdx.x < MT_ROWS) { sm_ref[buf][threadIdx.x] = next_ref; sm_view[buf][threadIdx.x] = next_view; }
-  };
-  if (first < behind) { fetch(first); put(0); }
-  __syncthreads();
-  int buf = 0;
-  for (int r0 = first; r0 < behind; r0 += MT_ROWS, buf ^= 1) {
-    const bool more = r0 + MT_ROWS < behind;
-    if (more) fetch(r0 + MT_ROWS);
-    // some row of the step does not see some key of the wave; none sees any
-    const int wmin = p0 + r0 / a.g, wmax = p0 + (min(r0 + MT_ROWS, behind) - 1) / a.g;
-    const bool cut = r0 + MT_ROWS > behind || attend_cut(k, all, sink, wmin, wmax, base, 64);
-    const bool none = base >= n || (k.causal && (base > wmax || (k.window > 0 && base + 63 <= wmin - k.window && base >= sink)));
-    if (!none) {
+      for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const TilePiece*)(sm + buf * BYTES + place_k<D>(32 * qb + (lane & 31), 2 * kk + half));
+      // (a row that sees nothing has weights of 0, and so has one behind the range)
+      const bool counts = r0 + 32 * qb + (lane & 31) < behind && !(now.lse[qb] == -INFINITY);
+      const float ref = counts ? now.lse[qb] * 1.44269504088896341f : INFINITY;
+      AttendView view = attend_view(k, all, sink, p0 + now.t[qb], base + 4 * half);
+      if (!counts) view.hi = -1;
 #pragma unroll
-      for (int qb = 0; qb < 2; ++qb) {
-        const int row = 32 * qb + (lane & 31);
-        TileFrag q[KK];
+      for (int b = 0; b < 2; ++b) {
+        f32x16 x;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const TilePiece*)(sm_q[buf] + place_k<D>(row, 2 * kk + half));
-        const float ref = sm_ref[buf][row];
-        const AttendView view = attend_from(sm_view[buf][row], base + 4 * half);
+        for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          f32x16 x;
+        for (int kk = 0; kk < KK; ++kk) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kk].v, q[kk].v, x, 0, 0, 0);
+        if (cut) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[e] = 0.f;
-#pragma unroll
-          for (int kk = 0; kk < KK; ++kk) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kk].v, q[kk].v, x, 0, 0, 0);
-          if (cut) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float v = attend_exp2(fmaf(x[e], a.scale2, -ref));
-              sum[b][e] += attend_sees(view, 32 * b + 8 * (e >> 2) + (e & 3)) ? v : 0.f;
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sum[b][e] += attend_exp2(fmaf(x[e], a.scale2, -ref));
+          for (int e = 0; e < 16; ++e) {
+            const float v = attend_exp2(fmaf(x[e], a.scale2, -ref));
+            sum[16 * b + e] += attend_sees(view, 32 * b + 8 * (e >> 2) + (e & 3)) ? v : 0.f;
           }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[16 * b + e] += attend_exp2(fmaf(x[e], a.scale2, -ref));
         }
       }
     }
-    if (more) put(buf ^ 1);
-    __syncthreads();
   }
+  // Sums over the 32 lanes of a half, half of the values passed on at each step: lane i ends with value i.
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int off = 16; off > 0; off >>= 1) {
+    const bool upper = lane & off;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float v = sum[b][e];
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) v += __shfl_xor(v, off);
-      const int j = base + 32 * b + 8 * (e >> 2) + 4 * half + (e & 3);
-      if ((lane & 31) == 0 && j < n) {
-        if (ms.nsplit > 1) ms.part[((size_t)split * a.S * a.H + set) * k.stride + j] = v;
-        else ms.mass[row_base + j] += v;
-      }
+    for (int e = 0; e < off; ++e) {
+      const float mine = upper ? sum[e + off] : sum[e], other = upper ? sum[e] : sum[e + off];
+      sum[e] = mine + __shfl_xor(other, off);
     }
+  }
+  const int e = lane & 31, j = base + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3);
+  if (j < n) {
+    if (ms.nsplit > 1) ms.part[((size_t)split * a.S * a.H + set) * k.stride + j] = sum[0];
+    else ms.mass[row_base + j] += sum[0];
+  }
 }
 
 __global__ __launch_bounds__(256) void k_attend_mass_add(const AttendArgs a, const AttendMass ms) {
   const AttendKeys& k = a.keys[0];
-  const int set = blockIdx.y, h = set % a.H, s = set / a.H, j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= attend_len(k, s, h)) return;
+  const int set = blockIdx.y, h = set % a.H, s = set / a.H, j = blockIdx.x * 256 + threadIdx.x, n = attend_len(k, s, h);
+  if (j >= n) return;
+  const MassRows rows = mass_rows(a, k, n, attend_sink(k, s, h), j & -MT_KEYS);
+  const int ranges = ((rows.r1 - rows.r0 + MT_ROWS - 1) / MT_ROWS + ms.per - 1) / ms.per;      // (the others have not written)
   float v = 0.f;
-  for (int i = 0; i < ms.nsplit; ++i) v += ms.part[((size_t)i * a.S * a.H + set) * k.stride + j];
-  ms.mass[(size_t)s * k.sample_rows + (size_t)h * k.stride + j] += v;
+#pragma unroll 4
+  for (int i = 0; i < ranges; ++i) v += ms.part[((size_t)i * a.S * a.H + set) * k.stride + j];
+  if (ranges > 0) ms.mass[(size_t)s * k.sample_rows + (size_t)h * k.stride + j] += v;
 }
 
-// Ranges of query rows of the kernel of many rows: four workgroups per compute unit and more, not less than 256 rows each.
-int attend_mass_ranges(const AttendArgs& a, int dtype) {
+// Steps of a range: three rounds of workgroups, two per compute unit, where half of a causal call's steps are not taken; not less than 8, beside which the
+// operands of the keys and the sums at the end cost little.  (2 x 8 heads, 2048 queries of 5 heads, us of the whole call: one round 263, two 245, three 240,
+// four with 4 steps at least 243.)
+AttendMass plan_attend_mass(const AttendArgs& a, int dtype) {
   const AttendKeys& k = a.keys[a.n_keys - 1];
-  const long rows = (long)a.T * a.g, blocks = (long)((k.stride + MT_KEYS - 1) / MT_KEYS) * a.S * a.H;
-  if (dtype != OBF_BF16 || rows <= kAttendFewRows) return 1;
-  const long want = (4 * kNumCU + blocks - 1) / blocks, most = (rows + 255) / 256;
-  return (int)(want < most ? want : most);
+  AttendMass ms = {nullptr, nullptr, 1, 0, 0};
+  const long rows = (long)a.T * a.g;
+  if (dtype != OBF_BF16 || rows <= kAttendFewRows) return ms;
+  ms.tiles = (k.stride + MT_KEYS - 1) / MT_KEYS;
+  const long steps = (rows + MT_ROWS - 1) / MT_ROWS, groups = (long)ms.tiles * a.S * a.H;
+  long per = groups * steps / (k.causal ? 2 : 1) / (3 * 2 * kNumCU);
+  per = per < 8 ? 8 : per;
+  per = per > steps ? steps : per;
+  ms.per = (int)per;
+  ms.nsplit = (int)((steps + per - 1) / per);
+  return ms;
 }
 
-obf_status_t launch_attend_mass(const AttendArgs& args, int d, int dtype, const float* lse, const AttendMass& mass, hipStream_t st) {
+obf_status_t launch_attend_mass(const AttendArgs& args, int d, int dtype, const float* lse, const AttendMass& ms, hipStream_t st) {
   ProfScope prof(ST_ATTEND_MASS, st);
   AttendArgs a = args;
   AttendKeys& k = a.keys[0];
-  AttendMass ms = mass;
-  if (dtype == OBF_BF16 && (long)a.T * a.g > kAttendFewRows) {
-    ms.tiles = (k.stride + MT_KEYS - 1) / MT_KEYS;
+  if (ms.tiles > 0) {
     const dim3 grid((unsigned)((long)ms.tiles * a.S * a.H * ms.nsplit));
     if (d == 128) hipLaunchKernelGGL(k_attend_mass_tile<128>, grid, dim3(MT_THREADS), 0, st, a, ms, lse);
     else hipLaunchKernelGGL(k_attend_mass_tile<64>, grid, dim3(MT_THREADS), 0, st, a, ms, lse);

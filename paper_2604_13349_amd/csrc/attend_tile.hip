@@ -57,9 +57,8 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   const bool second = a.fused || block >= a.keys[0].blocks;
   AttendKeys k = a.keys[0];
   if (second) { k = a.keys[1]; if (!a.fused) block -= a.keys[0].blocks; }
-  const int sets = k.samples * a.H, round = sets & 7 ? sets & -sets : 8, per_set = k.row_tiles * k.nsplit;
-  const int set = block % round + round * (block / (round * per_set));
-  const int within = block / round % per_set;
+  int within;
+  const int set = attend_set(block, k.samples * a.H, k.row_tiles * k.nsplit, within);
   const int split = within % k.nsplit, row_tile = k.row_tiles - 1 - within / k.nsplit;
   const int h = set % a.H, ks = set / a.H;
   const int set_rows = k.row_samples * a.T * a.g;

@@ -22,6 +22,21 @@ __device__ __forceinline__ void load_to_lds(const uint32_t lds, const uint32_t (
                "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4\n\ts_mov_b32 m0, %0"
                : "=&s"(m0) : "s"(lds), "v"(off[0]), "v"(off[1]), "s"(base) : "memory", "scc");
 }
+// The same from an address per lane and load.
+__device__ __forceinline__ void load_to_lds(const uint32_t lds, const void* const (&from)[4]) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\t"
+               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off\n\t"
+               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, off\n\t"
+               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(lds), "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]) : "memory", "scc");
+}
+__device__ __forceinline__ void load_to_lds(const uint32_t lds, const void* const (&from)[2]) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\t"
+               "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(lds), "v"(from[0]), "v"(from[1]) : "memory", "scc");
+}
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
