@@ -7,6 +7,8 @@
 
 namespace obf {
 
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t EvictRow;     // 16 bytes of a row
+
 constexpr int EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048;
 
 // larger float <=> larger key
@@ -98,35 +100,44 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) 
 
 constexpr int EG_THREADS = 256, EG_UNROLL = 4;
 
-__global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictArgs a) {
-  const int head = blockIdx.y, per = EG_THREADS / a.row_vec, c = threadIdx.x % a.row_vec;
-  const int r0 = blockIdx.x * per * EG_UNROLL + threadIdx.x / a.row_vec;
-  const int n = a.len_out[head];
-  const uint4* K = (const uint4*)a.K;
-  const uint4* V = (const uint4*)a.V;
-  int j[EG_UNROLL];
-  uint4 kv[EG_UNROLL], vv[EG_UNROLL];
+__global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictRow* __restrict__ K, const EvictRow* __restrict__ V, const float* __restrict__ mass,
+                                                           const int32_t* __restrict__ pos, const int32_t* __restrict__ idx, const int32_t* __restrict__ len,
+                                                           EvictRow* __restrict__ K_out, EvictRow* __restrict__ V_out, float* __restrict__ mass_out,
+                                                           int32_t* __restrict__ pos_out, const int row_vec, const int in_stride, const int out_stride) {
+  const int head = blockIdx.y, per = EG_THREADS / row_vec, c = threadIdx.x % row_vec;
+  const int r0 = blockIdx.x * per * EG_UNROLL + threadIdx.x / row_vec;
+  const int n = len[head];
+  if (blockIdx.x * per * EG_UNROLL >= n) return;
+  // (rows behind the end load the last one's again: no condition holds up a load)
+  size_t from[EG_UNROLL];
+  EvictRow kv[EG_UNROLL], vv[EG_UNROLL];
 #pragma unroll
-  for (int u = 0; u < EG_UNROLL; ++u) { const int r = r0 + u * per; j[u] = r < n ? a.idx[(size_t)head * a.out_stride + r] : -1; }
+  for (int u = 0; u < EG_UNROLL; ++u) from[u] = (size_t)head * in_stride + idx[(size_t)head * out_stride + min(r0 + u * per, n - 1)];
+#pragma unroll
+  for (int u = 0; u < EG_UNROLL; ++u) { kv[u] = K[from[u] * row_vec + c]; vv[u] = V[from[u] * row_vec + c]; }
 #pragma unroll
   for (int u = 0; u < EG_UNROLL; ++u)
-    if (j[u] >= 0) { const size_t s = ((size_t)head * a.in_stride + j[u]) * a.row_vec + c; kv[u] = K[s]; vv[u] = V[s]; }
-#pragma unroll
-  for (int u = 0; u < EG_UNROLL; ++u)
-    if (j[u] >= 0) {
-      const size_t row = (size_t)head * a.out_stride + r0 + u * per, from = (size_t)head * a.in_stride + j[u];
-      ((uint4*)a.K_out)[row * a.row_vec + c] = kv[u];
-      ((uint4*)a.V_out)[row * a.row_vec + c] = vv[u];
-      if (c == 0) a.mass_out[row] = a.mass[from];
-      if (c == 1 && a.pos) a.pos_out[row] = a.pos[from];
+    if (r0 + u * per < n) {
+      const size_t row = (size_t)head * out_stride + r0 + u * per;
+      K_out[row * row_vec + c] = kv[u];
+      V_out[row * row_vec + c] = vv[u];
     }
+  // a lane per row for what goes with it
+  const int r = blockIdx.x * per * EG_UNROLL + threadIdx.x;
+  if ((int)threadIdx.x < per * EG_UNROLL && r < n) {
+    const size_t row = (size_t)head * out_stride + r, at = (size_t)head * in_stride + idx[row];
+    mass_out[row] = mass[at];
+    if (pos) pos_out[row] = pos[at];
+  }
 }
 
 obf_status_t launch_evict(const EvictArgs& a, hipStream_t st) {
   ProfScope prof(ST_EVICT, st);
   hipLaunchKernelGGL(k_evict_select, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
   const int per = EG_THREADS / a.row_vec * EG_UNROLL;
-  hipLaunchKernelGGL(k_evict_rows, dim3((a.out_stride + per - 1) / per, a.heads), dim3(EG_THREADS), 0, st, a);
+  hipLaunchKernelGGL(k_evict_rows, dim3((a.out_stride + per - 1) / per, a.heads), dim3(EG_THREADS), 0, st,
+                     (const EvictRow*)a.K, (const EvictRow*)a.V, a.mass, a.pos, a.idx, a.len_out, (EvictRow*)a.K_out, (EvictRow*)a.V_out, a.mass_out, a.pos_out,
+                     a.row_vec, a.in_stride, a.out_stride);
   return check_launch("evict");
 }
 
