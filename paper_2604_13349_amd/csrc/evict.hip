@@ -105,9 +105,9 @@ __global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictRow* __res
                                                            EvictRow* __restrict__ K_out, EvictRow* __restrict__ V_out, float* __restrict__ mass_out,
                                                            int32_t* __restrict__ pos_out, const int row_vec, const int in_stride, const int out_stride) {
   const int head = blockIdx.y, per = EG_THREADS / row_vec, c = threadIdx.x % row_vec;
-  const int r0 = blockIdx.x * per * EG_UNROLL + threadIdx.x / row_vec;
-  const int n = len[head];
-  if (blockIdx.x * per * EG_UNROLL >= n) return;
+  const int block0 = (int)blockIdx.x * per * EG_UNROLL, r0 = block0 + (int)threadIdx.x / row_vec;
+  const int n = len[head];                                          // -1 for a head that was flagged
+  if (block0 >= n) return;
   // (rows behind the end load the last one's again: no condition holds up a load)
   size_t from[EG_UNROLL];
   EvictRow kv[EG_UNROLL], vv[EG_UNROLL];
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictRow* __res
       V_out[row * row_vec + c] = vv[u];
     }
   // a lane per row for what goes with it
-  const int r = blockIdx.x * per * EG_UNROLL + threadIdx.x;
+  const int r = block0 + (int)threadIdx.x;
   if ((int)threadIdx.x < per * EG_UNROLL && r < n) {
     const size_t row = (size_t)head * out_stride + r, at = (size_t)head * in_stride + idx[row];
     mass_out[row] = mass[at];

@@ -237,6 +237,10 @@ EVICT = [
     (BF, 128, 2, 400, (300, 400), 1, 0, 0, 2, True),
     (BF, 64, 2, 400, (300, 400), 0, 0, 3, 3, False),
     (BF, 64, 2, 33000, (32900, 33000), 5000, 11, 1, 5001, True),
+    (BF, 64, 3, 32768, (1, 32768), 3277, 100, 4, 3300, False),
+    (BF, 64, 3, 20000, (15000, 20000), 7000, 100, 4, 7004, True),
+    (BF, 64, 2, 1024, (1000, 1024), 512, 0, 0, 512, True),
+    (F32, 64, 2, 1025, (1025, 1025), 1000, 999, 24, 1024, False),
 ]
 
 
