@@ -1,8 +1,9 @@
 // Eviction by accumulated attention weight: per head the first rows, the newest rows and the rows of the largest mass are kept, in their order.
 //
-// First launch, a workgroup per head: the mass of the last row that is kept, by histograms of an order-preserving integer image of the masses
-// (2048 bins over the range that can still hold it), then the list of kept rows by a prefix count.  All decisions are integer compares: exact, ties to
-// the lowest index.  Second launch: the kept rows of K and V in 16-byte pieces, their masses and positions.
+// First launch, a workgroup per head: the mass of the last row that is kept, by a histogram of an order-preserving integer image of the masses
+// (2048 bins over the range that can still hold it) and again inside its bin until it is one key wide or its keys fit a list, whose entries then count the
+// larger ones among themselves; then the list of kept rows by prefix counts.  All decisions are integer compares: exact, ties to the lowest index.  Heads of
+// up to 32768 rows keep their keys in registers.  Second launch: the kept rows of K and V in 16-byte pieces, their masses and positions.
 #include "attend.hpp"
 
 namespace obf {
@@ -17,11 +18,16 @@ __device__ __forceinline__ uint32_t mass_key(const float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+constexpr int EV_LIST = 256;
+
+// PER keys per thread in registers, thread t those of rows t, t + 1024, ...; 0: read again for every pass.
+template <int PER>
 __global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) {
+  constexpr int REGS = PER > 0 ? PER : 1;
   __shared__ int hist[EV_BINS];
-  __shared__ uint32_t wlo[EV_WAVES], whi[EV_WAVES];
-  __shared__ int wgt[EV_WAVES], weq[EV_WAVES];
-  __shared__ int s_bin, s_above;
+  __shared__ uint32_t wlo[EV_WAVES], whi[EV_WAVES], list[EV_LIST], s_key;
+  __shared__ int wsum[EV_WAVES], s_bin, s_above, s_inside, s_listed;
+  __shared__ int before_gt[REGS * EV_WAVES], before_eq[REGS * EV_WAVES], s_gt[EV_WAVES], s_eq[EV_WAVES];
   const int head = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t* out = a.idx + (size_t)head * a.out_stride;
   const int n = a.len ? a.len[head] : a.len_all;
@@ -43,58 +49,121 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) 
   for (int i = tid; i < a.recent; i += EV_THREADS) out[first + want + i] = last + i;
   if (want == 0) return;
   const float* mass = a.mass + (size_t)head * a.in_stride;
+  uint32_t key[REGS];
+  if (PER > 0) {
+#pragma unroll
+    for (int c = 0; c < REGS; ++c) { const int i = first + c * EV_THREADS + tid; key[c] = i < last ? mass_key(mass[i]) : 0u; }
+  }
+  // f(key, place) for the rows of this thread
+  const auto each = [&](const auto f) {
+    if (PER > 0) {
+#pragma unroll
+      for (int c = 0; c < REGS; ++c) if (first + c * EV_THREADS + tid < last) f(key[c]);
+    } else {
+      for (int i = first + tid; i < last; i += EV_THREADS) f(mass_key(mass[i]));
+    }
+  };
   uint32_t lo = 0xffffffffu, hi = 0u;
-  for (int i = first + tid; i < last; i += EV_THREADS) { const uint32_t k = mass_key(mass[i]); lo = min(lo, k); hi = max(hi, k); }
+  each([&](const uint32_t k) { lo = min(lo, k); hi = max(hi, k); });
   for (int off = 32; off > 0; off >>= 1) { lo = min(lo, (uint32_t)__shfl_xor((int)lo, off)); hi = max(hi, (uint32_t)__shfl_xor((int)hi, off)); }
   if (lane == 0) { wlo[wave] = lo; whi[wave] = hi; }
+  if (tid == 0) s_listed = 0;
+  hist[tid] = 0; hist[tid + EV_THREADS] = 0;
   __syncthreads();
   lo = 0xffffffffu; hi = 0u;
+#pragma unroll
   for (int w = 0; w < EV_WAVES; ++w) { lo = min(lo, wlo[w]); hi = max(hi, whi[w]); }
   int need = want;                                                  // rank wanted among the keys of [lo, hi]
-  while (lo < hi) {                                                 // uniform
+  while (lo < hi) {                                                 // uniform; the histogram is clear
     const int shift = max(0, 32 - __clz((int)(hi - lo)) - 11);      // (hi - lo) >> shift < EV_BINS
-    for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
-    __syncthreads();
-    for (int i = first + tid; i < last; i += EV_THREADS) {
-      const uint32_t o = mass_key(mass[i]) - lo;                    // keys below the range wrap to above it
+    each([&](const uint32_t k) {
+      const uint32_t o = k - lo;                                    // keys below the range wrap to above it
       if (o <= hi - lo) atomicAdd(&hist[o >> shift], 1);
-    }
+    });
     __syncthreads();
     // from the top: this thread's bins are top and top - 1
     const int top = EV_BINS - 1 - 2 * tid;
     const int c0 = hist[top], c1 = hist[top - 1];
     int inc = c0 + c1;
     for (int off = 1; off < 64; off <<= 1) { const int x = __shfl_up(inc, off); if (lane >= off) inc += x; }
-    if (lane == 63) wgt[wave] = inc;
+    if (lane == 63) wsum[wave] = inc;
     __syncthreads();
     int before = inc - c0 - c1;
-    for (int w = 0; w < wave; ++w) before += wgt[w];
-    if (before < need && need <= before + c0) { s_bin = top; s_above = before; }
-    else if (before + c0 < need && need <= before + c0 + c1) { s_bin = top - 1; s_above = before + c0; }
+#pragma unroll
+    for (int w = 0; w < EV_WAVES; ++w) before += w < wave ? wsum[w] : 0;
+    if (before < need && need <= before + c0) { s_bin = top; s_above = before; s_inside = c0; }
+    else if (before + c0 < need && need <= before + c0 + c1) { s_bin = top - 1; s_above = before + c0; s_inside = c1; }
+    hist[top] = 0; hist[top - 1] = 0;
     __syncthreads();
     need -= s_above;
     const uint64_t bin_top = (uint64_t)lo + (((uint64_t)s_bin + 1u) << shift) - 1u;
     if (bin_top < (uint64_t)hi) hi = (uint32_t)bin_top;
     lo += (uint32_t)s_bin << shift;
-    __syncthreads();                                                // s_bin, hist and wgt are written again
+    if (lo < hi && s_inside <= EV_LIST) {
+      each([&](const uint32_t k) { if (k - lo <= hi - lo) list[atomicAdd(&s_listed, 1)] = k; });
+      __syncthreads();
+      if (tid < s_inside) {
+        const uint32_t k = list[tid];
+        int gt = 0, ge = 0;
+        for (int j = 0; j < s_inside; ++j) { gt += list[j] > k; ge += list[j] >= k; }
+        if (gt < need && need <= ge) { s_key = k; s_above = gt; }   // the same from every copy of the key
+      }
+      __syncthreads();
+      lo = hi = s_key;
+      need -= s_above;
+      break;
+    }
+    __syncthreads();                                                // s_bin and wsum are written again
   }
   // keys above lo are kept; of those equal to it the first `need`
-  int at = first, equal = 0;                                        // rows kept, and rows equal to lo, before this chunk
-  for (int c = first; c < last; c += EV_THREADS) {
-    const int i = c + tid;
-    const uint32_t k = i < last ? mass_key(mass[i]) : 0u;
-    const bool gt = i < last && k > lo, eq = i < last && k == lo;
-    const uint64_t bg = __ballot(gt), be = __ballot(eq), under = (1ull << lane) - 1ull;
-    if (lane == 0) { wgt[wave] = __popcll(bg); weq[wave] = __popcll(be); }
+  const uint64_t under = (1ull << lane) - 1ull;
+  if (PER > 0) {
+#pragma unroll
+    for (int c = 0; c < REGS; ++c) {
+      const bool valid = first + c * EV_THREADS + tid < last;
+      const uint64_t gt = __ballot(valid && key[c] > lo), eq = __ballot(valid && key[c] == lo);
+      if (lane == 0) { before_gt[c * EV_WAVES + wave] = __popcll(gt); before_eq[c * EV_WAVES + wave] = __popcll(eq); }
+    }
     __syncthreads();
-    int g = __popcll(bg & under), e = equal + __popcll(be & under), tg = 0, te = 0;
-    for (int w = 0; w < EV_WAVES; ++w) { if (w < wave) { g += wgt[w]; e += weq[w]; } tg += wgt[w]; te += weq[w]; }
-    // kept rows before this one: the larger ones, and of the equal ones as many as were still needed
-    const int eq_before = min(e, need) - min(equal, need);
-    if (gt || (eq && e < need)) out[at + g + eq_before] = i;
-    at += tg + min(equal + te, need) - min(equal, need);
-    equal += te;
+    // exclusive sums over (chunk, wave), the rows' order
+    const int mine_gt = tid < REGS * EV_WAVES ? before_gt[tid] : 0, mine_eq = tid < REGS * EV_WAVES ? before_eq[tid] : 0;
+    int g = mine_gt, e = mine_eq;
+    for (int off = 1; off < 64; off <<= 1) { const int x = __shfl_up(g, off), y = __shfl_up(e, off); if (lane >= off) { g += x; e += y; } }
+    if (lane == 63) { s_gt[wave] = g; s_eq[wave] = e; }
     __syncthreads();
+    if (tid < REGS * EV_WAVES) {
+      g -= mine_gt; e -= mine_eq;
+      for (int w = 0; w < wave; ++w) { g += s_gt[w]; e += s_eq[w]; }
+      before_gt[tid] = g; before_eq[tid] = e;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < REGS; ++c) {
+      const int i = first + c * EV_THREADS + tid;
+      const bool gt = i < last && key[c] > lo, eq = i < last && key[c] == lo;
+      const uint64_t bg = __ballot(gt), be = __ballot(eq);
+      const int eq_before = before_eq[c * EV_WAVES + wave] + __popcll(be & under);
+      if (gt || (eq && eq_before < need)) out[first + before_gt[c * EV_WAVES + wave] + __popcll(bg & under) + min(eq_before, need)] = i;
+    }
+  } else {
+    int at = first, equal = 0;                                      // rows kept, and rows equal to lo, before this chunk
+    for (int c = first; c < last; c += EV_THREADS) {
+      const int i = c + tid;
+      const uint32_t k = i < last ? mass_key(mass[i]) : 0u;
+      const bool gt = i < last && k > lo, eq = i < last && k == lo;
+      const uint64_t bg = __ballot(gt), be = __ballot(eq);
+      if (lane == 0) { s_gt[wave] = __popcll(bg); s_eq[wave] = __popcll(be); }
+      __syncthreads();
+      int g = __popcll(bg & under), e = equal + __popcll(be & under), tg = 0, te = 0;
+#pragma unroll
+      for (int w = 0; w < EV_WAVES; ++w) { if (w < wave) { g += s_gt[w]; e += s_eq[w]; } tg += s_gt[w]; te += s_eq[w]; }
+      // kept rows before this one: the larger ones, and of the equal ones as many as were still needed
+      const int eq_before = min(e, need) - min(equal, need);
+      if (gt || (eq && e < need)) out[at + g + eq_before] = i;
+      at += tg + min(equal + te, need) - min(equal, need);
+      equal += te;
+      __syncthreads();
+    }
   }
 }
 
@@ -133,7 +202,10 @@ __global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictRow* __res
 
 obf_status_t launch_evict(const EvictArgs& a, hipStream_t st) {
   ProfScope prof(ST_EVICT, st);
-  hipLaunchKernelGGL(k_evict_select, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
+  if (a.in_stride <= EV_THREADS) hipLaunchKernelGGL(k_evict_select<1>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
+  else if (a.in_stride <= 8 * EV_THREADS) hipLaunchKernelGGL(k_evict_select<8>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
+  else if (a.in_stride <= 32 * EV_THREADS) hipLaunchKernelGGL(k_evict_select<32>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
+  else hipLaunchKernelGGL(k_evict_select<0>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
   const int per = EG_THREADS / a.row_vec * EG_UNROLL;
   hipLaunchKernelGGL(k_evict_rows, dim3((a.out_stride + per - 1) / per, a.heads), dim3(EG_THREADS), 0, st,
                      (const EvictRow*)a.K, (const EvictRow*)a.V, a.mass, a.pos, a.idx, a.len_out, (EvictRow*)a.K_out, (EvictRow*)a.V_out, a.mass_out, a.pos_out,
