@@ -126,6 +126,7 @@ constexpr int kAttendFewRows = 32;    // query rows per set of keys up to which 
 constexpr int kAttendTileRows = 128;
 obf_status_t launch_attend_few(const AttendArgs& a, int tile_rows, int d, int dtype, hipStream_t st);
 obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);
+obf_status_t launch_attend_tile_few(const AttendArgs& a, int d, hipStream_t st);          // keys[0] by tiles of many rows, keys[1] by tiles of 16
 obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);   // joins the ranges; adds the logits' weights to the mass
 
 // Accumulated weights of the own rows.  tiles > 0: by the kernel of many rows, per steps of query rows in each of nsplit ranges, whose sums (unless there is one

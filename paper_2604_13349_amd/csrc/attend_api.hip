@@ -93,16 +93,20 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   const long own_rows = (long)a.T * a.g;
   // A sample's queries fill tiles of many rows by themselves: one pass over the message and the own rows, no partial results of the message.
   a.fused = a.n_keys > 1 && c->dtype == OBF_BF16 && own_rows > kAttendFewRows;
+  // Up to 32 rows the waves read the keys straight into registers for 16 rows at a time; for 17 to 32 rows at once where there are keys enough to fill the chip
+  // (us, 16 and 32 rows: 4 x 8 heads of 1000 rows 13.7 - 18.7, 32 x 8 of 1000 41.8 - 41.9, 16 x 8 of 4000 46 - 29, 8 x 8 of 32000 309 - 226).  fp32 caches have
+  // no other kernel, their 32 rows do not fit the registers (2 x 8 heads, 2048 queries of 4: 1009 - 1319).
   for (int i = 0; i < a.n_keys; ++i) {
     const long r = a.keys[i].row_samples * own_rows;
-    p.tile_rows[i] = c->dtype == OBF_BF16 && r > kAttendFewRows ? kAttendTileRows : r > 16 ? 32 : 16;
+    const bool many = a.n_keys == 1 && r > 16 && (long)a.S * a.H * c->token_stride >= (1L << 17);
+    p.tile_rows[i] = c->dtype != OBF_BF16 ? 16 : r > kAttendFewRows ? kAttendTileRows : many ? 32 : 16;
   }
   a.ranges = 0;
   for (int i = a.fused ? 1 : 0; i < a.n_keys; ++i) {
     AttendKeys& s = a.keys[i];
     s.row_tiles = (int)((s.row_samples * own_rows + p.tile_rows[i] - 1) / p.tile_rows[i]);
     const long blocks = (long)s.row_tiles * s.samples * a.H, rows = s.stride + (a.fused ? a.keys[0].stride : 0);
-        const long most_ranges = rows <= 512 ? 1 : (rows + 255) / 256, want = (2 * kNumCU + blocks - 1) / blocks;
+        const long most_ranges = rows <= 512 ? 1 : (rows + 255) / 256, fill = s.row_samples > 1 && p.tile_rows[i] == kAttendTileRows ? kNumCU : 2 * kNumCU, want = (fill + blocks - 1) / blocks;
     s.nsplit = (int)(want < most_ranges ? want : most_ranges);
     s.split0 = a.ranges;
     a.ranges += s.nsplit;
@@ -130,17 +134,8 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
 }
 
 static obf_status_t launch_plan(const AttendPlan& p, int d, int dtype, hipStream_t st) {
-  if (p.a.fused) return launch_attend_tile(p.a, d, st);
-  if (p.a.n_keys == 1 || p.tile_rows[0] == p.tile_rows[1])
-    return p.tile_rows[0] == kAttendTileRows ? launch_attend_tile(p.a, d, st) : launch_attend_few(p.a, p.tile_rows[0], d, dtype, st);
-  for (int i = 0; i < 2; ++i) {
-    AttendArgs one = p.a;
-    one.n_keys = 1;
-    one.keys[0] = p.a.keys[i];
-    if (p.tile_rows[i] == kAttendTileRows) OBF_TRY(launch_attend_tile(one, d, st));
-    else OBF_TRY(launch_attend_few(one, p.tile_rows[i], d, dtype, st));
-  }
-  return OBF_OK;
+  if (p.tile_rows[0] != kAttendTileRows) return launch_attend_few(p.a, p.tile_rows[0], d, dtype, st);
+  return p.a.n_keys == 1 || p.a.fused ? launch_attend_tile(p.a, d, st) : launch_attend_tile_few(p.a, d, st);
 }
 
 static obf_status_t check_attend_ws(const AttendPlan& p, const void* ws, size_t ws_bytes) {

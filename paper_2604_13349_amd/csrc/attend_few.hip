@@ -16,176 +16,12 @@ namespace obf {
 
 template <typename ET, int D, int NB, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
-  typedef FewTile<ET, D> Tile;
-  constexpr int DB = Tile::DB, ROWS = 16 * NB;
-  __shared__ __attribute__((aligned(16))) float sm_o[NW][ROWS][D];
-  __shared__ float sm_m[NW][ROWS], sm_l[NW][ROWS];
-  // which set of keys, tile of rows and range of keys
+  __shared__ __attribute__((aligned(16))) FewShared<D, NB, NW> sm;
   int block = blockIdx.x;
-  const bool second = block >= a.keys[0].blocks;
   AttendKeys k = a.keys[0];
-  if (second) { k = a.keys[1]; block -= a.keys[0].blocks; }
-  const int split = block % k.nsplit;
-  block /= k.nsplit;
-  const int row_tile = block % k.row_tiles, set = block / k.row_tiles;
-  const int h = set % a.H, ks = set / a.H;
-  const int set_rows = k.row_samples * a.T * a.g;
-  const int row0 = row_tile * ROWS;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4;
-  const int n = attend_len(k, ks, h), sink = attend_sink(k, ks, h);
-  // (a message is not causal: its queries have no positions)
-  const int pmin = n - a.T + row0 / a.g, pmax = n - a.T + (min(row0 + ROWS, set_rows) - 1) / a.g;
-  const AttendSpan span = attend_span(k, n, sink, pmin, pmax);
-  const int tiles = (span.count + 31) / 32, per = max(NW, (tiles + k.nsplit - 1) / k.nsplit);   // (a short head does not use all its ranges)
-  const int first = split * per, behind = min(tiles, first + per);
-  const bool joined = a.ranges > 1;
-  const ET* K = (const ET*)k.K + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
-  const ET* V = (const ET*)k.V + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
-
-  typename Tile::Query q[NB];
-  int pos[NB];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const AttendRow w = attend_row(a, k, ks, min(row0 + 16 * nb + (lane & 15), set_rows - 1));
-    Tile::load_query(q[nb], (const ET*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt, lane);
-    pos[nb] = n - a.T + w.t;
-  }
-  f32x4 o[NB][DB];
-  float m[NB], l[NB];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    m[nb] = -INFINITY; l[nb] = 0.f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) o[nb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  // A tile's logits are stored behind the next one's loads: the counter of outstanding accesses runs in order, and a wait for loads behind stores would wait
-  // for those too.  (A message's weights are not asked for.)
-  float* logits = a.logits && !second ? a.logits + ((size_t)set * a.logit_tiles * set_rows + (lane & 15)) * 32 + 4 * quad : nullptr;
-  f32x4 held[NB][2];
-  const auto keep = [&](const int i) {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      if (16 * nb + (lane & 15) < set_rows) {
-        float* at = logits + ((size_t)i * set_rows + 16 * nb) * 32;
-        *(f32x4*)at = held[nb][0];
-        *(f32x4*)(at + 16) = held[nb][1];
-      }
-  };
-  int i = first + wave;
-  for (; i < behind; i += NW) {
-    const int base = 32 * i;
-    typename Tile::Keys kf;
-    typename Tile::Vals vf;
-    Tile::load_keys(kf, K, span, base, lane);
-    Tile::load_vals(vf, V, span, base, lane);
-    if (logits && i > first + wave) keep(i - NW);
-    const bool cut = attend_cut(k, span, sink, pmin, pmax, base, 32);
-    float p[NB][2][4];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      f32x4 x[2];
-      Tile::scores(x, kf, q[nb]);
-      const AttendView view = attend_view(k, span, sink, pos[nb], base + 4 * quad);
-      float mx = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = x[b][r] * a.scale2;
-          if (cut) v = attend_sees(view, 16 * b + r) ? v : -INFINITY;
-          x[b][r] = v;
-          mx = fmaxf(mx, v);
-        }
-      held[nb][0] = x[0]; held[nb][1] = x[1];
-      if (__any(mx > m[nb] + kAttendSlack)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float next = fmaxf(m[nb], mx);
-        const float f = next > -INFINITY ? attend_exp2(m[nb] - next) : 1.f;
-        m[nb] = next;
-        l[nb] *= f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[nb][db] *= f;
-      }
-      const float ref = m[nb] > -INFINITY ? m[nb] : 0.f;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { p[nb][b][r] = attend_exp2(x[b][r] - ref); l[nb] += p[nb][b][r]; }
-    }
-    // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
-    if (cut && k.causal && a.T > 1 && __any(Tile::not_finite(vf))) {
-#pragma unroll 1
-      for (int v = base; v < min(span.count, base + 32); ++v) {
-        const ET* krow = K + few_row<D>(span, v);
-        const ET* row = V + few_row<D>(span, v);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const AttendRow w = attend_row(a, k, ks, min(row0 + 16 * nb + (lane & 15), set_rows - 1));
-          const ET* qrow = (const ET*)a.Q + (size_t)w.s * a.qs + (size_t)(h * a.g + w.gi) * a.qh + (size_t)w.t * a.qt;
-          float dot = 0.f;
-#pragma unroll 1
-          for (int c = 0; c < D; ++c) dot = fmaf(Tile::value(krow, c), Tile::value(qrow, c), dot);
-          if (attend_sees(attend_view(k, span, sink, pos[nb]), v)) {
-            const float wt = attend_exp2(fmaf(dot, a.scale2, -(m[nb] > -INFINITY ? m[nb] : 0.f)));
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-              for (int c = 0; c < 4; ++c) o[nb][db][c] = fmaf(wt, Tile::value(row, Tile::channel(quad, db, c)), o[nb][db][c]);
-          }
-        }
-      }
-    } else {
-      Tile::template values<NB>(o, vf, p);
-    }
-  }
-  if (logits && i > first + wave) keep(i - NW);
-
-  // the waves' parts
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    l[nb] += __shfl_xor(l[nb], 16);
-    l[nb] += __shfl_xor(l[nb], 32);
-    const int r = 16 * nb + (lane & 15);
-    if (quad == 0) { sm_m[wave][r] = m[nb]; sm_l[wave][r] = l[nb]; }
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) sm_o[wave][r][Tile::channel(quad, db, c)] = o[nb][db][c];
-  }
-  __syncthreads();
-  constexpr int PIECES = D / 4;
-  for (int e = threadIdx.x; e < ROWS * PIECES; e += NW * 64) {
-    const int r = e / PIECES, c = (e % PIECES) * 4;
-    if (row0 + r >= set_rows) break;
-    float top = sm_m[0][r];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm_m[w][r]);
-    const float ref = top > -INFINITY ? top : 0.f;
-    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = attend_exp2(sm_m[w][r] - ref);
-      sum = fmaf(f, sm_l[w][r], sum);
-      const float4 x = *(const float4*)&sm_o[w][r][c];
-      v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
-    }
-    const float inv = top > -INFINITY ? 1.f / sum : 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = top > -INFINITY ? v[i] * inv : 0.f;
-    const float lse2 = top > -INFINITY ? top + attend_log2(sum) : -INFINITY;
-    const AttendRow w = attend_row(a, k, ks, row0 + r);
-    const size_t number = attend_row_number(a, h, w);
-    if (joined) {
-      const size_t at = (size_t)(k.split0 + split) * a.rows + number;
-      if (c == 0) a.part_lse[at] = lse2;
-      if (top > -INFINITY) *(float4*)(a.part_O + at * D + c) = make_float4(v[0], v[1], v[2], v[3]);   // (nobody reads the others)
-    } else {
-      if (c == 0 && a.lse) a.lse[number] = lse2 * 0.69314718055994531f;
-      store4((ET*)a.O + (size_t)w.s * a.os + (size_t)(h * a.g + w.gi) * a.oh + (size_t)w.t * a.ot + c, v);
-    }
-  }
+  const bool second = block >= k.blocks;
+  if (second) { block -= k.blocks; k = a.keys[1]; }
+  attend_few<ET, D, NB, NW>(a, k, block, !second, sm);
 }
 
 // Joins the ranges of a query row, O = sum_i 2^(lse_i - lse) O_i, and turns the logits of the own keys into weights, mass_j += sum_r 2^(x_rj - lse_r).
@@ -296,21 +132,20 @@ __global__ __launch_bounds__(JN_THREADS) void k_attend_join(const AttendArgs a, 
   store4((ET*)a.O + (size_t)s * a.os + (size_t)hq * a.oh + (size_t)t * a.ot + c, v);
 }
 
-#ifndef FEW_NW
-#define FEW_NW 4
-#endif
-template <typename ET, int D>
-static void few_launch(const AttendArgs& a, int rows, hipStream_t st) {
-  const int blocks = a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0);
-  if (rows == 16) hipLaunchKernelGGL((k_attend_few<ET, D, 1, FEW_NW>), dim3(blocks), dim3(FEW_NW * 64), 0, st, a);
-  else hipLaunchKernelGGL((k_attend_few<ET, D, 2, 2>), dim3(blocks), dim3(128), 0, st, a);
-}
-
-// rows: of a workgroup's tile, 16 or 32
+// rows: of a workgroup's tile, 16, or 32 (bf16)
 obf_status_t launch_attend_few(const AttendArgs& a, int rows, int d, int dtype, hipStream_t st) {
   ProfScope prof(ST_ATTEND, st);
-  if (dtype == OBF_BF16) { if (d == 128) few_launch<uint16_t, 128>(a, rows, st); else few_launch<uint16_t, 64>(a, rows, st); }
-  else { if (d == 128) few_launch<float, 128>(a, rows, st); else few_launch<float, 64>(a, rows, st); }
+  const dim3 grid(a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0)), threads(256);
+  if (dtype == OBF_F32) {
+    if (d == 128) hipLaunchKernelGGL((k_attend_few<float, 128, 1, 4>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_few<float, 64, 1, 4>), grid, threads, 0, st, a);
+  } else if (rows == 16) {
+    if (d == 128) hipLaunchKernelGGL((k_attend_few<uint16_t, 128, 1, 4>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_few<uint16_t, 64, 1, 4>), grid, threads, 0, st, a);
+  } else {
+    if (d == 128) hipLaunchKernelGGL((k_attend_few<uint16_t, 128, 2, 4>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_few<uint16_t, 64, 2, 4>), grid, threads, 0, st, a);
+  }
   return check_launch("attend");
 }
 

@@ -88,6 +88,12 @@ CASES = [
     (BF, 128, 1, 2, 4, 150, 150, (100, 150), False, 0, 0),
     (BF, 64, 1, 2, 1, 1, 300, (100, 300), False, 0, 0),
     (BF, 128, 1, 1, 1, 300, 300, (300, 300), True, 90, 130),
+    (BF, 128, 1, 2, 4, 5, 66000, (100, 300), True, 0, 0),
+    (BF, 64, 1, 2, 3, 8, 66000, (100, 300), True, 40, 3),
+    (BF, 128, 1, 2, 1, 32, 66000, (20, 300), False, 0, 0),
+    (BF, 128, 1, 2, 4, 8, 66000, (200, 400), True, 64, 4),
+    (BF, 128, 2, 2, 17, 1, 300, (100, 300), True, 0, 0),
+    (BF, 128, 1, 1, 33, 1, 300, (100, 300), True, 0, 0),
     (F32, 64, 1, 1, 1, 1, 1, (1, 1), True, 0, 0),
     (F32, 64, 2, 2, 2, 1, 333, (1, 333), True, 0, 0),
     (F32, 128, 2, 2, 5, 1, 700, (500, 700), True, 128, 4),
@@ -125,7 +131,7 @@ def test_first_rows_per_head_stay_visible(T):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("T,window", [(2, 0), (40, 0), (70, 11), (150, 64)])
+@pytest.mark.parametrize("T,window", [(2, 0), (13, 5), (40, 0), (70, 11), (150, 64)])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
 def test_hidden_rows_of_any_value_do_not_reach_a_query(dtype, T, window, value):
     """Rows that later queries see (or, behind a window, earlier ones saw) hold infinities or no numbers: a query that does not see them is as if they were 0."""
@@ -185,6 +191,9 @@ SHARED = [
     (BF, 128, 3, 2, 4, 2, 90, (2, 90), 333, (1, 333), 16),
     (BF, 128, 2, 1, 5, 70, 100, (70, 100), 270, (200, 270), 0),
     (BF, 64, 3, 1, 2, 64, 100, (64, 100), 129, (129, 129), 33),
+    (BF, 128, 3, 2, 8, 3, 50, (3, 50), 700, (600, 700), 9),
+    (BF, 64, 2, 2, 4, 6, 50, (6, 50), 64, (0, 64), 0),
+    (BF, 128, 2, 2, 3, 40, 600, (500, 600), 1000, (900, 1000), 0),
     (F32, 64, 3, 2, 2, 1, 50, (1, 50), 150, (100, 150), 0),
     (F32, 128, 2, 1, 3, 20, 50, (20, 50), 65, (65, 65), 0),
 ]
