@@ -105,8 +105,14 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   for (int i = a.fused ? 1 : 0; i < a.n_keys; ++i) {
     AttendKeys& s = a.keys[i];
     s.row_tiles = (int)((s.row_samples * own_rows + p.tile_rows[i] - 1) / p.tile_rows[i]);
-    const long blocks = (long)s.row_tiles * s.samples * a.H, rows = s.stride + (a.fused ? a.keys[0].stride : 0);
-        const long most_ranges = rows <= 512 ? 1 : (rows + 255) / 256, fill = s.row_samples > 1 && p.tile_rows[i] == kAttendTileRows ? kNumCU : 2 * kNumCU, want = (fill + blocks - 1) / blocks;
+    const long blocks = (long)s.row_tiles * s.samples * a.H, seen = s.window > 0 ? (long)s.window + s.sink + p.tile_rows[i] / a.g + 1 : s.stride;
+    const long rows = (seen < s.stride ? seen : s.stride) + (a.fused ? a.keys[0].stride : 0);     // that a tile sees, at most (but for sink_len)
+    // Ranges where the sets do not fill the chip, two workgroups per compute unit (one where a message's tiles of many rows share it with the own rows' loads);
+    // none for short caches, whose join would take longer (us, ranges and none: 128 sets of 590 rows 17.0 - 15.4, 256 of 1000 31 - 28, of 1500 43.3 - 39.7,
+    // 252 workgroups of fp32 rows 20 - 13.5; 64 sets of 1000 15.8 - 18.6, 128 of 2000 32.4 - 34.7; 8 sets of 340 9.8 - 8.1, of 1000 11.8 - 12.6).
+    const bool none = rows <= 512 || (blocks >= 128 && rows <= 8 * blocks && rows <= 2048);
+    const long most_ranges = none ? 1 : (rows + 255) / 256, fill = s.row_samples > 1 && p.tile_rows[i] == kAttendTileRows ? kNumCU : 2 * kNumCU;
+    const long want = (fill + blocks - 1) / blocks;
     s.nsplit = (int)(want < most_ranges ? want : most_ranges);
     s.split0 = a.ranges;
     a.ranges += s.nsplit;
