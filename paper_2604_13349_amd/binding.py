@@ -634,34 +634,43 @@ def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sin
 _EVICT_OUT = ("K_out", "V_out", "mass_out", "pos_out", "idx", "len_out")
 
 
+def _flat(t: Optional[torch.Tensor]):
+    """The same of a tensor that has to be contiguous."""
+    return None if t is None else (t.shape, t.is_contiguous(), t.dtype, t.get_device())
+
+
 @functools.lru_cache(maxsize=1024)
-def _evict_plan(K, V, mass, pos, kv_len, sink_len, budget, sink, out_stride, outs):
-    """Checks an eviction by the tensors' metadata.  Returns (heads, out_stride, shapes and dtypes of the outputs)."""
+def _evict_plan(K, V, mass, pos, kv_len, sink_len, budget, sink, out_stride, given):
+    """Checks an eviction by the tensors' metadata; given: of the outputs in the order of _EVICT_OUT.  Returns (heads, rows, d, dtype, out_stride, shapes and
+    dtypes of the outputs)."""
+    named = (("K", K), ("V", V), ("mass", mass), ("pos", pos), ("kv_len", kv_len), ("sink_len", sink_len)) + tuple(zip(_EVICT_OUT, given))
+    if K[3] < 0:
+        raise ValueError("tensors must be on a GPU")
+    for name, m in named:
+        if m is not None and m[3] != K[3]:
+            raise ValueError(f"{name} is not on K's GPU")
+        if m is not None and not m[1]:
+            raise ValueError(f"{name} must be contiguous")
     if len(K[0]) < 2 or K[2] not in (torch.float32, torch.bfloat16):
         raise ValueError("K must be [..., rows, d], float32 or bfloat16")
-    _same_device((("K", K), ("V", V), ("mass", mass), ("pos", pos), ("kv_len", kv_len), ("sink_len", sink_len)) + outs)
     lead, rows, d = tuple(K[0][:-2]), K[0][-2], K[0][-1]
-    _want("K", K, K[0], K[2])
-    _want("V", V, K[0], K[2])
-    _want("mass", mass, lead + (rows,), torch.float32)
-    _want("pos", pos, lead + (rows,), torch.int32)
-    _want("kv_len", kv_len, lead, torch.int32)
-    _want("sink_len", sink_len, lead, torch.int32)
-    given = dict(outs)
+    outs = dict(zip(_EVICT_OUT, given))
     if out_stride is None:
-        if given.get("K_out") is not None:
-            out_stride = given["K_out"][0][-2]
+        if outs["K_out"] is not None:
+            out_stride = outs["K_out"][0][-2]
         elif sink_len is not None:
             raise ValueError("out_stride is needed with sink_len")
         else:
             out_stride = max(1, min(budget + sink, rows))
-    want = {"K_out": (lead + (out_stride, d), K[2]), "V_out": (lead + (out_stride, d), K[2]), "mass_out": (lead + (out_stride,), torch.float32),
-            "idx": (lead + (out_stride,), torch.int32), "len_out": (lead, torch.int32)}
-    if pos is not None:
-        want["pos_out"] = (lead + (out_stride,), torch.int32)
-    for name, (shape, dtype) in want.items():
-        _want(name, given.get(name), shape, dtype)
-    return int(np.prod(lead)) if lead else 1, out_stride, want
+    want = {"V": (K[0], K[2]), "mass": (lead + (rows,), torch.float32), "pos": (lead + (rows,), torch.int32), "kv_len": (lead, torch.int32),
+            "sink_len": (lead, torch.int32), "K_out": (lead + (out_stride, d), K[2]), "V_out": (lead + (out_stride, d), K[2]),
+            "mass_out": (lead + (out_stride,), torch.float32), "pos_out": (lead + (out_stride,), torch.int32), "idx": (lead + (out_stride,), torch.int32),
+            "len_out": (lead, torch.int32)}
+    for name, m in named[1:]:
+        if m is not None and (tuple(m[0]) != tuple(want[name][0]) or m[2] != want[name][1]):
+            raise ValueError(f"{name} must be {want[name][1]} {list(want[name][0])}")
+    return (int(np.prod(lead)) if lead else 1, rows, d, OBF_BF16 if K[2] == torch.bfloat16 else OBF_F32, out_stride,
+            {k: want[k] for k in _EVICT_OUT if k != "pos_out" or pos is not None})
 
 
 def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, sink_len=None, pos=None, out=None, out_stride: Optional[int] = None):
@@ -669,17 +678,16 @@ def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, 
     int32 [...].  out: buffers to fill, K_out, V_out [..., out_stride, d], mass_out, pos_out, idx [..., out_stride], len_out [...]; those not given are
     allocated with out_stride rows per head (default: sink + budget; needed with sink_len).  Rows behind len_out stay as they are."""
     o = out if out is not None else {}
-    heads, out_stride, want = _evict_plan(_meta(K), _meta(V), _meta(mass), _meta(pos), _meta(kv_len), _meta(sink_len), budget, sink, out_stride,
-                                          tuple((k, _meta(o[k])) for k in _EVICT_OUT if k in o))
+    heads, rows, d, dtype, out_stride, want = _evict_plan(_flat(K), _flat(V), _flat(mass), _flat(pos), _flat(kv_len), _flat(sink_len), budget, sink, out_stride,
+                                                          tuple([_flat(o.get(k)) for k in _EVICT_OUT]))
     for name in want:
         if name not in o:
             o[name] = torch.empty(want[name][0], dtype=want[name][1], device=K.device)
-    rows, d = K.shape[-2], K.shape[-1]
     with _on(K.device) as stream:
         _check(load_library().obf_evict(
-            heads, d, OBF_BF16 if K.dtype == torch.bfloat16 else OBF_F32, K.data_ptr(), V.data_ptr(), mass.data_ptr(), _addr(pos), _addr(kv_len), rows, rows,
-            budget, recent, _addr(sink_len), sink, o["K_out"].data_ptr(), o["V_out"].data_ptr(), o["mass_out"].data_ptr(),
-            o["pos_out"].data_ptr() if pos is not None else None, o["idx"].data_ptr(), o["len_out"].data_ptr(), out_stride, stream))
+            heads, d, dtype, K.data_ptr(), V.data_ptr(), mass.data_ptr(), _addr(pos), _addr(kv_len), rows, rows, budget, recent, _addr(sink_len), sink,
+            o["K_out"].data_ptr(), o["V_out"].data_ptr(), o["mass_out"].data_ptr(), o["pos_out"].data_ptr() if pos is not None else None, o["idx"].data_ptr(),
+            o["len_out"].data_ptr(), out_stride, stream))
     return o
 
 
