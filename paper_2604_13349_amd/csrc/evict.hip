@@ -19,10 +19,41 @@ __device__ __forceinline__ uint32_t mass_key(const float f) {
 }
 
 constexpr int EV_LIST = 256;
+constexpr long kEvictOwnRows = 128 << 10;      // bytes of a head's kept rows up to which its own workgroup copies them
 
-// PER keys per thread in registers, thread t those of rows t, t + 1024, ...; 0: read again for every pass.
+// Rows r0, r0 + step, ... of a head, UNROLL at a time, by the threads of a row's 16-byte pieces c; n: rows kept, at least one.
+template <int UNROLL>
+__device__ __forceinline__ void evict_rows(const EvictArgs& a, const int head, const int n, const int r0, const int step, const int c) {
+  const EvictRow *K = (const EvictRow*)a.K, *V = (const EvictRow*)a.V;
+  EvictRow *K_out = (EvictRow*)a.K_out, *V_out = (EvictRow*)a.V_out;
+  const int32_t* idx = a.idx + (size_t)head * a.out_stride;
+  // (rows behind the end load the last one's again: no condition holds up a load)
+  size_t from[UNROLL];
+  EvictRow kv[UNROLL], vv[UNROLL];
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) from[u] = (size_t)head * a.in_stride + idx[min(r0 + u * step, n - 1)];
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) { kv[u] = K[from[u] * a.row_vec + c]; vv[u] = V[from[u] * a.row_vec + c]; }
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u)
+    if (r0 + u * step < n) {
+      const size_t row = (size_t)head * a.out_stride + r0 + u * step;
+      K_out[row * a.row_vec + c] = kv[u];
+      V_out[row * a.row_vec + c] = vv[u];
+    }
+}
+
+// What goes with row r.
+__device__ __forceinline__ void evict_beside(const EvictArgs& a, const int head, const int r) {
+  const size_t row = (size_t)head * a.out_stride + r, at = (size_t)head * a.in_stride + a.idx[row];
+  a.mass_out[row] = a.mass[at];
+  if (a.pos) a.pos_out[row] = a.pos[at];
+}
+
+// The list of a head's kept rows; returns their number, or -1.  PER keys per thread in registers, thread t those of rows t, t + 1024, ...; 0: read again for
+// every pass.
 template <int PER>
-__global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) {
+__device__ __forceinline__ int evict_list(const EvictArgs& a) {
   constexpr int REGS = PER > 0 ? PER : 1;
   __shared__ int hist[EV_BINS];
   __shared__ uint32_t wlo[EV_WAVES], whi[EV_WAVES], list[EV_LIST], s_key;
@@ -36,18 +67,18 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) 
   if (n < 0 || n > a.in_stride || kept > a.out_stride) {            // no length, or no room: flagged, nothing of the head is written
     for (int i = tid; i < a.out_stride; i += EV_THREADS) out[i] = -1;
     if (tid == 0) a.len_out[head] = -1;
-    return;
+    return -1;
   }
   if (tid == 0) a.len_out[head] = kept;
   for (int i = kept + tid; i < a.out_stride; i += EV_THREADS) out[i] = -1;
   if (kept == n) {
     for (int i = tid; i < n; i += EV_THREADS) out[i] = i;
-    return;
+    return kept;
   }
   const int last = n - a.recent, want = a.budget - a.recent;        // of the rows first .. last - 1 the `want` of largest mass are kept
   for (int i = tid; i < first; i += EV_THREADS) out[i] = i;
   for (int i = tid; i < a.recent; i += EV_THREADS) out[first + want + i] = last + i;
-  if (want == 0) return;
+  if (want == 0) return kept;
   const float* mass = a.mass + (size_t)head * a.in_stride;
   uint32_t key[REGS];
   if (PER > 0) {
@@ -165,51 +196,48 @@ __global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a) 
       __syncthreads();
     }
   }
+  return kept;
+}
+
+// with_rows: the workgroup copies its head's rows too.
+template <int PER>
+__global__ __launch_bounds__(EV_THREADS) void k_evict_select(const EvictArgs a, const int with_rows) {
+  const int n = evict_list<PER>(a);
+  if (!with_rows || n <= 0) return;
+  __syncthreads();                                                  // (the list, written by the whole workgroup)
+  const int step = EV_THREADS / a.row_vec, c = threadIdx.x % a.row_vec;
+  for (int r = (int)threadIdx.x / a.row_vec; r < n; r += 2 * step) evict_rows<2>(a, blockIdx.x, n, r, step, c);
+  for (int r = threadIdx.x; r < n; r += EV_THREADS) evict_beside(a, blockIdx.x, r);
 }
 
 constexpr int EG_THREADS = 256, EG_UNROLL = 4;
 
-__global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictRow* __restrict__ K, const EvictRow* __restrict__ V, const float* __restrict__ mass,
-                                                           const int32_t* __restrict__ pos, const int32_t* __restrict__ idx, const int32_t* __restrict__ len,
-                                                           EvictRow* __restrict__ K_out, EvictRow* __restrict__ V_out, float* __restrict__ mass_out,
-                                                           int32_t* __restrict__ pos_out, const int row_vec, const int in_stride, const int out_stride) {
-  const int head = blockIdx.y, per = EG_THREADS / row_vec, c = threadIdx.x % row_vec;
-  const int block0 = (int)blockIdx.x * per * EG_UNROLL, r0 = block0 + (int)threadIdx.x / row_vec;
-  const int n = len[head];                                          // -1 for a head that was flagged
+__global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictArgs a) {
+  const int head = blockIdx.y, per = EG_THREADS / a.row_vec;
+  const int block0 = (int)blockIdx.x * per * EG_UNROLL;
+  const int n = a.len_out[head];                                    // -1 for a head that was flagged
   if (block0 >= n) return;
-  // (rows behind the end load the last one's again: no condition holds up a load)
-  size_t from[EG_UNROLL];
-  EvictRow kv[EG_UNROLL], vv[EG_UNROLL];
-#pragma unroll
-  for (int u = 0; u < EG_UNROLL; ++u) from[u] = (size_t)head * in_stride + idx[(size_t)head * out_stride + min(r0 + u * per, n - 1)];
-#pragma unroll
-  for (int u = 0; u < EG_UNROLL; ++u) { kv[u] = K[from[u] * row_vec + c]; vv[u] = V[from[u] * row_vec + c]; }
-#pragma unroll
-  for (int u = 0; u < EG_UNROLL; ++u)
-    if (r0 + u * per < n) {
-      const size_t row = (size_t)head * out_stride + r0 + u * per;
-      K_out[row * row_vec + c] = kv[u];
-      V_out[row * row_vec + c] = vv[u];
-    }
+  evict_rows<EG_UNROLL>(a, head, n, block0 + (int)threadIdx.x / a.row_vec, per, threadIdx.x % a.row_vec);
   // a lane per row for what goes with it
   const int r = block0 + (int)threadIdx.x;
-  if ((int)threadIdx.x < per * EG_UNROLL && r < n) {
-    const size_t row = (size_t)head * out_stride + r, at = (size_t)head * in_stride + idx[row];
-    mass_out[row] = mass[at];
-    if (pos) pos_out[row] = pos[at];
-  }
+  if ((int)threadIdx.x < per * EG_UNROLL && r < n) evict_beside(a, head, r);
 }
 
 obf_status_t launch_evict(const EvictArgs& a, hipStream_t st) {
   ProfScope prof(ST_EVICT, st);
-  if (a.in_stride <= EV_THREADS) hipLaunchKernelGGL(k_evict_select<1>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
-  else if (a.in_stride <= 8 * EV_THREADS) hipLaunchKernelGGL(k_evict_select<8>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
-  else if (a.in_stride <= 32 * EV_THREADS) hipLaunchKernelGGL(k_evict_select<32>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
-  else hipLaunchKernelGGL(k_evict_select<0>, dim3(a.heads), dim3(EV_THREADS), 0, st, a);
-  const int per = EG_THREADS / a.row_vec * EG_UNROLL;
-  hipLaunchKernelGGL(k_evict_rows, dim3((a.out_stride + per - 1) / per, a.heads), dim3(EG_THREADS), 0, st,
-                     (const EvictRow*)a.K, (const EvictRow*)a.V, a.mass, a.pos, a.idx, a.len_out, (EvictRow*)a.K_out, (EvictRow*)a.V_out, a.mass_out, a.pos_out,
-                     a.row_vec, a.in_stride, a.out_stride);
+  // A head's own workgroup copies its rows where they are few: one launch for two (us, two and one, heads x rows kept of 512 bytes: 2 x 64 8.9 - 7.3,
+  // 64 x 205 12.8 - 11.5, 288 x 120 22.7 - 21.0, 1000 x 100 41 - 37; 8 x 400 12.0 - 13.0, 288 x 1229 93 - 110).
+  const long bytes = (long)(a.out_stride < a.budget + a.sink ? a.out_stride : a.budget + a.sink) * a.row_vec * 32;
+  const int with_rows = bytes <= kEvictOwnRows;
+  const dim3 grid(a.heads), threads(EV_THREADS);
+  if (a.in_stride <= EV_THREADS) hipLaunchKernelGGL(k_evict_select<1>, grid, threads, 0, st, a, with_rows);
+  else if (a.in_stride <= 8 * EV_THREADS) hipLaunchKernelGGL(k_evict_select<8>, grid, threads, 0, st, a, with_rows);
+  else if (a.in_stride <= 32 * EV_THREADS) hipLaunchKernelGGL(k_evict_select<32>, grid, threads, 0, st, a, with_rows);
+  else hipLaunchKernelGGL(k_evict_select<0>, grid, threads, 0, st, a, with_rows);
+  if (!with_rows) {
+    const int per = EG_THREADS / a.row_vec * EG_UNROLL;
+    hipLaunchKernelGGL(k_evict_rows, dim3((a.out_stride + per - 1) / per, a.heads), dim3(EG_THREADS), 0, st, a);
+  }
   return check_launch("evict");
 }
 
