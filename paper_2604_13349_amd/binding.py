@@ -453,6 +453,14 @@ def append_message(prev_K, prev_V, prev_len, keep_K, keep_V, n_keep, gen_K, gen_
     return msg_K, msg_V, msg_len
 
 
+def _int(name: str, v) -> int:
+    """A number that the C side takes as int32 (which refuses negative ones itself)."""
+    v = int(v)
+    if abs(v) >= 1 << 31:
+        raise ValueError(f"{name} out of range")
+    return v
+
+
 def _meta(t: Optional[torch.Tensor]):
     """What a call is checked and laid out by; never a tensor's address."""
     return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
@@ -488,6 +496,8 @@ def _row_strides(name: str, m, d: int):
     shape, stride = m[0], m[1]
     if stride[3] != 1 and shape[3] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
+    if not any(w for n, w in zip(shape[:3], stride) if n > 1) and max(shape[:3]) > 1:
+        raise ValueError(f"{name}: one row expanded to all")          # (three strides of 0 stand for a contiguous tensor)
     return [stride[i] if shape[i] > 1 else d * max(1, shape[2]) for i in range(3)]
 
 
@@ -585,7 +595,7 @@ def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, pref
     pk, pv, pl = prefix if prefix is not None else (None, None, None)
     O, lse = o["O"], o["lse"]
     c, need, front, copy_lens = _attend_plan(_meta(Q), _meta(K), _meta(V), _meta(O), _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), _meta(pk),
-                                             _meta(pv), _meta(pl), causal, window, sink)
+                                             _meta(pv), _meta(pl), bool(causal), _int("window", window), _int("sink", sink))
     lib = load_library()
     with _on(Q.device) as stream:
         ws = o.get("ws")
@@ -619,8 +629,8 @@ def attend_shared(Q, prefix_K, prefix_V, K, V, prefix_len=None, kv_len=None, cau
 def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sink_len=None, ws=None):
     """obf_attend_mass: adds to mass float32 [S,H,rows], in place, the attention weight of the rows of K under the lse [S,H*g,T] of an earlier call (whose
     workspace may be handed over as ws)."""
-    c, need, _, copy_lens = _attend_plan(_meta(Q), _meta(K), None, None, _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), None, None, None, causal,
-                                         window, sink)
+    c, need, _, copy_lens = _attend_plan(_meta(Q), _meta(K), None, None, _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), None, None, None, bool(causal),
+                                         _int("window", window), _int("sink", sink))
     with _on(Q.device) as stream:
         if ws is None or ws.numel() < need:
             ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
@@ -678,6 +688,7 @@ def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, 
     int32 [...].  out: buffers to fill, K_out, V_out [..., out_stride, d], mass_out, pos_out, idx [..., out_stride], len_out [...]; those not given are
     allocated with out_stride rows per head (default: sink + budget; needed with sink_len).  Rows behind len_out stay as they are."""
     o = out if out is not None else {}
+    budget, recent, sink = _int("budget", budget), _int("recent", recent), _int("sink", sink)
     heads, rows, d, dtype, out_stride, want = _evict_plan(_flat(K), _flat(V), _flat(mass), _flat(pos), _flat(kv_len), _flat(sink_len), budget, sink, out_stride,
                                                           tuple([_flat(o.get(k)) for k in _EVICT_OUT]))
     for name in want:

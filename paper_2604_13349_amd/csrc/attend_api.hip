@@ -37,12 +37,12 @@ static obf_status_t check_attend(const obf_attend_t* c) {
   if (c->n_queries > kAttendMaxQueries) { set_error("attend: n_queries above the supported %d", kAttendMaxQueries); return OBF_ERR_UNSUPPORTED; }
   if (c->group > kAttendMaxGroup) { set_error("attend: group above the supported %d", kAttendMaxGroup); return OBF_ERR_UNSUPPORTED; }
   if ((int64_t)c->n_samples * c->n_kv_heads > 65535) { set_error("attend: more than 65535 heads in one call"); return OBF_ERR_UNSUPPORTED; }
-  if ((int64_t)c->n_samples * c->n_kv_heads * c->group * c->n_queries > ((int64_t)1 << 28)) {
-    set_error("attend: more than 2^28 query rows in one call");
+  if ((int64_t)c->n_samples * c->n_kv_heads * c->group * c->n_queries > ((int64_t)1 << 26)) {
+    set_error("attend: more than 2^26 query rows in one call");
     return OBF_ERR_UNSUPPORTED;
   }
-  if ((int64_t)c->n_samples * c->n_kv_heads * c->token_stride > ((int64_t)1 << 36)) {
-    set_error("attend: more than 2^36 cache rows in one call");
+  if ((int64_t)c->n_samples * c->n_kv_heads * c->token_stride > ((int64_t)1 << 30)) {
+    set_error("attend: more than 2^30 cache rows in one call");
     return OBF_ERR_UNSUPPORTED;
   }
   return OBF_OK;
@@ -151,6 +151,11 @@ static obf_status_t check_attend_ws(const AttendPlan& p, const void* ws, size_t 
   return OBF_OK;
 }
 
+static obf_status_t check_apart(const void* O, const void* Q, const void* K, const void* V) {
+  if (O == Q || O == K || O == V) { set_error("O must not be an input"); return OBF_ERR_INVALID_ARG; }
+  return OBF_OK;
+}
+
 static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
                                int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
                                const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, hipStream_t st) {
@@ -191,6 +196,7 @@ obf_status_t obf_attend(const obf_attend_t* call, const void* Q, const void* K, 
                         void* O, float* lse, float* mass, void* ws, size_t ws_bytes, void* stream) {
   OBF_TRY(check_attend(call));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("O", O));
+  OBF_TRY(check_apart(O, Q, K, V));
   return run_attend(call, Q, nullptr, nullptr, nullptr, 0, 0, K, V, kv_len, sink_len, O, lse, mass, ws, ws_bytes, (hipStream_t)stream);
 }
 
@@ -205,6 +211,7 @@ obf_status_t obf_attend_shared(const obf_attend_t* call, const void* Q, const vo
   if (prefix_stride > kAttendMaxStride) { set_error("attend: prefix_stride above the supported %d", kAttendMaxStride); return OBF_ERR_UNSUPPORTED; }
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("prefix_K", prefix_K)); OBF_TRY(check_aligned("prefix_V", prefix_V));
   OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("O", O));
+  OBF_TRY(check_apart(O, Q, K, V));
   return run_attend(call, Q, prefix_K, prefix_V, prefix_len, prefix_len_all, prefix_stride, K, V, kv_len, sink_len, O, lse, nullptr, ws, ws_bytes,
                     (hipStream_t)stream);
 }

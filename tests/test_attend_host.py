@@ -25,10 +25,10 @@ def _call(**kw):
     return c
 
 
-FAKE = C.c_void_p(1 << 20)      # never dereferenced: every call below fails on the host
+FAKE, FAKE_O = C.c_void_p(1 << 20), C.c_void_p(1 << 40)      # never dereferenced: every call below fails on the host
 
 
-def _attend(lib, c, Q=FAKE, K=FAKE, V=FAKE, O=FAKE, ws=FAKE, ws_bytes=1 << 40):
+def _attend(lib, c, Q=FAKE, K=FAKE, V=FAKE, O=FAKE_O, ws=FAKE, ws_bytes=1 << 40):
     rc = lib.obf_attend(C.byref(c) if c is not None else None, Q, K, V, None, None, O, None, None, ws, ws_bytes, None)
     return rc, lib.obf_last_error().decode()
 
@@ -40,8 +40,8 @@ REFUSED = [
     (dict(len_stride=1), 1, "len_stride"), (dict(len_stride=-1), 1, "len_stride"), (dict(sample_stride=199), 1, "sample_stride"),
     (dict(q_stride=(1024, 128, 4)), 1, "16 bytes"), (dict(o_stride=(1024, -8, 128)), 1, "16 bytes"),
     (dict(head_dim=96), 2, "head_dim"), (dict(token_stride=(1 << 24) + 1), 2, "token_stride"), (dict(n_queries=(1 << 20) + 1), 2, "n_queries"),
-    (dict(group=129), 2, "group"), (dict(n_samples=32768), 2, "65535"), (dict(n_samples=4096, n_queries=1 << 15), 2, "2^28"),
-    (dict(n_samples=16384, token_stride=1 << 23), 2, "2^36"),
+    (dict(group=129), 2, "group"), (dict(n_samples=32768), 2, "65535"), (dict(n_samples=4096, n_queries=1 << 13), 2, "2^26"),
+    (dict(n_samples=16384, token_stride=1 << 16), 2, "2^30"),
 ]
 
 
@@ -63,6 +63,7 @@ def test_refused_pointers_and_workspaces(lib):
         assert rc == 1 and name in msg
         rc, msg = _attend(lib, c, **{name: C.c_void_p((1 << 20) + 8)})
         assert rc == 1 and "aligned" in msg
+    assert _attend(lib, c, O=FAKE)[0] == 1
     assert _attend(lib, c, ws=None)[0] == 1
     assert _attend(lib, c, ws=C.c_void_p((1 << 20) + 16))[0] == 1
     need = lib.obf_attend_workspace_bytes(C.byref(c), 0)
@@ -71,7 +72,7 @@ def test_refused_pointers_and_workspaces(lib):
     assert lib.obf_attend_workspace_bytes(C.byref(c), -1) == 0
 
     def shared(pk=FAKE, pv=FAKE, n=10, stride=10):
-        return lib.obf_attend_shared(C.byref(c), FAKE, pk, pv, None, n, stride, FAKE, FAKE, None, None, FAKE, None, FAKE, need, None)
+        return lib.obf_attend_shared(C.byref(c), FAKE, pk, pv, None, n, stride, FAKE, FAKE, None, None, FAKE_O, None, FAKE, need, None)
 
     assert shared(pk=None) == 1 and shared(pv=None) == 1 and shared(n=11) == 1 and shared(n=-1) == 1 and shared(stride=0, n=0) == 1
     assert shared(n=1, stride=(1 << 24) + 1) == 2

@@ -354,6 +354,21 @@ def test_captured_calls_replay(T):
                 assert torch.equal(got[2]["K_out"][s, h, :n], K[s, h, got[2]["idx"][s, h, :n].long()])
 
 
+def test_queries_shared_by_samples_or_heads():
+    """Broadcast queries (strides of 0) and one KV head per query head."""
+    B = _b()
+    Q, K, V = _make(23, BF, 64, 3, 2, 3, 5, 90)
+    kv_len = _lens(7, 3, 2, 5, 90)
+    for q in (Q[:1].expand(3, 6, 5, 64), Q[:, :1].expand(3, 6, 5, 64), Q[:, :, :1].expand(3, 6, 5, 64)):
+        O, lse, _, tO, tl, _ = R.attend(q, K, V, kv_len)
+        qd = q[[0]].cuda().expand(3, 6, 5, 64) if q.stride(0) == 0 else q[:, [0]].cuda().expand(3, 6, 5, 64) if q.stride(1) == 0 \
+            else q[:, :, [0]].cuda().expand(3, 6, 5, 64)
+        assert 0 in qd.stride()
+        o = B.attend(qd, K.cuda(), V.cuda(), kv_len=kv_len.cuda())
+        _check("O", o["O"], O, tO)
+        _check("lse", o["lse"], lse, tl)
+
+
 def test_two_calls_on_two_streams():
     B = _b()
     Q, K, V = (x.cuda() for x in _make(18, BF, 128, 4, 4, 4, 1, 3000))
@@ -384,6 +399,8 @@ def test_binding_refuses_tensors_that_do_not_match():
            lambda: B.attend(Q.cpu(), K, V), lambda: B.attend(Q, K, V, kv_len=n.cpu()), lambda: B.attend(Q.half(), K.half(), V.half()),
            lambda: B.attend(Q, K, V, out={"O": torch.empty((2, 4, 3, 64), dtype=BF, device="cuda")}),
            lambda: B.attend(Q, K, V, out={"O": torch.empty((1, 4, 3, 128), dtype=BF, device="cuda").expand(2, 4, 3, 128)}),
+           lambda: B.attend(Q[:1, :1, :1].expand(2, 4, 3, 128), K, V), lambda: B.attend(Q, K, V, window=1 << 31), lambda: B.attend(Q, K, V, sink=1 << 32),
+           lambda: B.evict(K, V, mass, 1 << 32), lambda: B.attend(Q, K[:1].expand(2, 2, 40, 128), V[:1].expand(2, 2, 40, 128)),
            lambda: B.attend_shared(Q, K, V, K, V), lambda: B.attend_shared(Q, K[0].float(), V[0].float(), K, V),
            lambda: B.attend_shared(Q, K[0], V[0], K, V, prefix_len=n), lambda: B.attend_mass(Q, K, mass, mass),
            lambda: B.evict(K, V, mass[..., :39], 8), lambda: B.evict(K, V, mass, 8, sink_len=n), lambda: B.evict(K, V, mass, 8, pos=mass)]
@@ -391,7 +408,8 @@ def test_binding_refuses_tensors_that_do_not_match():
         with pytest.raises(ValueError):
             f()
             pytest.fail(f"call {i} was taken")
-    for f in (lambda: B.attend(Q, K, V, window=-1), lambda: B.attend(Q, K, V, window=3, causal=False), lambda: B.attend(Q, K, V, sink=-1),
+    for f in (lambda: B.attend(Q, K, V, out={"O": Q}), lambda: B.attend(Q[..., 1:65], K[..., :64].contiguous(), V[..., :64].contiguous()),
+              lambda: B.attend(Q, K, V, window=-1), lambda: B.attend(Q, K, V, window=3, causal=False), lambda: B.attend(Q, K, V, sink=-1),
               lambda: B.evict(K, V, mass, 8, recent=9), lambda: B.evict(K, V, mass, -1), lambda: B.evict(K, V, mass, 8, sink=3, out_stride=10),
               lambda: B.evict(K, V, mass, 40, out={"K_out": K, "V_out": torch.empty_like(V)}),
               lambda: B.attend(torch.empty((1 << 8, 2), dtype=BF, device="cuda").expand(1, 1, 1 << 8, 2), torch.empty((1, 1, 5, 2), dtype=BF, device="cuda"),
