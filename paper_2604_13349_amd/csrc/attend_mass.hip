@@ -105,28 +105,54 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)sm;
   const uint16_t* Q = (const uint16_t*)a.Q + (size_t)s * a.qs + (size_t)h * a.g * a.qh;
   const float* head_lse = lse + ((size_t)s * a.H + h) * a.g * a.T;
-  // 64 rows from r0 on to LDS (those behind the range repeat its last one), and of the lane's two its normaliser and query
+  // A thread's rows of a step: LOADS whose pieces it loads, and two whose normaliser and query its lane needs.  From step to step they move by 64 rows, that is
+  // by `dt` queries and `dg` query heads, with a carry: additions, where the row's number would have to be divided and multiplied anew.
+  const int dt = MT_ROWS / a.g, dg = MT_ROWS % a.g;
+  const long move = dt * a.qt + dg * a.qh, carry = a.qt - a.g * a.qh;
+  const int move_lse = dt + dg * a.T, carry_lse = 1 - a.g * a.T;
+  const AttendStep start = attend_step(a, first);
+  const uint16_t* piece[LOADS];
+  int piece_gi[LOADS], row_gi[2], row_t[2], row_lse[2];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int row = i * (MT_THREADS / PIECES) + (int)threadIdx.x / PIECES, place = threadIdx.x % PIECES;
+    const AttendRow w = attend_row(a, start, s, row);
+    piece_gi[i] = w.gi;
+    piece[i] = Q + (long)w.gi * a.qh + (long)w.t * a.qt + 8 * (place ^ (D == 128 ? row & 15 : (row >> 1) & 7));
+  }
+#pragma unroll
+  for (int qb = 0; qb < 2; ++qb) {
+    const AttendRow w = attend_row(a, start, s, 32 * qb + (lane & 31));
+    row_gi[qb] = w.gi; row_t[qb] = w.t; row_lse[qb] = w.gi * a.T + w.t;
+  }
+  const uint16_t* const any = Q + (long)start.gi * a.qh + (long)start.t * a.qt;          // a row of the range, in the place of those behind it
+  // The step's rows from r0 on to LDS, and of the lane's two the normaliser and the query; then on to the next step's.
   struct Rows { float lse[2]; int t[2]; };
   const auto fill = [&](Rows& x, const int buf, const int r0) {
-    const AttendStep at = attend_step(a, r0);
-    const int most = behind - 1 - r0;
     const void* from[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int row = i * (MT_THREADS / PIECES) + (int)threadIdx.x / PIECES, place = threadIdx.x % PIECES;
-      const AttendRow w = attend_row(a, at, s, min(row, most));
-      from[i] = Q + (size_t)w.gi * a.qh + (size_t)w.t * a.qt + 8 * (place ^ (D == 128 ? row & 15 : (row >> 1) & 7));
+      const int row = i * (MT_THREADS / PIECES) + (int)threadIdx.x / PIECES;
+      from[i] = r0 + row < behind ? piece[i] : any;
+      piece_gi[i] += dg;
+      piece[i] += move;
+      if (piece_gi[i] >= a.g) { piece_gi[i] -= a.g; piece[i] += carry; }
     }
     load_to_lds(lds + buf * BYTES + wave * 1024, from);
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-      const AttendRow w = attend_row(a, at, s, min(32 * qb + (lane & 31), most));
-      x.lse[qb] = head_lse[(size_t)w.gi * a.T + w.t];
-      x.t[qb] = w.t;
+      const bool there = r0 + 32 * qb + (lane & 31) < behind;
+      x.lse[qb] = head_lse[there ? row_lse[qb] : 0];
+      x.t[qb] = row_t[qb];
+      row_gi[qb] += dg; row_t[qb] += dt; row_lse[qb] += move_lse;
+      if (row_gi[qb] >= a.g) { row_gi[qb] -= a.g; row_t[qb] += 1; row_lse[qb] += carry_lse; }
     }
   };
   Rows now, next = {};
   fill(next, 0, first);
+  // queries of the step's first and last row
+  int q0 = start.t, g0 = start.gi;
+  const int q_last = (behind - 1) / a.g;
   TileFrag kf[2][KK];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
@@ -142,7 +168,9 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
     wait_loads<0>();
     __syncthreads();                                   // the rows are there, and nobody reads the other ones any more
     if (r0 + MT_ROWS < behind) fill(next, buf ^ 1, r0 + MT_ROWS);
-    const int qmin = p0 + r0 / a.g, qmax = p0 + (min(r0 + MT_ROWS, behind) - 1) / a.g;
+    const int qmin = p0 + q0, qmax = p0 + min(q_last, q0 + (int)(((uint32_t)(g0 + MT_ROWS - 1) * a.g_inv) >> 23));
+    g0 += dg; q0 += dt;
+    if (g0 >= a.g) { g0 -= a.g; q0 += 1; }
     // none of the rows sees a key of the wave
     if (base >= n || (k.causal && (base > qmax || (k.window > 0 && base + 63 <= qmin - k.window && base >= sink)))) continue;
     const bool cut = r0 + MT_ROWS > behind || attend_cut(k, all, sink, qmin, qmax, base, 64);
