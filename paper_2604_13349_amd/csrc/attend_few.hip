@@ -10,6 +10,12 @@
 // most tiles need no exchange between lanes.
 // bf16: P is split into two bf16 parts, each with its own product, so that it keeps 16 bits; the matrix pipe has the room where the caches' bytes bound
 // the kernel.  fp32: all products by v_mfma_f32_16x16x4_f32.
+//
+// Four waves of 16 rows each a workgroup.  Long caches are bound by their bytes: 16 x 8 heads of 8192 to 32768 rows 246 us, 5.4 TB/s read (a large copy moves
+// 4.9), 48 x 8 heads of 1044 visible rows 37 us, 5.4; short ones by the launch and one chain of loads: 8 heads of 100 to 340 rows 8 us.  Eight waves a
+// workgroup: 5 to 20 % slower but for few long heads (8 of 32000 rows 35 us for 38).  Loads one tile ahead: the same times.  With the logits kept (32 x 8 heads
+// of 1000 to 4096 rows) 75 us for 60 without, where a second pass over the keys takes 58.  fp32, 3 x 2 heads, 333 queries of 2: 12 us, the chain of
+// products of a wave (32 rows a workgroup: 21 us).
 #include "attend_few.hpp"
 
 namespace obf {
@@ -26,7 +32,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_few(const AttendArgs a) {
 
 // Joins the ranges of a query row, O = sum_i 2^(lse_i - lse) O_i, and turns the logits of the own keys into weights, mass_j += sum_r 2^(x_rj - lse_r).
 // GROUPS lanes share a row's ranges and a lane has four channels, so that the loads of many ranges are in flight; bound by the partial results' bytes, or
-// by its launch.  Workgroups behind those of the rows take 32 tiles of keys of a set each, for which they join the normalisers of its few rows themselves.
+// by its launch (2048 rows of 17 ranges 6.6 us, 512 of four 5.6).  Workgroups behind those of the rows take 32 tiles of keys of a set each, for which they join the normalisers of its few rows themselves.
 constexpr int JN_THREADS = 256, JN_TILES = 32;
 
 template <typename ET, int D, int GROUPS>

@@ -70,7 +70,8 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
 // 64 at a time, loaded straight to it while the present ones' weights are taken (operands read from memory row by row cost a cache line per lane and load).
 // The rows are cut into ranges of ms.per steps, so that a head's early keys, which many queries see, take no longer than its late ones; the ranges' sums are
 // added in their order by k_attend_mass_add.
-// Bound by the vector work, a multiply-add, an exponential and an addition per weight, beside which the products of head_dim 128 take two thirds.
+// Two samples of 40 heads and 2048 queries: 103 us; the vector work (a multiply-add, an exponential and an addition per weight) takes half of the cycles, the
+// products a fifth beside it, the last workgroups a quarter.  Loads three steps ahead, both keys' products before their weights: no faster.
 constexpr int MT_WAVES = 4, MT_THREADS = MT_WAVES * 64, MT_KEYS = MT_WAVES * 64, MT_ROWS = 64;
 
 // query rows r0 .. r1 - 1 that see a key of the 256 from base on
