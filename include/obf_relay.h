@@ -354,8 +354,8 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
  *   mass      float, one per cache row with the row numbers of K: accumulated attention weight
  * Logits are q . k / sqrt(head_dim), Q and K as given.  Of a head of n rows query t stands at position p = n - n_queries + t and
  * sees the rows j < n with, if causal, j <= p and, if window > 0 (causal only), j > p - window or j < sink.  A query that sees
- * nothing gets O = 0 and lse = -inf.  What a query does not see never reaches its result, not-a-number and infinities included;
- * rows at and behind a head's length are not read.
+ * nothing gets O = 0 and lse = -inf.  What a query does not see never reaches its result, not-a-number and infinities included
+ * (what it sees does); rows at and behind a head's length are not read.
  * Sums and softmax statistics are single precision; O is rounded once to dtype.  With dtype OBF_BF16 the softmax weights enter
  * the product with V as two bf16 parts, or as one where n_queries * group (over all samples, for a message) is above 32.
  * Limits: head_dim 64 or 128; group <= 128; n_queries <= 2^20; strides of rows <= 2^24; n_samples*n_kv_heads <= 65535; at most
@@ -380,8 +380,9 @@ typedef struct {
   int64_t o_stride[3];
 } obf_attend_t;
 
-/* Bytes of workspace of obf_attend and obf_attend_mass (prefix_stride 0) or obf_attend_shared; 0 if the call is not supported.  Host function. */
-size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride);
+/* Bytes of workspace of obf_attend (prefix_stride 0) or obf_attend_shared; with_mass: of obf_attend with mass, which also serves
+ * obf_attend_mass.  0 if the call is not supported.  Host function. */
+size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride, int32_t with_mass);
 
 /* Attention of the queries over their own caches.  mass (nullable): the weight every visible row receives, summed over the
  * head's group of query heads and the queries, is added to mass[row]; what it adds is the same from call to call. */

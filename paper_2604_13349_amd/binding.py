@@ -125,7 +125,7 @@ def load_library():
     lib.obf_append_message.argtypes = [i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, i32, vp]
     ap = C.POINTER(_Attend)
     lib.obf_attend_workspace_bytes.restype = sz
-    lib.obf_attend_workspace_bytes.argtypes = [ap, i32]
+    lib.obf_attend_workspace_bytes.argtypes = [ap, i32, i32]
     lib.obf_attend.restype = C.c_int
     lib.obf_attend.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.obf_attend_shared.restype = C.c_int
@@ -558,7 +558,7 @@ def _attend_plan(Q, K, V, O, lse, mass, kv_len, sink_len, prefix_K, prefix_V, pr
         _want("prefix_len", prefix_len, (H,), torch.int32)
         front = prefix_K[0][1]
     lib = load_library()
-    need = int(lib.obf_attend_workspace_bytes(C.byref(c), front))
+    need = int(lib.obf_attend_workspace_bytes(C.byref(c), front, int(mass is not None)))
     if need == 0:
         raise ObfError(2, lib.obf_last_error().decode())
     return c, need, front, copy_lens
@@ -632,7 +632,7 @@ def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sin
     c, need, _, copy_lens = _attend_plan(_meta(Q), _meta(K), None, None, _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), None, None, None, bool(causal),
                                          _int("window", window), _int("sink", sink))
     with _on(Q.device) as stream:
-        if ws is None or ws.numel() < need:
+        if ws is None or ws.numel() < need or ws.device != Q.device:
             ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
         if copy_lens:
             kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))

@@ -64,7 +64,7 @@ struct AttendPlan {
   size_t part_O, part_lse, lse, mass, logits, total;
 };
 
-static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
+static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride, bool with_mass) {
   AttendPlan p;
   AttendArgs& a = p.a;
   a = AttendArgs();
@@ -124,16 +124,17 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride) {
   p.part_lse = at;
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
   p.lse = at;
-  at += ((size_t)a.rows * sizeof(float) + 255) & ~(size_t)255;
+  if (with_mass) at += ((size_t)a.rows * sizeof(float) + 255) & ~(size_t)255;
   p.ms = plan_attend_mass(a, c->dtype);
   p.mass = at;
-  if (p.ms.nsplit > 1) at += ((size_t)p.ms.nsplit * a.S * a.H * c->token_stride * sizeof(float) + 255) & ~(size_t)255;
+  if (with_mass && p.ms.nsplit > 1) at += ((size_t)p.ms.nsplit * a.S * a.H * c->token_stride * sizeof(float) + 255) & ~(size_t)255;
   // Few query rows: the logits are kept and weighted at the end, 4 bytes a row and key written and read beside the 2 d or 4 d of a key, where a second pass
   // would read the keys again.
   const bool keep = a.n_keys == 1 && own_rows <= p.tile_rows[0] && own_rows <= kAttendFewRows;
   p.logits = at;
-  a.logit_tiles = c->token_stride / 32 + 2;        // (the last tiles of a span's two parts are cut off)
-  if (keep) at += (size_t)a.rows * a.logit_tiles * 32 * sizeof(float);
+  a.logit_tiles = (c->token_stride + 31) / 32;
+  if (with_mass && keep) at += (size_t)a.rows * a.logit_tiles * 32 * sizeof(float);
+  if (at == 0) at = 256;
   p.total = at;
   p.keep_logits = keep;
   return p;
@@ -159,7 +160,7 @@ static obf_status_t check_apart(const void* O, const void* Q, const void* K, con
 static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
                                int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
                                const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, hipStream_t st) {
-  AttendPlan p = plan_attend(c, prefix_stride);
+  AttendPlan p = plan_attend(c, prefix_stride, mass != nullptr);
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   AttendArgs& a = p.a;
   char* base = (char*)ws;
@@ -186,10 +187,10 @@ using namespace obf;
 
 extern "C" {
 
-size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride) {
+size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride, int32_t with_mass) {
   if (check_attend(call) != OBF_OK) return 0;
   if (prefix_stride < 0 || prefix_stride > kAttendMaxStride) { set_error("attend: prefix_stride outside [0, %d]", kAttendMaxStride); return 0; }
-  return plan_attend(call, prefix_stride).total;
+  return plan_attend(call, prefix_stride, with_mass != 0).total;
 }
 
 obf_status_t obf_attend(const obf_attend_t* call, const void* Q, const void* K, const void* V, const int32_t* kv_len, const int32_t* sink_len,
@@ -220,7 +221,7 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
                              const int32_t* sink_len, float* mass, void* ws, size_t ws_bytes, void* stream) {
   OBF_TRY(check_attend(call));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_NONNULL(lse); OBF_NONNULL(mass);
-  AttendPlan p = plan_attend(call, 0);
+  AttendPlan p = plan_attend(call, 0, true);
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   p.a.Q = Q;
   p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(JN_THREADS) void k_attend_join(const AttendArgs a, 
     }
   }
   if (!valid) return;
-  const bool any = top != -INFINITY;
+  const bool any = sum != 0.f;                         // (also where it is no number)
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = any ? v[i] / sum : 0.f;
   const int t = (int)(row % a.T), hq = (int)(row / a.T % ((size_t)a.H * a.g)), s = (int)(row / a.T / ((size_t)a.H * a.g));

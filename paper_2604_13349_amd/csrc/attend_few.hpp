@@ -320,16 +320,17 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const AttendKeys
       const float4 x = *(const float4*)&sm.o[w][r][c];
       v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
     }
-    const float inv = top > -INFINITY ? 1.f / sum : 0.f;
+    // (a sum of 0: no key is visible; a sum that is no number: some visible logit is none, whatever `top` is)
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = top > -INFINITY ? v[i] * inv : 0.f;
-    const float lse2 = top > -INFINITY ? top + attend_log2(sum) : -INFINITY;
+    for (int i = 0; i < 4; ++i) v[i] *= inv;
+    const float lse2 = sum != 0.f ? top + attend_log2(sum) : -INFINITY;
     const AttendRow w = attend_row(a, k, ks, row0 + r);
     const size_t number = attend_row_number(a, h, w);
     if (joined) {
       const size_t at = (size_t)(k.split0 + split) * a.rows + number;
       if (c == 0) a.part_lse[at] = lse2;
-      if (top > -INFINITY) *(float4*)(a.part_O + at * D + c) = make_float4(v[0], v[1], v[2], v[3]);   // (nobody reads the others)
+      if (sum != 0.f) *(float4*)(a.part_O + at * D + c) = make_float4(v[0], v[1], v[2], v[3]);   // (nobody reads the others)
     } else {
       if (c == 0 && a.lse) a.lse[number] = lse2 * 0.69314718055994531f;
       store4((ET*)a.O + (size_t)w.s * a.os + (size_t)(h * a.g + w.gi) * a.oh + (size_t)w.t * a.ot + c, v);

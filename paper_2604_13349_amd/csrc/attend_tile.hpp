@@ -237,7 +237,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
 
   l += __shfl_xor(l, 32);
   if (r >= set_rows) return;
-  const bool any = m > -INFINITY;
+  const bool any = l != 0.f;                           // some key is visible (or some visible logit no number)
   const float inv = any ? 1.f / l : 0.f;
   const float lse2 = any ? m + attend_log2(l) : -INFINITY;
   const size_t number = attend_row_number(a, h, w);

@@ -50,7 +50,7 @@ def test_refused_descriptors(lib, change, status, word):
     c = _call(**change)
     rc, msg = _attend(lib, c)
     assert rc == status and word in msg
-    assert lib.obf_attend_workspace_bytes(C.byref(c), 0) == 0
+    assert lib.obf_attend_workspace_bytes(C.byref(c), 0, 1) == 0
     assert lib.obf_attend_shared(C.byref(c), FAKE, FAKE, FAKE, None, 10, 10, FAKE, FAKE, None, None, FAKE, None, FAKE, 1 << 40, None) == status
     assert lib.obf_attend_mass(C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE, FAKE, 1 << 40, None) == status
 
@@ -66,13 +66,14 @@ def test_refused_pointers_and_workspaces(lib):
     assert _attend(lib, c, O=FAKE)[0] == 1
     assert _attend(lib, c, ws=None)[0] == 1
     assert _attend(lib, c, ws=C.c_void_p((1 << 20) + 16))[0] == 1
-    need = lib.obf_attend_workspace_bytes(C.byref(c), 0)
-    assert need > 0 and _attend(lib, c, ws_bytes=need - 1)[0] == 3
-    assert lib.obf_attend_workspace_bytes(C.byref(c), 4000) > need
-    assert lib.obf_attend_workspace_bytes(C.byref(c), -1) == 0
+    less, need = (lib.obf_attend_workspace_bytes(C.byref(c), 0, m) for m in (0, 1))
+    assert 0 < less < need and _attend(lib, c, ws_bytes=less - 1)[0] == 3
+    assert lib.obf_attend(C.byref(c), FAKE, FAKE, FAKE, None, None, FAKE_O, None, FAKE, FAKE, need - 1, None) == 3
+    assert lib.obf_attend_workspace_bytes(C.byref(c), 4000, 0) > less
+    assert lib.obf_attend_workspace_bytes(C.byref(c), -1, 0) == 0
 
     def shared(pk=FAKE, pv=FAKE, n=10, stride=10):
-        return lib.obf_attend_shared(C.byref(c), FAKE, pk, pv, None, n, stride, FAKE, FAKE, None, None, FAKE_O, None, FAKE, need, None)
+        return lib.obf_attend_shared(C.byref(c), FAKE, pk, pv, None, n, stride, FAKE, FAKE, None, None, FAKE_O, None, FAKE, less, None)
 
     assert shared(pk=None) == 1 and shared(pv=None) == 1 and shared(n=11) == 1 and shared(n=-1) == 1 and shared(stride=0, n=0) == 1
     assert shared(n=1, stride=(1 << 24) + 1) == 2

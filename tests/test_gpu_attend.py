@@ -48,9 +48,14 @@ def _check(name, got, want, tol):
     assert not bad.any(), f"{name}: {int(bad.sum())} values off, worst {((got - want).abs() / tol.clamp(min=1e-300))[bad].max():.3g} times the bound"
 
 
+def _p_eps(dtype, rows):
+    """How the weights enter the product with V: as they are, as two bf16 parts (half a step of half a step), as one."""
+    return 0.0 if dtype == F32 else 2.0 ** -16 if rows <= 32 else 2.0 ** -8
+
+
 def _attend_and_check(Q, K, V, kv_len, mass=True, spoil=math.nan, **kw):
     B = _b()
-    O, lse, add, tO, tl, tm = R.attend(Q, K, V, kv_len, **kw)
+    O, lse, add, tO, tl, tm = R.attend(Q, K, V, kv_len, p_eps=_p_eps(Q.dtype, Q.shape[1] // K.shape[1] * Q.shape[2]), **kw)
     Kd, Vd = _spoil(K, kv_len, spoil).cuda(), _spoil(V, kv_len, spoil).cuda()
     call = dict(kw)
     if kw.get("sink_len") is not None:
@@ -148,11 +153,38 @@ def test_hidden_rows_of_any_value_do_not_reach_a_query(dtype, T, window, value):
         clean = torch.tensor([not set(where) & set(R.visible(n, T, t, True, window, 2)) for t in range(T)])
         if not clean.any():
             continue
-        O, lse, _, tO, tl, _ = R.attend(Q, Kz, Vz, kv_len, **kw)
+        O, lse, _, tO, tl, _ = R.attend(Q, Kz, Vz, kv_len, p_eps=_p_eps(dtype, 2 * T), **kw)
         o = B.attend(Q.cuda(), Kb.cuda(), Vb.cuda(), kv_len=kv_len.cuda(), **kw)
         _check("O", o["O"][:, :, clean], O[:, :, clean], tO[:, :, clean])
         _check("lse", o["lse"][:, :, clean], lse[:, :, clean], tl[:, :, clean])
         assert not torch.isfinite(o["O"][:, :, ~clean].float()).all() if (~clean).any() else True
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,rows", [(1, 90), (1, 9000), (40, 90), (40, 9000)])
+def test_visible_logits_that_are_no_numbers_reach_the_result(dtype, T, rows):
+    """A query, or all visible keys of a head, without numbers: no number comes out, not the zeros of a query that sees nothing; the other rows are as before."""
+    B = _b()
+    Q, K, V = _make(24, dtype, 128, 1, 2, 2, T, rows)
+    # (the other rows' bits may differ: a wave's rows take over larger references together, and a row without numbers never asks for one)
+    O, lse, _, tO, tl, _ = R.attend(Q, K, V, torch.full((1, 2), rows), p_eps=_p_eps(dtype, 2 * T))
+    Q, K, V = Q.cuda(), K.cuda(), V.cuda()
+    bad = Q.clone()
+    bad[0, 1, T - 1] = math.nan
+    mass = torch.zeros((1, 2, rows), device="cuda")
+    o = B.attend(bad, K, V, mass=mass)
+    assert torch.isnan(o["O"][0, 1, T - 1]).all() and torch.isnan(o["lse"][0, 1, T - 1])
+    assert torch.isnan(mass[0, 0]).all() and torch.isfinite(mass[0, 1]).all()
+    keep = torch.ones((4, T), dtype=torch.bool)
+    keep[1, T - 1] = False
+    _check("O", o["O"][0].cpu()[keep], O[0][keep], tO[0][keep])
+    _check("lse", o["lse"][0].cpu()[keep], lse[0][keep], tl[0][keep])
+    K[0, 0] = math.nan
+    o = B.attend(Q, K, V)
+    assert torch.isnan(o["O"][0, :2]).all() and torch.isnan(o["lse"][0, :2]).all()
+    _check("O", o["O"][0, 2:], O[0, 2:], tO[0, 2:])
+    o = B.attend_shared(Q, K[0, :, :70].contiguous(), V[0, :, :70].contiguous(), K[:, :, :50].contiguous(), V[:, :, :50].contiguous())
+    assert torch.isnan(o["O"][0, :2]).all() and torch.isfinite(o["O"][0, 2:].float()).all()
 
 
 @pytest.mark.parametrize("T", [1, 60])
@@ -207,7 +239,7 @@ def test_attend_shared(case):
     _, PK, PV = _make(22, dtype, d, 1, H, g, T, P)
     kv_len, plen = _lens(3, S, H, lo, hi), _lens(4, 1, H, plo, phi)
     kw = dict(causal=True, window=window, sink=2)
-    O, lse, add, tO, tl, tm = R.attend(Q, K, V, kv_len, prefix=(PK[0], PV[0], plen[0]), **kw)
+    O, lse, add, tO, tl, tm = R.attend(Q, K, V, kv_len, prefix=(PK[0], PV[0], plen[0]), p_eps=_p_eps(dtype, S * T * g), **kw)
     Kd, Vd = _spoil(K, kv_len, math.nan).cuda(), _spoil(V, kv_len, math.nan).cuda()
     PKd, PVd = _spoil(PK, plen, math.nan).cuda()[0], _spoil(PV, plen, math.nan).cuda()[0]
     o = B.attend_shared(Q.cuda(), PKd, PVd, Kd, Vd, prefix_len=plen[0].cuda(), kv_len=kv_len.cuda(), **kw)
