@@ -86,11 +86,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
   for (int kk = 0; kk < KK; ++kk) q[kk].u = *(const TilePiece*)(qrow + 16 * kk + 8 * half);
 
   f32x16 o[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m, l;
+  // A product takes 0 times a hidden value: one that is not finite makes a row's O no number, and the pass is repeated with care for those.
+  int careful = 0;
 
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)sm;
   // lane's places
@@ -117,10 +115,19 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
     }
     const AttendView view = attend_view(kt, st, sink, pos, base + 4 * half);
     if (CUT) {
+      // (attend_sees in two steps, the second only where the window begins inside the tile)
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[b][e] = attend_sees(view, 32 * b + 8 * (e >> 2) + (e & 3)) ? x[b][e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) x[b][e] = 32 * b + 8 * (e >> 2) + (e & 3) <= view.hi ? x[b][e] : -INFINITY;
+      if (kt.causal && kt.window > 0 && base <= pmax - kt.window - st.skip)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = 32 * b + 8 * (e >> 2) + (e & 3);
+            x[b][e] = (j > view.lo) | (j < view.first) ? x[b][e] : -INFINITY;
+          }
     }
     float top[4];
 #pragma unroll
@@ -149,8 +156,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
       s0 += x[0][e]; s1 += x[1][e];
     }
     l += s0 + s1;
-    if (CUT && kt.causal) {
-      // A product takes 0 times a hidden value; where that value is not finite, the tile's terms are added one by one instead.
+    if (CUT && careful && kt.causal) {
+      // where a value is not finite, the tile's terms are added one by one
       bool bad = false;
       for (int e = lane; e < TILE / 16; e += 64) {
         const TilePiece y = *(const TilePiece*)(tv + e * 16);
@@ -209,30 +216,45 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
     tile_fill<D, false>(lds + buf * TILE, from_k, from, v, wave, lane);
     tile_fill<D, true>(lds + (2 + buf) * TILE, from_v, from, v, wave, lane);
   };
-  int i = first, buf = 0;
+  int i, buf;
   // Tile i is there, nobody reads the other one any more: the loads of tile i + 1.
   const auto begin = [&]() {
     wait_loads<0>();
     __syncthreads();
     if (i + 1 < behind) fill(buf ^ 1, i + 1);
   };
-  if (first < behind) fill(0, first);
-  // (two loops, so that the common one has the registers to itself)
-  while (i < behind) {
-    const int whole = min(behind, i < front_whole ? front_whole : i >= whole0 ? whole1 : i);
-    for (; i < whole; ++i, buf ^= 1) {
-      begin();
-      take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, k, span, 0);
+  for (;; careful = 1) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[db][e] = 0.f;
+    m = -INFINITY; l = 0.f;
+    i = first; buf = 0;
+    if (first < behind) fill(0, first);
+    // (two loops, so that the common one has the registers to itself)
+    while (i < behind) {
+      const int whole = min(behind, i < front_whole ? front_whole : i >= whole0 ? whole1 : i);
+      for (; i < whole; ++i, buf ^= 1) {
+        begin();
+        take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, k, span, 0);
+      }
+      const int cut = min(behind, i < front_tiles ? front_tiles : i < whole0 ? whole0 : behind);
+      for (; i < cut; ++i, buf ^= 1) {
+        AttendKeys kt = k;
+        AttendSpan st = span;
+        int v = (i - front_tiles) * AT_KEYS;
+        if (i < front_tiles) { kt.causal = 0; kt.window = 0; st = front_span; v = i * AT_KEYS; }
+        begin();
+        take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, kt, st, v);
+      }
     }
-    const int cut = min(behind, i < front_tiles ? front_tiles : i < whole0 ? whole0 : behind);
-    for (; i < cut; ++i, buf ^= 1) {
-      AttendKeys kt = k;
-      AttendSpan st = span;
-      int v = (i - front_tiles) * AT_KEYS;
-      if (i < front_tiles) { kt.causal = 0; kt.window = 0; st = front_span; v = i * AT_KEYS; }
-      begin();
-      take(TileCut<true>(), sm + buf * TILE, sm + (2 + buf) * TILE, kt, st, v);
-    }
+    if (careful || !k.causal) break;
+    bool bad = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) bad |= !(fabsf(o[db][e]) < INFINITY);
+    if (!__syncthreads_or(bad)) break;                 // (also: nobody reads the tiles any more)
   }
 
   l += __shfl_xor(l, 32);
