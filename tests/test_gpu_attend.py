@@ -325,6 +325,22 @@ def test_evict_flags_bad_lengths_and_heads_without_room():
     assert (o["idx"][[0, 1, 2, 4]] == -1).all() and o["idx"][3].tolist() == R.evict(mass[3], 50, 10, 2, 3) + [-1, -1]
 
 
+def test_evict_takes_the_largest_budgets():
+    """budget, recent and sink of 2^31 - 1: their sums pass 32 bits, and every row is kept."""
+    B = _b()
+    _, K, V = _make(3, BF, 64, 1, 4, 1, 1, 700)
+    mass = torch.rand((4, 700), generator=torch.Generator().manual_seed(4))
+    kv_len = torch.tensor([700, 0, 1, 333], dtype=torch.int32)
+    most = 2**31 - 1
+    for budget, recent, sink in ((most, 0, 9), (most, most, 0), (most, 5, most), (0, 0, most)):
+        o = B.evict(K[0].cuda(), V[0].cuda(), mass.cuda(), budget, kv_len=kv_len.cuda(), recent=recent, sink=sink, out_stride=700)
+        assert o["len_out"].tolist() == kv_len.tolist(), (budget, recent, sink)
+        for h, n in enumerate(kv_len.tolist()):
+            assert o["idx"][h].tolist() == list(range(n)) + [-1] * (700 - n)
+            assert torch.equal(o["K_out"][h, :n].cpu(), K[0, h, :n]) and torch.equal(o["V_out"][h, :n].cpu(), V[0, h, :n])
+            assert torch.equal(o["mass_out"][h, :n].cpu(), mass[h, :n])
+
+
 def test_repeated_calls_and_a_used_workspace_change_no_bit():
     B = _b()
     Q, K, V = (x.cuda() for x in _make(15, BF, 128, 2, 2, 4, 1, 2000))
