@@ -69,8 +69,10 @@ __global__ __launch_bounds__(JN_THREADS) void k_attend_join(const AttendArgs a, 
       if (a.ranges > 1) {
         float top = -INFINITY, sum = 0.f;
         for (int i = 0; i < a.ranges; ++i) top = fmaxf(top, a.part_lse[(size_t)i * a.rows + row]);
-        for (int i = 0; i < a.ranges; ++i) { const float x = a.part_lse[(size_t)i * a.rows + row]; if (x > -INFINITY) sum += attend_exp2(x - top); }
-        ref = top > -INFINITY ? top + attend_log2(sum) : -INFINITY;
+        // (as in the join of O: a part that is no number makes the normaliser none, and with it the weights of all that the row sees)
+        const float base = top > -INFINITY ? top : 0.f;
+        for (int i = 0; i < a.ranges; ++i) { const float x = a.part_lse[(size_t)i * a.rows + row]; if (x != -INFINITY) sum += attend_exp2(x - base); }
+        ref = sum != 0.f ? base + attend_log2(sum) : -INFINITY;
       } else {
         ref = a.lse[row] * 1.44269504088896341f;
       }

@@ -546,3 +546,21 @@ def test_caches_whose_offsets_pass_32_bits(T):
         worth[:4] = worth[at - 50:] = math.inf
         keep = torch.sort(torch.sort(worth, descending=True, stable=True).indices[:304]).values
         assert torch.equal(e["idx"][0, h].long(), keep) and torch.equal(e["K_out"][0, h], K[0, h, keep])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,rows,where", [(1, 90, [50]), (1, 9000, [5000]), (1, 9000, range(0, 9000, 100)), (3, 9000, [4000]), (40, 300, [100])])
+def test_one_visible_key_without_numbers_takes_every_weight_of_its_rows(dtype, T, rows, where):
+    """Also where the keys are cut into ranges and only some, or all, of those hold such a key: the weights come from the row's whole normaliser."""
+    B = _b()
+    Q, K, V = (x.cuda() for x in _make(25, dtype, 128, 1, 2, 2, T, rows))
+    want = torch.zeros((1, 2, rows), device="cuda")
+    B.attend(Q, K, V, mass=want)
+    K[0, 0, list(where)] = math.nan
+    mass = torch.zeros((1, 2, rows), device="cuda")
+    o = B.attend(Q, K, V, mass=mass)
+    assert torch.isnan(o["O"][0, :2]).all() and torch.isnan(o["lse"][0, :2]).all()
+    assert torch.isnan(mass[0, 0]).all() and torch.equal(mass[0, 1], want[0, 1])
+    again = torch.zeros((1, 2, rows), device="cuda")
+    B.attend_mass(Q, K, o["lse"], again)
+    assert torch.isnan(again[0, 0]).all() and torch.isfinite(again[0, 1]).all()
