@@ -174,7 +174,8 @@ __global__ __launch_bounds__(MT_THREADS, 2) void k_attend_mass_tile(const Attend
     if (g0 >= a.g) { g0 -= a.g; q0 += 1; }
     // none of the rows sees a key of the wave
     if (base >= n || (k.causal && (base > qmax || (k.window > 0 && base + 63 <= qmin - k.window && base >= sink)))) continue;
-    const bool cut = r0 + MT_ROWS > behind || attend_cut(k, all, sink, qmin, qmax, base, 64);
+    // (a row whose lse says that it does not count is masked too: its query may hold anything)
+    const bool cut = r0 + MT_ROWS > behind || attend_cut(k, all, sink, qmin, qmax, base, 64) || __any(fminf(now.lse[0], now.lse[1]) == -INFINITY);
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
       TileFrag q[KK];

@@ -564,3 +564,24 @@ def test_one_visible_key_without_numbers_takes_every_weight_of_its_rows(dtype, T
     again = torch.zeros((1, 2, rows), device="cuda")
     B.attend_mass(Q, K, o["lse"], again)
     assert torch.isnan(again[0, 0]).all() and torch.isfinite(again[0, 1]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [2, 60])
+def test_queries_that_do_not_count_may_hold_anything(dtype, T):
+    """A query whose lse the caller set to -inf (a padded one) adds nothing, whatever it holds."""
+    B = _b()
+    n = T + 200
+    Q, K, V = _make(26, dtype, 128, 1, 2, 2, T, n)
+    kv_len = torch.full((1, 2), n)
+    _, lse, add, _, _, tol = R.attend(Q, K, V, kv_len)
+    o = B.attend(Q.cuda(), K.cuda(), V.cuda())
+    off = [1] if T == 2 else [3, 17, 18, 59]
+    for t in off:
+        one = torch.full((1, 2), n - T + t + 1)
+        add = add - R.attend(Q[:, :, t:t + 1], K, V, one)[2]
+    Q[:, :, off] = math.nan
+    o["lse"][:, :, off] = -math.inf
+    mass = torch.zeros((1, 2, n), device="cuda")
+    B.attend_mass(Q.cuda(), K.cuda(), o["lse"], mass)
+    _check("mass", mass, add, tol + 2 * R.U * add)
