@@ -238,7 +238,8 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
         begin();
         take(TileCut<false>(), sm + buf * TILE, sm + (2 + buf) * TILE, k, span, 0);
       }
-      const int cut = min(behind, i < front_tiles ? front_tiles : i < whole0 ? whole0 : behind);
+      // (none with masks where the message's whole tiles end at the first whole one of the own rows)
+      const int cut = min(behind, i < front_tiles ? front_tiles : i < whole0 ? whole0 : i < whole1 ? i : behind);
       for (; i < cut; ++i, buf ^= 1) {
         AttendKeys kt = k;
         AttendSpan st = span;

@@ -585,3 +585,20 @@ def test_queries_that_do_not_count_may_hold_anything(dtype, T):
     mass = torch.zeros((1, 2, n), device="cuda")
     B.attend_mass(Q.cuda(), K.cuda(), o["lse"], mass)
     _check("mass", mass, add, tol + 2 * R.U * add)
+
+
+@pytest.mark.parametrize("P", [63, 64, 128, 1024])
+@pytest.mark.parametrize("window", [0, 90])
+def test_messages_of_whole_tiles_before_a_prompt(P, window):
+    """Tiles without masks of the message, then at once those of the own rows."""
+    B = _b()
+    S, H, g, T, rows, d = 2, 8, 2, 40, 400, 128
+    Q, K, V = _make(30, BF, d, S, H, g, T, rows)
+    _, PK, PV = _make(31, BF, d, 1, H, g, 1, P)
+    kv_len = _lens(12, S, H, 300, rows)
+    plen = torch.full((H,), P, dtype=torch.int32)
+    kw = dict(window=window, sink=2)
+    O, lse, _, tO, tl, _ = R.attend(Q, K, V, kv_len, prefix=(PK[0], PV[0], plen), **kw)
+    o = B.attend_shared(Q.cuda(), PK[0].cuda(), PV[0].cuda(), _spoil(K, kv_len, math.nan).cuda(), _spoil(V, kv_len, math.nan).cuda(), kv_len=kv_len.cuda(), **kw)
+    _check("lse", o["lse"], lse, tl)
+    _check("O", o["O"], O, tO)
