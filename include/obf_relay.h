@@ -349,7 +349,8 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
  *             so a layer of [n_samples][n_layers][n_kv_heads][token_stride][head_dim] is a call's cache as it lies
  *   kv_len    rows per (sample, head), DEVICE int32, entry s * len_stride + h (len_stride 0: n_kv_heads); NULL: kv_len_all in
  *             all.  A length below 0 or above token_stride (the -1 of obf_append_message) counts as a head without rows.
- *   sink_len  first rows that stay visible, laid out as kv_len (the inherited message); NULL: `sink` in all
+ *   sink_len  first rows that stay visible, laid out as kv_len (the inherited message); NULL: `sink` in all.  With sink_len, `sink`
+ *             only says about how many those are, for the launch (0: any number); results do not depend on it.
  *   lse       nullable, float [n_samples][n_kv_heads*group][n_queries]: log of the sum of exp(logit) over the visible rows
  *   mass      float, one per cache row with the row numbers of K: accumulated attention weight
  * Logits are q . k / sqrt(head_dim), Q and K as given.  Of a head of n rows query t stands at position p = n - n_queries + t and
@@ -381,7 +382,7 @@ typedef struct {
 } obf_attend_t;
 
 /* Bytes of workspace of obf_attend (prefix_stride 0) or obf_attend_shared; with_mass: of obf_attend with mass, which also serves
- * obf_attend_mass.  0 if the call is not supported.  Host function. */
+ * obf_attend_mass.  Enough with and without sink_len.  0 if the call is not supported.  Host function. */
 size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride, int32_t with_mass);
 
 /* Attention of the queries over their own caches.  mass (nullable): the weight every visible row receives, summed over the

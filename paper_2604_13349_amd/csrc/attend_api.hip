@@ -64,7 +64,8 @@ struct AttendPlan {
   size_t part_O, part_lse, lse, mass, logits, total;
 };
 
-static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride, bool with_mass) {
+// sinks_per_head: sink_len is given (or may be, where a workspace is asked for: its size is the larger one then).
+static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride, bool with_mass, bool sinks_per_head) {
   AttendPlan p;
   AttendArgs& a = p.a;
   a = AttendArgs();
@@ -105,8 +106,11 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride, bool wit
   for (int i = a.fused ? 1 : 0; i < a.n_keys; ++i) {
     AttendKeys& s = a.keys[i];
     s.row_tiles = (int)((s.row_samples * own_rows + p.tile_rows[i] - 1) / p.tile_rows[i]);
-    const long blocks = (long)s.row_tiles * s.samples * a.H, seen = s.window > 0 ? (long)s.window + s.sink + p.tile_rows[i] / a.g + 1 : s.stride;
-    const long rows = (seen < s.stride ? seen : s.stride) + (a.fused ? a.keys[0].stride : 0);     // that a tile sees, at most (but for sink_len)
+    // Rows that a tile sees, at most; first rows counted per head may be any number of them, unless `sink` says about how many (us, ranges for the window and
+    // for all rows: 8 heads of 8200 rows, window of 64, 8000 first rows, one query 73 - 17.5, 64 queries 277 - 34; 1 to 40 first rows, one query 9.4 - 13.4).
+    const bool few_seen = s.window > 0 && (s.sink > 0 || !sinks_per_head);
+    const long blocks = (long)s.row_tiles * s.samples * a.H, seen = few_seen ? (long)s.window + s.sink + p.tile_rows[i] / a.g + 1 : s.stride;
+    const long rows = (seen < s.stride ? seen : s.stride) + (a.fused ? a.keys[0].stride : 0);
     // Ranges where the sets do not fill the chip, two workgroups per compute unit (one where a message's tiles of many rows share it with the own rows' loads);
     // none for short caches, whose join would take longer (us, ranges and none: 128 sets of 590 rows 17.0 - 15.4, 256 of 1000 31 - 28, of 1500 43.3 - 39.7,
     // 252 workgroups of fp32 rows 20 - 13.5; 64 sets of 1000 15.8 - 18.6, 128 of 2000 32.4 - 34.7; 8 sets of 340 9.8 - 8.1, of 1000 11.8 - 12.6).
@@ -160,7 +164,7 @@ static obf_status_t check_apart(const void* O, const void* Q, const void* K, con
 static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
                                int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
                                const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, hipStream_t st) {
-  AttendPlan p = plan_attend(c, prefix_stride, mass != nullptr);
+  AttendPlan p = plan_attend(c, prefix_stride, mass != nullptr, sink_len != nullptr);
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   AttendArgs& a = p.a;
   char* base = (char*)ws;
@@ -190,7 +194,7 @@ extern "C" {
 size_t obf_attend_workspace_bytes(const obf_attend_t* call, int32_t prefix_stride, int32_t with_mass) {
   if (check_attend(call) != OBF_OK) return 0;
   if (prefix_stride < 0 || prefix_stride > kAttendMaxStride) { set_error("attend: prefix_stride outside [0, %d]", kAttendMaxStride); return 0; }
-  return plan_attend(call, prefix_stride, with_mass != 0).total;
+  return plan_attend(call, prefix_stride, with_mass != 0, true).total;
 }
 
 obf_status_t obf_attend(const obf_attend_t* call, const void* Q, const void* K, const void* V, const int32_t* kv_len, const int32_t* sink_len,
@@ -221,7 +225,7 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
                              const int32_t* sink_len, float* mass, void* ws, size_t ws_bytes, void* stream) {
   OBF_TRY(check_attend(call));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_NONNULL(lse); OBF_NONNULL(mass);
-  AttendPlan p = plan_attend(call, 0, true);
+  AttendPlan p = plan_attend(call, 0, true, sink_len != nullptr);
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   p.a.Q = Q;
   p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;

@@ -128,3 +128,16 @@ def test_definition_on_known_answers():
     assert O[0, 0, T - 1, 0] == pytest.approx((10 + 11 + 12 + 0) / 4) and O[0, 0, 0, 0] == pytest.approx(11)
     assert R.evict([5., 1., 9., 9., 2., 9., 0.], 7, 4, 1, 1) == [0, 2, 3, 5, 6]
     assert R.evict([5., 1., 9.], 3, 4, 1, 1) == [0, 1, 2]
+
+
+def test_first_rows_per_head_of_unknown_number_get_ranges(lib):
+    """A window beside sink_len: unless `sink` says that they are few, the launch and its workspace are planned for heads that see all their rows."""
+    sizes = {}
+    for sink in (0, 30, 8000):
+        c = _call(n_samples=1, n_kv_heads=8, token_stride=8200, kv_len_all=8200, window=64, sink=sink)
+        sizes[sink] = lib.obf_attend_workspace_bytes(C.byref(c), 0, 0)
+    assert sizes[30] < sizes[0] and sizes[8000] <= sizes[0]
+    c = _call(n_samples=1, n_kv_heads=8, token_stride=8200, kv_len_all=8200, window=64)
+    assert lib.obf_attend(C.byref(c), FAKE, FAKE, FAKE, None, FAKE, FAKE_O, None, None, FAKE, sizes[0] - 1, None) == 3
+    whole = _call(n_samples=1, n_kv_heads=8, token_stride=8200, kv_len_all=8200)
+    assert sizes[0] == lib.obf_attend_workspace_bytes(C.byref(whole), 0, 0)

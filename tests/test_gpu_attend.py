@@ -602,3 +602,14 @@ def test_messages_of_whole_tiles_before_a_prompt(P, window):
     o = B.attend_shared(Q.cuda(), PK[0].cuda(), PV[0].cuda(), _spoil(K, kv_len, math.nan).cuda(), _spoil(V, kv_len, math.nan).cuda(), kv_len=kv_len.cuda(), **kw)
     _check("lse", o["lse"], lse, tl)
     _check("O", o["O"], O, tO)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [1, 9, 40])
+def test_long_and_short_first_rows_per_head(dtype, T):
+    """An inherited message of thousands of rows behind a small window, beside heads with few first rows; what `sink` says of them changes no result but by rounding."""
+    Q, K, V = _make(32, dtype, 128, 1, 4, 2, T, 4000)
+    sink_len = torch.tensor([[3500, 0, 4000, 7]], dtype=torch.int32)
+    kv_len = torch.tensor([[4000, 3900, 3000, 60]], dtype=torch.int32)
+    for sink in (0, 8, 3500):
+        _attend_and_check(Q, K, V, kv_len, causal=True, window=64, sink=sink, sink_len=sink_len)
