@@ -358,7 +358,7 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
  * nothing gets O = 0 and lse = -inf.  What a query does not see never reaches its result, not-a-number and infinities included
  * (what it sees does; an infinity among the visible rows may make a result not-a-number); rows at and behind a head's length are not read.
  * Sums and softmax statistics are single precision; O is rounded once to dtype.  With dtype OBF_BF16 the softmax weights enter
- * the product with V as two bf16 parts, or as one where n_queries * group (over all samples, for a message) is above 32.
+ * the product with V as two bf16 parts, or as one where n_queries * group is above 32 (by the sample's own rows, also for a message).
  * Limits: head_dim 64 or 128; group <= 128; n_queries <= 2^20; strides of rows <= 2^24; n_samples*n_kv_heads <= 65535; at most
  * 2^26 query rows and 2^30 cache rows; Q, K, V, O 16-byte aligned, strides of Q and O multiples of 16 bytes.  O may not overlap an input.  Results do
  * not depend on what the workspace held, and are the same from call to call.  Two calls that may overlap in time (or two captured

@@ -8,7 +8,9 @@
 // 2^(x - m), and V^T P^T, whose operand P^T is the first product's result as it lies in its lanes; V's operand is read from LDS transposed
 // (ds_read_b64_tr_b16).  m follows the row's maximum only where that outgrows it by 2^8.
 // Pieces of 16 bytes (K) and 64 bytes (V) of a row lie in LDS permuted by the row's number, so that the operand reads use all banks.
-// P is rounded to bf16, 2^-8 of a weight at most: at this many rows the matrix pipe bounds the kernel, and the result is rounded as coarsely.
+// P is rounded to bf16, 2^-8 of a weight at most: at this many rows the matrix pipe bounds the kernel, and the result is rounded as coarsely (8192 queries: 1.7e-3
+// of the result's norm off 64 bits, where its own rounding makes 1.5e-3).  As two parts, as few rows have them: 957 us for 702, 250 for 189 (head_dim 64,
+// window), 340 for 265 (8 x 500 queries behind a message).  A sample's few rows against a message have two parts too (64 samples behind 8192 rows: 41.7 us for 40.1).
 //
 // Two workgroups share a compute unit, so that one's products run beside the other's exponentials.  32 query heads of 8192 queries over 9421 rows: 710 us,
 // 1.01 PFLOP/s (the library's largest product reaches 1.22), the matrix pipe busy half the time at a clock that its power holds at 1.7 to 1.95 GHz.  Two
@@ -28,16 +30,17 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs 
   AttendKeys k = a.keys[0];
   if (a.fused) k = a.keys[1];
   else if (block >= k.blocks) { block -= k.blocks; k = a.keys[1]; }
-  attend_tile<D>(a, k, block, sm);
+  attend_tile<D, 1>(a, k, block, sm);
 }
 
-// A message's rows against all samples' queries, and the samples' own rows against theirs, in one launch: products beside loads.
+// A message's rows against all samples' queries, and the samples' own rows against theirs, in one launch: products beside loads.  The weights of both enter V's
+// product as two parts, so that what a sample gets does not hang on the number of samples beside it.
 template <int D>
 __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile_few(const AttendArgs a) {
   constexpr int BYTES = attend_tile_bytes<D>() > (int)sizeof(FewShared<D, 1, 4>) ? attend_tile_bytes<D>() : (int)sizeof(FewShared<D, 1, 4>);
   __shared__ __attribute__((aligned(1024))) char sm[BYTES];
   const int block = blockIdx.x, tiles = a.keys[0].blocks;
-  if (block < tiles) attend_tile<D>(a, a.keys[0], block, sm);
+  if (block < tiles) attend_tile<D, 2>(a, a.keys[0], block, sm);
   else attend_few<uint16_t, D, 1, 4>(a, a.keys[1], block - tiles, false, *(FewShared<D, 1, 4>*)sm);
 }
 

@@ -54,8 +54,8 @@ __device__ __forceinline__ float tile_max(const float a, const float b) { return
 
 template <int D> constexpr int attend_tile_bytes() { return 4 * AT_KEYS * D * 2; }     // K, K, V, V
 
-// Workgroup `block` of those of one set of keys (with a.fused: the message's, then the own).
-template <int D>
+// Workgroup `block` of those of one set of keys (with a.fused: the message's, then the own).  PARTS: bf16 parts of a weight in the product with V.
+template <int D, int PARTS>
 __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKeys& k, const int block, char* sm) {
   constexpr int KK = D / 16, DB = D / 32, TILE = AT_KEYS * D * 2;
   // set of keys, tile of rows and range of keys; the rows with the most keys first
@@ -126,7 +126,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int j = 32 * b + 8 * (e >> 2) + (e & 3);
-            x[b][e] = (j > view.lo) | (j < view.first) ? x[b][e] : -INFINITY;
+            x[b][e] = ((j > view.lo) | (j < view.first)) ? x[b][e] : -INFINITY;
           }
     }
     float top[4];
@@ -186,15 +186,20 @@ __device__ __forceinline__ void attend_tile(const AttendArgs& a, const AttendKey
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      TileFrag p;
+      TileFrag p, rest;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p.v[e] = (__bf16)x[t >> 1][8 * (t & 1) + e];
+      for (int e = 0; e < 8; ++e) {
+        const float w = x[t >> 1][8 * (t & 1) + e];
+        p.v[e] = (__bf16)w;
+        if (PARTS == 2) rest.v[e] = (__bf16)(w - (float)p.v[e]);
+      }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         TileFrag v;
         v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tv + at_v[db] + t * 16 * 2 * D));
         v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tv + at_v[db] + (t * 16 + 8) * 2 * D));
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p.v, o[db], 0, 0, 0);
+        if (PARTS == 2) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, rest.v, o[db], 0, 0, 0);
       }
     }
   };

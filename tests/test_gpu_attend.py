@@ -613,3 +613,16 @@ def test_long_and_short_first_rows_per_head(dtype, T):
     kv_len = torch.tensor([[4000, 3900, 3000, 60]], dtype=torch.int32)
     for sink in (0, 8, 3500):
         _attend_and_check(Q, K, V, kv_len, causal=True, window=64, sink=sink, sink_len=sink_len)
+
+
+@pytest.mark.parametrize("S,T,d", [(8, 1, 128), (9, 1, 128), (40, 1, 64), (5, 3, 64), (3, 8, 128)])
+def test_precision_of_few_queries_does_not_depend_on_the_batch(S, T, d):
+    """Up to 32 query rows per sample and KV head the weights keep 16 bits, however many samples share the message."""
+    B = _b()
+    Q, K, V = _make(27, BF, d, S, 1, 4, T, 40)
+    _, PK, PV = _make(28, BF, d, 1, 1, 4, 1, 700)
+    kv_len, plen = _lens(3, S, 1, T, 40), torch.tensor([700], dtype=torch.int32)
+    O, lse, _, tO, tl, _ = R.attend(Q, K, V, kv_len, prefix=(PK[0], PV[0], plen), p_eps=2.0 ** -16)
+    o = B.attend_shared(Q.cuda(), PK[0].cuda(), PV[0].cuda(), K.cuda(), V.cuda(), prefix_len=plen.cuda(), kv_len=kv_len.cuda())
+    _check("lse", o["lse"], lse, tl)
+    _check("O", o["O"], O, tO)
