@@ -360,9 +360,10 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
  * Sums and softmax statistics are single precision; O is rounded once to dtype.  With dtype OBF_BF16 the softmax weights enter
  * the product with V as two bf16 parts, or as one where n_queries * group is above 32 (by the sample's own rows, also for a message).
  * Limits: head_dim 64 or 128; group <= 128; n_queries <= 2^20; strides of rows <= 2^24; n_samples*n_kv_heads <= 65535; at most
- * 2^26 query rows and 2^30 cache rows; Q, K, V, O 16-byte aligned, strides of Q and O multiples of 16 bytes.  O may not overlap an input.  Results do
- * not depend on what the workspace held, and are the same from call to call.  Two calls that may overlap in time (or two captured
- * graphs) need a workspace each. */
+ * 2^26 query rows and 2^30 cache rows; Q, K, V, O 16-byte aligned, strides of Q and O multiples of 16 bytes.
+ * Outputs and workspace may not overlap one another or an input (what the host can see of it is OBF_ERR_INVALID_ARG).
+ * Results do not depend on what the workspace held, and are the same from call to call.  Two calls that may overlap in time
+ * (or two captured graphs) need a workspace each. */
 typedef struct {
   int32_t n_samples;
   int32_t n_kv_heads;

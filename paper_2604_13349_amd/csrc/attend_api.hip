@@ -156,9 +156,52 @@ static obf_status_t check_attend_ws(const AttendPlan& p, const void* ws, size_t 
   return OBF_OK;
 }
 
-static obf_status_t check_apart(const void* O, const void* Q, const void* K, const void* V) {
-  if (O == Q || O == K || O == V) { set_error("O must not be an input"); return OBF_ERR_INVALID_ARG; }
+// Memory that a call certainly reads or writes: all of a tensor without gaps, the first run of one with gaps (whose gaps may hold another).
+struct Region { const char* name; const void* p; size_t bytes; };
+
+static obf_status_t check_apart(const Region* outs, const int n_outs, const Region* ins, const int n_ins) {
+  for (int i = 0; i < n_outs; ++i) {
+    const auto meets = [&](const Region& r) {
+      if (!attend_overlap(outs[i].p, outs[i].bytes, r.p, r.bytes)) return false;
+      set_error("%s must not overlap %s", outs[i].name, r.name);
+      return true;
+    };
+    for (int j = 0; j < n_ins; ++j) if (meets(ins[j])) return OBF_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j) if (meets(outs[j])) return OBF_ERR_INVALID_ARG;
+  }
   return OBF_OK;
+}
+
+// Elements of a Q or O.
+static size_t region_rows(const AttendArgs& a, const long d, const long s, const long h, const long t) {
+  const long heads = (long)a.H * a.g, all = a.S * heads * a.T * d;
+  if ((a.S - 1) * s + (heads - 1) * h + (a.T - 1) * t + d == all) return (size_t)all;
+  if (a.T > 1 && t != d) return (size_t)d;
+  if (heads > 1 && h != a.T * d) return (size_t)(a.T * d);
+  return (size_t)(heads * a.T * d);
+}
+// Rows of a cache, entries of its lengths.
+static size_t region_cache(const AttendArgs& a, const AttendKeys& k) {
+  const size_t one = (size_t)a.H * k.stride;
+  return k.samples > 1 && (size_t)k.sample_rows == one ? one * k.samples : one;
+}
+static size_t region_lens(const AttendArgs& a, const AttendKeys& k) { return (size_t)a.H * (k.samples > 1 && k.len_stride == a.H ? k.samples : 1); }
+
+static obf_status_t check_attend_apart(const obf_attend_t* c, const AttendPlan& p, const float* lse, const bool lse_out, const float* mass, const void* ws) {
+  const AttendArgs& a = p.a;
+  const size_t es = c->dtype == OBF_BF16 ? 2 : 4, row = c->head_dim * es;
+  const AttendKeys& own = a.keys[a.n_keys - 1];
+  const AttendKeys& front = a.keys[0];
+  const bool shared = a.n_keys > 1;
+  const Region first = {"lse", lse, (size_t)a.rows * 4}, none = {"", nullptr, 0};
+  const Region outs[] = {{"O", a.O, a.O ? region_rows(a, c->head_dim, a.os, a.oh, a.ot) * es : 0}, lse_out ? first : none,
+                         {"mass", mass, region_cache(a, own) * 4}, {"the workspace", ws, p.total}};
+  const Region ins[] = {{"Q", a.Q, region_rows(a, c->head_dim, a.qs, a.qh, a.qt) * es}, {"K", own.K, region_cache(a, own) * row},
+                        {"V", own.V, region_cache(a, own) * row}, {"kv_len", own.len, region_lens(a, own) * 4},
+                        {"sink_len", own.sink_len, region_lens(a, own) * 4}, lse_out ? none : first,
+                        {"prefix_K", shared ? front.K : nullptr, region_cache(a, front) * row}, {"prefix_V", shared ? front.V : nullptr, region_cache(a, front) * row},
+                        {"prefix_len", shared ? front.len : nullptr, region_lens(a, front) * 4}};
+  return check_apart(outs, sizeof(outs) / sizeof(outs[0]), ins, sizeof(ins) / sizeof(ins[0]));
 }
 
 static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void* prefix_K, const void* prefix_V, const int32_t* prefix_len,
@@ -168,8 +211,7 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   AttendArgs& a = p.a;
   char* base = (char*)ws;
-  if (mass && !lse) lse = (float*)(base + p.lse);
-  a.Q = Q; a.O = O; a.lse = lse;
+  a.Q = Q; a.O = O;
   a.part_O = (float*)(base + p.part_O);
   a.part_lse = (float*)(base + p.part_lse);
   AttendKeys& own = a.keys[a.n_keys - 1];
@@ -178,6 +220,9 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
     AttendKeys& m = a.keys[0];
     m.K = prefix_K; m.V = prefix_V; m.len = prefix_len; m.len_all = prefix_len_all;
   }
+  OBF_TRY(check_attend_apart(c, p, lse, true, mass, ws));
+  if (mass && !lse) lse = (float*)(base + p.lse);
+  a.lse = lse;
   if (mass && p.keep_logits) { a.logits = (float*)(base + p.logits); a.mass = mass; }
   OBF_TRY(launch_plan(p, c->head_dim, c->dtype, st));
   if (a.ranges > 1 || a.logits) OBF_TRY(launch_attend_join(a, c->head_dim, c->dtype, st));
@@ -201,7 +246,6 @@ obf_status_t obf_attend(const obf_attend_t* call, const void* Q, const void* K, 
                         void* O, float* lse, float* mass, void* ws, size_t ws_bytes, void* stream) {
   OBF_TRY(check_attend(call));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("O", O));
-  OBF_TRY(check_apart(O, Q, K, V));
   return run_attend(call, Q, nullptr, nullptr, nullptr, 0, 0, K, V, kv_len, sink_len, O, lse, mass, ws, ws_bytes, (hipStream_t)stream);
 }
 
@@ -216,7 +260,6 @@ obf_status_t obf_attend_shared(const obf_attend_t* call, const void* Q, const vo
   if (prefix_stride > kAttendMaxStride) { set_error("attend: prefix_stride above the supported %d", kAttendMaxStride); return OBF_ERR_UNSUPPORTED; }
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("prefix_K", prefix_K)); OBF_TRY(check_aligned("prefix_V", prefix_V));
   OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V)); OBF_TRY(check_aligned("O", O));
-  OBF_TRY(check_apart(O, Q, K, V));
   return run_attend(call, Q, prefix_K, prefix_V, prefix_len, prefix_len_all, prefix_stride, K, V, kv_len, sink_len, O, lse, nullptr, ws, ws_bytes,
                     (hipStream_t)stream);
 }
@@ -229,6 +272,7 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
   OBF_TRY(check_attend_ws(p, ws, ws_bytes));
   p.a.Q = Q;
   p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;
+  OBF_TRY(check_attend_apart(call, p, lse, false, mass, ws));
   p.ms.mass = mass; p.ms.part = (float*)((char*)ws + p.mass);
   return launch_attend_mass(p.a, call->head_dim, call->dtype, lse, p.ms, (hipStream_t)stream);
 }

@@ -141,3 +141,35 @@ def test_first_rows_per_head_of_unknown_number_get_ranges(lib):
     assert lib.obf_attend(C.byref(c), FAKE, FAKE, FAKE, None, FAKE, FAKE_O, None, None, FAKE, sizes[0] - 1, None) == 3
     whole = _call(n_samples=1, n_kv_heads=8, token_stride=8200, kv_len_all=8200)
     assert sizes[0] == lib.obf_attend_workspace_bytes(C.byref(whole), 0, 0)
+
+
+def test_outputs_that_meet_inputs_are_refused(lib):
+    """Every output, and the workspace, against every input and one another: the same start, the other's last byte, an output around an input."""
+    S, H, g, T, rows, d, P = 2, 2, 4, 3, 100, 128, 10
+    c = _call(n_queries=T)
+    size = {"Q": S * H * g * T * d * 2, "K": S * H * rows * d * 2, "V": S * H * rows * d * 2, "O": S * H * g * T * d * 2, "kv_len": S * H * 4, "sink_len": S * H * 4,
+            "lse": S * H * g * T * 4, "mass": S * H * rows * 4, "prefix_K": H * P * d * 2, "prefix_V": H * P * d * 2, "prefix_len": H * 4}
+    names = {"attend": ("Q", "K", "V", "kv_len", "sink_len", "O", "lse", "mass"), "mass": ("Q", "K", "lse", "kv_len", "sink_len", "mass"),
+             "shared": ("Q", "prefix_K", "prefix_V", "prefix_len", "K", "V", "kv_len", "sink_len", "O", "lse")}
+    outs = {"attend": ("O", "lse", "mass", "ws"), "mass": ("mass", "ws"), "shared": ("O", "lse", "ws")}
+
+    def call(kind, at):
+        p = {k: C.c_void_p(v) for k, v in at.items()}
+        a = [p[k] for k in names[kind]]
+        if kind == "attend":
+            return lib.obf_attend(C.byref(c), *a, p["ws"], size["ws"], None)
+        if kind == "mass":
+            return lib.obf_attend_mass(C.byref(c), *a, p["ws"], size["ws"], None)
+        return lib.obf_attend_shared(C.byref(c), *a[:4], P, P, *a[4:], p["ws"], size["ws"], None)
+
+    for kind in names:
+        size["ws"] = lib.obf_attend_workspace_bytes(C.byref(c), P if kind == "shared" else 0, int(kind != "shared"))
+        apart = {k: (i + 1) << 30 for i, k in enumerate(names[kind] + ("ws",))}
+        for o in outs[kind]:
+            for other in apart:
+                if other == o:
+                    continue
+                for at in (apart[other], apart[other] + (size[other] - 1) // 256 * 256, apart[other] - size[o] // 512 * 256):
+                    if apart[other] - size[o] < at:
+                        assert call(kind, {**apart, o: at}) == 1, (kind, o, other)
+                        assert o.replace("ws", "workspace") in lib.obf_last_error().decode()
