@@ -414,7 +414,7 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
  *   left as they were;  idx [n_heads][out_stride]: the rows kept, -1 behind them;  len_out [n_heads].
  * kv_len (DEVICE int32 [n_heads]; NULL: kv_len_all).  A head whose length lies outside [0, in_stride], or whose kept rows exceed
  * out_stride (possible with sink_len only), gets len_out = -1, idx -1 and no rows.  recent <= budget, min(budget + sink, in_stride) <= out_stride.
- * Outputs may not overlap inputs (what the host can see of it is OBF_ERR_INVALID_ARG). */
+ * Outputs may not overlap inputs or one another (OBF_ERR_INVALID_ARG). */
 obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const void* K, const void* V, const float* mass,
                        const int32_t* pos, const int32_t* kv_len, int32_t kv_len_all, int32_t in_stride, int32_t budget,
                        int32_t recent, const int32_t* sink_len, int32_t sink, void* K_out, void* V_out, float* mass_out,

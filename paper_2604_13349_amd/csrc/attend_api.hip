@@ -296,13 +296,11 @@ obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const v
   if (!pos != !pos_out) { set_error("pos and pos_out come together"); return OBF_ERR_INVALID_ARG; }
   const size_t row = (size_t)head_dim * (dtype == OBF_BF16 ? 2 : 4);
   const size_t in = (size_t)n_heads * in_stride, out = (size_t)n_heads * out_stride;
-  if (attend_overlap(K, in * row, K_out, out * row) || attend_overlap(K, in * row, V_out, out * row) || attend_overlap(V, in * row, K_out, out * row) ||
-      attend_overlap(V, in * row, V_out, out * row) || attend_overlap(K_out, out * row, V_out, out * row) ||
-      attend_overlap(mass, in * 4, mass_out, out * 4) || attend_overlap(pos, in * 4, pos_out, out * 4)) {
-    set_error("outputs must not overlap the caches they are taken from");
-    return OBF_ERR_INVALID_ARG;
-  }
-  if (kv_len && attend_overlap(kv_len, (size_t)n_heads * 4, len_out, (size_t)n_heads * 4)) { set_error("len_out must not overlap kv_len"); return OBF_ERR_INVALID_ARG; }
+  const size_t heads = (size_t)n_heads * 4;
+  const Region outs[] = {{"K_out", K_out, out * row}, {"V_out", V_out, out * row}, {"mass_out", mass_out, out * 4}, {"pos_out", pos_out, out * 4}, {"idx", idx, out * 4},
+                         {"len_out", len_out, heads}};
+  const Region ins[] = {{"K", K, in * row}, {"V", V, in * row}, {"mass", mass, in * 4}, {"pos", pos, in * 4}, {"kv_len", kv_len, heads}, {"sink_len", sink_len, heads}};
+  OBF_TRY(check_apart(outs, sizeof(outs) / sizeof(outs[0]), ins, sizeof(ins) / sizeof(ins[0])));
   EvictArgs a;
   a.K = K; a.V = V; a.mass = mass; a.pos = pos; a.len = kv_len; a.sink_len = sink_len;
   a.heads = n_heads; a.len_all = kv_len_all; a.in_stride = in_stride; a.budget = budget; a.recent = recent; a.sink = sink; a.out_stride = out_stride;

@@ -173,3 +173,24 @@ def test_outputs_that_meet_inputs_are_refused(lib):
                     if apart[other] - size[o] < at:
                         assert call(kind, {**apart, o: at}) == 1, (kind, o, other)
                         assert o.replace("ws", "workspace") in lib.obf_last_error().decode()
+
+
+def test_evictions_whose_outputs_meet_inputs_are_refused(lib):
+    heads, d, rows, room = 4, 128, 50, 12
+    ins = {"K": heads * rows * d * 2, "V": heads * rows * d * 2, "mass": heads * rows * 4, "pos": heads * rows * 4, "kv_len": heads * 4, "sink_len": heads * 4}
+    outs = {"K_out": heads * room * d * 2, "V_out": heads * room * d * 2, "mass_out": heads * room * 4, "pos_out": heads * room * 4, "idx": heads * room * 4, "len_out": heads * 4}
+    size = {**ins, **outs}
+    apart = {k: (i + 1) << 30 for i, k in enumerate(size)}
+
+    def evict(**moved):
+        p = {k: C.c_void_p(v) for k, v in {**apart, **moved}.items()}
+        return lib.obf_evict(heads, d, 1, p["K"], p["V"], p["mass"], p["pos"], p["kv_len"], rows, rows, 10, 4, p["sink_len"], 0, p["K_out"], p["V_out"], p["mass_out"],
+                             p["pos_out"], p["idx"], p["len_out"], room, None)
+
+    for o in outs:
+        for other in size:
+            if other == o:
+                continue
+            for at in (apart[other], apart[other] + (size[other] - 1) // 16 * 16, apart[other] - (size[o] - 1) // 16 * 16):
+                assert evict(**{o: at}) == 1, (o, other)
+                assert o in lib.obf_last_error().decode() and other in lib.obf_last_error().decode()
