@@ -344,7 +344,7 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
  *
  * obf_attend_t, one layer of a batch:
  *   Q, O      element (s, i, t, c) at s * stride[0] + i * stride[1] + t * stride[2] + c; all three strides 0: contiguous
- *             [n_samples][n_kv_heads*group][n_queries][head_dim].  Query head i belongs to KV head i / group.
+ *             [n_samples][n_kv_heads*group][n_queries][head_dim].  Rows of O do not overlap (those of Q may).  Query head i belongs to KV head i / group.
  *   K, V      row (s, h, j) at s * sample_stride + h * token_stride + j (in rows; sample_stride 0: n_kv_heads * token_stride),
  *             so a layer of [n_samples][n_layers][n_kv_heads][token_stride][head_dim] is a call's cache as it lies
  *   kv_len    rows per (sample, head), DEVICE int32, entry s * len_stride + h (len_stride 0: n_kv_heads); NULL: kv_len_all in

@@ -11,6 +11,21 @@ static bool attend_overlap(const void* a, size_t an, const void* b, size_t bn) {
   return a && b && (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
 }
 
+// Whether rows of `row` elements meet, at strides[i] between the counts[i] of each of three dimensions: from the smallest stride up, each has to pass what lies
+// below it.
+static bool rows_meet(const int64_t (&strides)[3], const int64_t (&counts)[3], const int64_t row) {
+  __int128 span = row;                                 // (before the limits of the numbers are checked)
+  bool done[3] = {counts[0] == 1, counts[1] == 1, counts[2] == 1};
+  for (;;) {
+    int next = -1;
+    for (int i = 0; i < 3; ++i) if (!done[i] && (next < 0 || strides[i] < strides[next])) next = i;
+    if (next < 0) return false;
+    if (strides[next] < span) return true;
+    done[next] = true;
+    span += (__int128)(counts[next] - 1) * strides[next];
+  }
+}
+
 static obf_status_t check_attend(const obf_attend_t* c) {
   if (!c) { set_error("attend: descriptor is NULL"); return OBF_ERR_INVALID_ARG; }
   if (c->n_samples < 1 || c->n_kv_heads < 1 || c->group < 1 || c->n_queries < 1 || c->token_stride < 1) {
@@ -32,6 +47,10 @@ static obf_status_t check_attend(const obf_attend_t* c) {
       set_error("attend: strides of Q and O must be multiples of 16 bytes and not negative");
       return OBF_ERR_INVALID_ARG;
     }
+  if ((c->o_stride[0] || c->o_stride[1] || c->o_stride[2]) && rows_meet(c->o_stride, {c->n_samples, (int64_t)c->n_kv_heads * c->group, c->n_queries}, c->head_dim)) {
+    set_error("attend: rows of O must not overlap");
+    return OBF_ERR_INVALID_ARG;
+  }
   if (c->head_dim != 64 && c->head_dim != 128) { set_error("head_dim %d unsupported (64 or 128)", c->head_dim); return OBF_ERR_UNSUPPORTED; }
   if (c->token_stride > kAttendMaxStride) { set_error("attend: token_stride above the supported %d", kAttendMaxStride); return OBF_ERR_UNSUPPORTED; }
   if (c->n_queries > kAttendMaxQueries) { set_error("attend: n_queries above the supported %d", kAttendMaxQueries); return OBF_ERR_UNSUPPORTED; }

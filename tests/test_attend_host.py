@@ -194,3 +194,17 @@ def test_evictions_whose_outputs_meet_inputs_are_refused(lib):
             for at in (apart[other], apart[other] + (size[other] - 1) // 16 * 16, apart[other] - (size[o] - 1) // 16 * 16):
                 assert evict(**{o: at}) == 1, (o, other)
                 assert o in lib.obf_last_error().decode() and other in lib.obf_last_error().decode()
+
+
+def test_rows_of_outputs_that_overlap_are_refused(lib):
+    """Samples, query heads and queries (2, 8, 5) at strides that put two rows in one place; and other orders, with gaps, that do not."""
+    for o in ((1024, 128, 64), (128, 128, 128), (0, 640, 128), (5112, 640, 128), (5120, 632, 128), (640, 1272, 128)):
+        c = _call(n_queries=5, o_stride=o)
+        rc, msg = _attend(lib, c)
+        assert rc == 1 and "overlap" in msg, o
+        assert lib.obf_attend_workspace_bytes(C.byref(c), 0, 0) == 0
+    for o in ((0, 0, 0), (5120, 640, 128), (5120, 128, 1024), (1024, 128, 2048), (640, 1280, 128), (8192, 648, 128)):
+        c = _call(n_queries=5, o_stride=o)
+        assert lib.obf_attend_workspace_bytes(C.byref(c), 0, 0) > 0, o
+    one = _call(n_samples=1, n_kv_heads=1, group=1, n_queries=5, o_stride=(0, 0, 128))
+    assert lib.obf_attend_workspace_bytes(C.byref(one), 0, 0) > 0
