@@ -586,6 +586,13 @@ class _on:
             self.back.__exit__(*exc)
 
 
+def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    """ws, if it holds `need` bytes of its own on the device, or a new one."""
+    if ws is None or ws.nbytes < need or ws.device != device or not ws.is_contiguous():
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    return ws
+
+
 def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, prefix=None):
     o = out if out is not None else {}
     if "O" not in o:
@@ -598,17 +605,15 @@ def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, pref
                                              _meta(pv), _meta(pl), bool(causal), _int("window", window), _int("sink", sink))
     lib = load_library()
     with _on(Q.device) as stream:
-        ws = o.get("ws")
-        if ws is None or ws.numel() < need or ws.device != Q.device:
-            ws = o["ws"] = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        ws = o["ws"] = _workspace(o.get("ws"), need, Q.device)
         if copy_lens:
             kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
         if prefix is None:
             _check(lib.obf_attend(C.byref(c), Q.data_ptr(), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(sink_len), O.data_ptr(), lse.data_ptr(),
-                                  _addr(mass), ws.data_ptr(), ws.numel(), stream))
+                                  _addr(mass), ws.data_ptr(), ws.nbytes, stream))
         else:
             _check(lib.obf_attend_shared(C.byref(c), Q.data_ptr(), pk.data_ptr(), pv.data_ptr(), _addr(pl), front, front, K.data_ptr(), V.data_ptr(),
-                                         _addr(kv_len), _addr(sink_len), O.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), stream))
+                                         _addr(kv_len), _addr(sink_len), O.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.nbytes, stream))
     return o
 
 
@@ -632,12 +637,11 @@ def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sin
     c, need, _, copy_lens = _attend_plan(_meta(Q), _meta(K), None, None, _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), None, None, None, bool(causal),
                                          _int("window", window), _int("sink", sink))
     with _on(Q.device) as stream:
-        if ws is None or ws.numel() < need or ws.device != Q.device:
-            ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        ws = _workspace(ws, need, Q.device)
         if copy_lens:
             kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
         _check(load_library().obf_attend_mass(C.byref(c), Q.data_ptr(), K.data_ptr(), lse.data_ptr(), _addr(kv_len), _addr(sink_len), mass.data_ptr(),
-                                              ws.data_ptr(), ws.numel(), stream))
+                                              ws.data_ptr(), ws.nbytes, stream))
     return mass
 
 

@@ -208,3 +208,12 @@ def test_rows_of_outputs_that_overlap_are_refused(lib):
         assert lib.obf_attend_workspace_bytes(C.byref(c), 0, 0) > 0, o
     one = _call(n_samples=1, n_kv_heads=1, group=1, n_queries=5, o_stride=(0, 0, 128))
     assert lib.obf_attend_workspace_bytes(C.byref(one), 0, 0) > 0
+
+
+def test_a_workspace_that_is_not_as_large_as_it_looks_is_not_used():
+    cpu = torch.device("cpu")
+    for ws in (None, torch.zeros(1, dtype=torch.uint8).expand(4096), torch.zeros(8192, dtype=torch.uint8)[::2], torch.zeros(4095, dtype=torch.uint8)):
+        got = B._workspace(ws, 4096, cpu)
+        assert got is not ws and got.is_contiguous() and got.nbytes == 4096
+    for ws in (torch.zeros(4096, dtype=torch.uint8), torch.zeros(1024), torch.zeros((2, 3000), dtype=torch.uint8)):
+        assert B._workspace(ws, 4096, cpu) is ws

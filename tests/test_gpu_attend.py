@@ -626,3 +626,16 @@ def test_precision_of_few_queries_does_not_depend_on_the_batch(S, T, d):
     o = B.attend_shared(Q.cuda(), PK[0].cuda(), PV[0].cuda(), K.cuda(), V.cuda(), prefix_len=plen.cuda(), kv_len=kv_len.cuda())
     _check("lse", o["lse"], lse, tl)
     _check("O", o["O"], O, tO)
+
+
+def test_an_expanded_workspace_is_replaced():
+    B = _b()
+    Q, K, V = (x.cuda() for x in _make(33, BF, 128, 1, 2, 2, 1, 3000))
+    want = B.attend(Q, K, V)
+    byte = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    o = B.attend(Q, K, V, out={"ws": byte.expand(want["ws"].nbytes)})
+    assert torch.equal(o["O"], want["O"]) and o["ws"].is_contiguous() and byte.item() == 0
+    mass = [torch.zeros((1, 2, 3000), device="cuda") for _ in range(2)]
+    B.attend_mass(Q, K, want["lse"], mass[0])
+    B.attend_mass(Q, K, want["lse"], mass[1], ws=byte.expand(1 << 24))
+    assert torch.equal(mass[0], mass[1]) and byte.item() == 0
