@@ -586,6 +586,14 @@ class _on:
             self.back.__exit__(*exc)
 
 
+def _forward_only(*tensors):
+    """These calls have no backward pass: what should get a gradient through them is refused, rather than answered without one."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("forward only: no gradient reaches a tensor that requires one (call under torch.no_grad(), or detach it)")
+
+
 def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
     """ws, if it holds `need` bytes of its own on the device, or a new one."""
     if ws is None or ws.nbytes < need or ws.device != device or not ws.is_contiguous():
@@ -594,12 +602,13 @@ def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
 
 
 def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, prefix=None):
+    pk, pv, pl = prefix if prefix is not None else (None, None, None)
+    _forward_only(Q, K, V, pk, pv, mass)
     o = out if out is not None else {}
     if "O" not in o:
         o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
     if "lse" not in o:
         o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
-    pk, pv, pl = prefix if prefix is not None else (None, None, None)
     O, lse = o["O"], o["lse"]
     c, need, front, copy_lens = _attend_plan(_meta(Q), _meta(K), _meta(V), _meta(O), _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), _meta(pk),
                                              _meta(pv), _meta(pl), bool(causal), _int("window", window), _int("sink", sink))
@@ -621,7 +630,7 @@ def attend(Q, K, V, kv_len=None, causal=True, window=0, sink=0, sink_len=None, m
     """obf_attend: Q [S,H*g,T,d] (any strides of 16 bytes, last dimension contiguous) over the caches K, V [S,H,rows,d] (samples any whole number of rows
     apart) with kv_len int32 [S,H] rows per head (None: all).  sink_len int32 [S,H]: first rows that stay visible behind a window, per head, in place of
     `sink`, which then says about how many they are, if that is known (for the launch alone).  mass float32 [S,H,rows], in place: accumulated attention weight.  out: a dict returned by an earlier call of the same shape, whose buffers and
-    workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws."""
+    workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws.  Forward only: tensors that require a gradient are refused while gradients are recorded."""
     return _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out)
 
 
@@ -634,6 +643,7 @@ def attend_shared(Q, prefix_K, prefix_V, K, V, prefix_len=None, kv_len=None, cau
 def attend_mass(Q, K, lse, mass, kv_len=None, causal=True, window=0, sink=0, sink_len=None, ws=None):
     """obf_attend_mass: adds to mass float32 [S,H,rows], in place, the attention weight of the rows of K under the lse [S,H*g,T] of an earlier call (whose
     workspace may be handed over as ws)."""
+    _forward_only(Q, K, lse, mass)
     c, need, _, copy_lens = _attend_plan(_meta(Q), _meta(K), None, None, _meta(lse), _meta(mass), _meta(kv_len), _meta(sink_len), None, None, None, bool(causal),
                                          _int("window", window), _int("sink", sink))
     with _on(Q.device) as stream:
@@ -691,6 +701,7 @@ def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, 
     """obf_evict on K, V [..., rows, d], mass float32 [..., rows] and pos (int32, optional) [..., rows]; leading dimensions = heads, kv_len and sink_len
     int32 [...].  out: buffers to fill, K_out, V_out [..., out_stride, d], mass_out, pos_out, idx [..., out_stride], len_out [...]; those not given are
     allocated with out_stride rows per head (default: sink + budget; needed with sink_len).  Rows behind len_out stay as they are."""
+    _forward_only(K, V, mass)
     o = out if out is not None else {}
     budget, recent, sink = _int("budget", budget), _int("recent", recent), _int("sink", sink)
     heads, rows, d, dtype, out_stride, want = _evict_plan(_flat(K), _flat(V), _flat(mass), _flat(pos), _flat(kv_len), _flat(sink_len), budget, sink, out_stride,

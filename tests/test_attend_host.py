@@ -217,3 +217,17 @@ def test_a_workspace_that_is_not_as_large_as_it_looks_is_not_used():
         assert got is not ws and got.is_contiguous() and got.nbytes == 4096
     for ws in (torch.zeros(4096, dtype=torch.uint8), torch.zeros(1024), torch.zeros((2, 3000), dtype=torch.uint8)):
         assert B._workspace(ws, 4096, cpu) is ws
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    x, m = torch.zeros((1, 1, 1, 64)), torch.zeros((1, 1, 1))
+    g, gm = x.clone().requires_grad_(), m.clone().requires_grad_()
+    calls = [lambda: B.attend(g, x, x), lambda: B.attend(x, g, x), lambda: B.attend(x, x, g), lambda: B.attend(x, x, x, mass=gm), lambda: B.attend_shared(g, x[0], x[0], x, x),
+             lambda: B.attend_shared(x, g[0], x[0], x, x), lambda: B.attend_shared(x, x[0], g[0], x, x), lambda: B.attend_mass(g, x, m, m), lambda: B.attend_mass(x, g, m, m),
+             lambda: B.attend_mass(x, x, gm, m), lambda: B.attend_mass(x, x, m, gm), lambda: B.evict(g, x, m, 1), lambda: B.evict(x, g, m, 1), lambda: B.evict(x, x, gm, 1)]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+            pytest.fail(f"call {i} was taken")
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):       # (as without: the tensors of this test are not on one)
+            call()
