@@ -93,7 +93,6 @@ __device__ __forceinline__ AttendView attend_view(const AttendKeys& k, const Att
   return {(k.causal ? min(p - s.skip, s.count - 1) : s.count - 1) - from, (k.causal && k.window > 0 ? p - k.window - s.skip : -1) - from,
           (s.skip > 0 ? s.split : sink) - from};
 }
-__device__ __forceinline__ AttendView attend_from(const AttendView v, const int from) { return {v.hi - from, v.lo - from, v.first - from}; }
 __device__ __forceinline__ bool attend_sees(const AttendView v, const int j) { return (j <= v.hi) & ((j > v.lo) | (j < v.first)); }
 // Whether some query at pmin .. pmax does not see some of the entries v .. v + width - 1.
 __device__ __forceinline__ bool attend_cut(const AttendKeys& k, const AttendSpan s, const int sink, const int pmin, const int pmax, const int v, const int width) {
@@ -125,7 +124,7 @@ __device__ __forceinline__ size_t attend_row_number(const AttendArgs& a, const i
 constexpr int kAttendFewRows = 32;    // query rows per set of keys up to which the waves read the keys straight into registers
 constexpr int kAttendTileRows = 128;
 obf_status_t launch_attend_few(const AttendArgs& a, int tile_rows, int d, int dtype, hipStream_t st);
-obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);
+obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st);              // keys[0] alone, or (fused) both sets
 obf_status_t launch_attend_tile_few(const AttendArgs& a, int d, hipStream_t st);          // keys[0] by tiles of many rows, keys[1] by tiles of 16
 obf_status_t launch_attend_join(const AttendArgs& a, int d, int dtype, hipStream_t st);   // joins the ranges; adds the logits' weights to the mass
 

@@ -26,11 +26,9 @@ namespace obf {
 template <int D>
 __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile(const AttendArgs a) {
   __shared__ __attribute__((aligned(1024))) char sm[attend_tile_bytes<D>()];
-  int block = blockIdx.x;
   AttendKeys k = a.keys[0];
   if (a.fused) k = a.keys[1];
-  else if (block >= k.blocks) { block -= k.blocks; k = a.keys[1]; }
-  attend_tile<D, 1>(a, k, block, sm);
+  attend_tile<D, 1>(a, k, blockIdx.x, sm);
 }
 
 // A message's rows against all samples' queries, and the samples' own rows against theirs, in one launch: products beside loads.  The weights of both enter V's
@@ -46,7 +44,7 @@ __global__ __launch_bounds__(AT_THREADS, 2) void k_attend_tile_few(const AttendA
 
 obf_status_t launch_attend_tile(const AttendArgs& a, int d, hipStream_t st) {
   ProfScope prof(ST_ATTEND, st);
-  const int blocks = a.fused ? a.keys[1].blocks : a.keys[0].blocks + (a.n_keys > 1 ? a.keys[1].blocks : 0);
+  const int blocks = a.keys[a.fused ? 1 : 0].blocks;
   if (d == 128) hipLaunchKernelGGL(k_attend_tile<128>, dim3(blocks), dim3(AT_THREADS), 0, st, a);
   else hipLaunchKernelGGL(k_attend_tile<64>, dim3(blocks), dim3(AT_THREADS), 0, st, a);
   return check_launch("attend");
