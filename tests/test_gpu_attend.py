@@ -639,3 +639,23 @@ def test_an_expanded_workspace_is_replaced():
     B.attend_mass(Q, K, want["lse"], mass[0])
     B.attend_mass(Q, K, want["lse"], mass[1], ws=byte.expand(1 << 24))
     assert torch.equal(mass[0], mass[1]) and byte.item() == 0
+
+
+@pytest.mark.parametrize("T", [1, 100])
+def test_a_used_workspace_changes_no_weight(T):
+    B = _b()
+    Q, K, V = (x.cuda() for x in _make(15, BF, 128, 2, 2, 4, T, 2000))
+    kv_len = _lens(1, 2, 2, 1500, 2000).cuda()
+    mass = [torch.zeros(2, 2, 2000, device="cuda") for _ in range(3)]
+    o = B.attend(Q, K, V, kv_len=kv_len, mass=mass[0])
+    first = o["O"].clone(), o["lse"].clone()
+    o["ws"].fill_(255)
+    again = B.attend(Q, K, V, kv_len=kv_len, mass=mass[1], out=o)
+    assert torch.equal(again["O"], first[0]) and torch.equal(again["lse"], first[1]) and torch.equal(mass[0], mass[1])
+
+
+@pytest.mark.parametrize("d,S,H,g,T,window", [(128, 1, 8, 2, 70, 0), (64, 2, 8, 2, 40, 33), (128, 2, 8, 3, 20, 0), (64, 3, 8, 1, 140, 0), (128, 1, 6, 2, 40, 0)])
+def test_heads_in_multiples_of_eight(d, S, H, g, T, window):
+    """Samples times KV heads in one, two and three rounds of eight, and in rounds of two: the order in which the sets of keys go round the dies."""
+    Q, K, V = _make(29, BF, d, S, H, g, T, 300)
+    _attend_and_check(Q, K, V, _lens(11, S, H, T, 300), window=window, sink=3)
