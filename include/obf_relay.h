@@ -407,8 +407,9 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
 
 /* Eviction by accumulated attention weight.  Of a head of n rows the first s (sink_len[h], DEVICE int32, or `sink`; they travel
  * outside the budget, as in obf_window_t) and min(budget, n - s) of the others are kept: the newest `recent` ones and those of
- * the largest mass, ties to the lowest index, by the order of the fp32 bit patterns (obf_select_topk's).  Kept rows keep their
- * order and are copied bit for bit:
+ * the largest mass, ties to the lowest index, by the order of the fp32 bit patterns (obf_select_topk's).  With sink_len, `sink`
+ * only says about how many the first rows are, for the launch (0: any number).  Kept rows keep their order and are copied bit
+ * for bit:
  *   K, V [n_heads][in_stride][head_dim], mass [n_heads][in_stride], pos (nullable int32, the same)   ->
  *   K_out, V_out [n_heads][out_stride][head_dim], mass_out, pos_out [n_heads][out_stride]; rows at and behind len_out[h] are
  *   left as they were;  idx [n_heads][out_stride]: the rows kept, -1 behind them;  len_out [n_heads].

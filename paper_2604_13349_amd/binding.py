@@ -700,7 +700,8 @@ def _evict_plan(K, V, mass, pos, kv_len, sink_len, budget, sink, out_stride, giv
 def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, sink_len=None, pos=None, out=None, out_stride: Optional[int] = None):
     """obf_evict on K, V [..., rows, d], mass float32 [..., rows] and pos (int32, optional) [..., rows]; leading dimensions = heads, kv_len and sink_len
     int32 [...].  out: buffers to fill, K_out, V_out [..., out_stride, d], mass_out, pos_out, idx [..., out_stride], len_out [...]; those not given are
-    allocated with out_stride rows per head (default: sink + budget; needed with sink_len).  Rows behind len_out stay as they are."""
+    allocated with out_stride rows per head (default: sink + budget; needed with sink_len, beside which `sink` only says about how many first rows there are, if
+    that is known).  Rows behind len_out stay as they are."""
     _forward_only(K, V, mass)
     o = out if out is not None else {}
     budget, recent, sink = _int("budget", budget), _int("recent", recent), _int("sink", sink)

@@ -227,8 +227,9 @@ __global__ __launch_bounds__(EG_THREADS) void k_evict_rows(const EvictArgs a) {
 obf_status_t launch_evict(const EvictArgs& a, hipStream_t st) {
   ProfScope prof(ST_EVICT, st);
   // A head's own workgroup copies its rows where they are few: one launch for two (us, two and one, heads x rows kept of 512 bytes: 2 x 64 8.9 - 7.3,
-  // 64 x 205 12.8 - 11.5, 288 x 120 22.7 - 21.0, 1000 x 100 41 - 37; 8 x 400 12.0 - 13.0, 288 x 1229 93 - 110).
-  const long most = (long)a.budget + a.sink, bytes = (a.out_stride < most ? a.out_stride : most) * a.row_vec * 32;
+  // 64 x 205 12.8 - 11.5, 288 x 120 22.7 - 21.0, 1000 x 100 41 - 37; 8 x 400 12.0 - 13.0, 288 x 1229 93 - 110).  First rows counted per head may be any number
+  // of them that fits, unless `sink` says about how many (8 x 8064 rows: 28 - 109).
+  const long most = a.sink_len && a.sink == 0 ? (long)a.out_stride : (long)a.budget + a.sink, bytes = (a.out_stride < most ? a.out_stride : most) * a.row_vec * 32;
   const int with_rows = bytes <= kEvictOwnRows;
   const dim3 grid(a.heads), threads(EV_THREADS);
   if (a.in_stride <= EV_THREADS) hipLaunchKernelGGL(k_evict_select<1>, grid, threads, 0, st, a, with_rows);

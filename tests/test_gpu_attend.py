@@ -659,3 +659,20 @@ def test_heads_in_multiples_of_eight(d, S, H, g, T, window):
     """Samples times KV heads in one, two and three rounds of eight, and in rounds of two: the order in which the sets of keys go round the dies."""
     Q, K, V = _make(29, BF, d, S, H, g, T, 300)
     _attend_and_check(Q, K, V, _lens(11, S, H, T, 300), window=window, sink=3)
+
+
+@pytest.mark.parametrize("sink", [0, 9, 2500])
+def test_evictions_behind_long_and_short_first_rows(sink):
+    """An inherited message of thousands of rows beside a small budget; what `sink` says of its length changes nothing."""
+    B = _b()
+    _, K, V = _make(34, BF, 64, 1, 5, 1, 1, 3000)
+    mass = torch.rand((5, 3000), generator=torch.Generator().manual_seed(8))
+    kv_len = torch.tensor([3000, 2900, 2600, 100, 0], dtype=torch.int32)
+    sink_len = torch.tensor([2500, 0, 2599, 2000, 7], dtype=torch.int32)
+    o = B.evict(K[0].cuda(), V[0].cuda(), mass.cuda(), 40, kv_len=kv_len.cuda(), recent=8, sink=sink, sink_len=sink_len.cuda(), out_stride=2700)
+    for h in range(5):
+        keep = R.evict(mass[h], int(kv_len[h]), 40, 8, int(sink_len[h]))
+        n = len(keep)
+        assert int(o["len_out"][h]) == n and o["idx"][h].tolist() == keep + [-1] * (2700 - n)
+        assert torch.equal(o["K_out"][h, :n].cpu(), K[0, h, keep]) and torch.equal(o["V_out"][h, :n].cpu(), V[0, h, keep])
+        assert torch.equal(o["mass_out"][h, :n].cpu(), mass[h, keep])
