@@ -356,7 +356,8 @@ obf_status_t obf_compress_relay_static(const obf_shape_t* shape, const void* K, 
  * Logits are q . k / sqrt(head_dim), Q and K as given.  Of a head of n rows query t stands at position p = n - n_queries + t and
  * sees the rows j < n with, if causal, j <= p and, if window > 0 (causal only), j > p - window or j < sink.  A query that sees
  * nothing gets O = 0 and lse = -inf.  What a query does not see never reaches its result, not-a-number and infinities included
- * (what it sees does; an infinity among the visible rows may make a result not-a-number); rows at and behind a head's length are not read.
+ * (what it sees does; an infinity among the visible rows, or values whose weighted sum leaves single precision before it is
+ * divided, may make a result not-a-number); rows at and behind a head's length are not read.
  * Sums and softmax statistics are single precision; O is rounded once to dtype.  With dtype OBF_BF16 the softmax weights enter
  * the product with V as two bf16 parts, or as one where n_queries * group is above 32 (by the sample's own rows, also for a message).
  * Limits: head_dim 64 or 128; group <= 128; n_queries <= 2^20; strides of rows <= 2^24; n_samples*n_kv_heads <= 65535; at most

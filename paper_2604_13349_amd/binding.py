@@ -586,12 +586,10 @@ class _on:
             self.back.__exit__(*exc)
 
 
-def _forward_only(*tensors):
+def _forward_only(a, b, c, *more):
     """These calls have no backward pass: what should get a gradient through them is refused, rather than answered without one."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("forward only: no gradient reaches a tensor that requires one (call under torch.no_grad(), or detach it)")
+    if torch.is_grad_enabled() and (a.requires_grad or b.requires_grad or c.requires_grad or more and any(t is not None and t.requires_grad for t in more)):
+        raise ValueError("forward only: no gradient reaches a tensor that requires one (call under torch.no_grad(), or detach it)")
 
 
 def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
@@ -602,8 +600,14 @@ def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
 
 
 def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, prefix=None):
-    pk, pv, pl = prefix if prefix is not None else (None, None, None)
-    _forward_only(Q, K, V, pk, pv, mass)
+    pk = pv = pl = None
+    if prefix is not None:
+        pk, pv, pl = prefix
+        _forward_only(Q, K, V, pk, pv)
+    elif mass is not None:
+        _forward_only(Q, K, V, mass)
+    else:
+        _forward_only(Q, K, V)
     o = out if out is not None else {}
     if "O" not in o:
         o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)

@@ -15,7 +15,7 @@
 // 4.9), 48 x 8 heads of 1044 visible rows 37 us, 5.4; short ones by the launch and one chain of loads: 8 heads of 100 to 340 rows 8 us.  Eight waves a
 // workgroup: 5 to 20 % slower but for few long heads (8 of 32000 rows 35 us for 38).  Loads one tile ahead: the same times.  With the logits kept (32 x 8 heads
 // of 1000 to 4096 rows) 75 us for 60 without, where a second pass over the keys takes 58.  fp32, 3 x 2 heads, 333 queries of 2: 12 us, the chain of
-// products of a wave (32 rows a workgroup: 21 us).
+// products of a wave (32 rows a workgroup: 21 us).  32 rows a workgroup of head_dim 128 do not fit the registers whole: 96 bytes a lane lie in scratch memory.
 #include "attend_few.hpp"
 
 namespace obf {

@@ -70,8 +70,9 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
 // 64 at a time, loaded straight to it while the present ones' weights are taken (operands read from memory row by row cost a cache line per lane and load).
 // The rows are cut into ranges of ms.per steps, so that a head's early keys, which many queries see, take no longer than its late ones; the ranges' sums are
 // added in their order by k_attend_mass_add.
-// Two samples of 40 heads and 2048 queries: 103 us; the vector work (a multiply-add, an exponential and an addition per weight) takes half of the cycles, the
-// products a fifth beside it, the last workgroups a quarter.  Loads three steps ahead, both keys' products before their weights: no faster.
+// Two samples of 40 heads and 2048 queries: 100 us; vector work takes 0.38 of the cycles, the products 0.19, a quarter of that beside it.  Of 6.4 vector
+// instructions per exponential three are the weights' (a multiply-add, the exponential, an addition): the rows' addresses take some 80 a step of about 300, the
+// fixed part of a range some 500, and the masked blocks bring scalars back that have no register.  Loads three steps ahead, both keys' products before their weights: no faster.
 constexpr int MT_WAVES = 4, MT_THREADS = MT_WAVES * 64, MT_KEYS = MT_WAVES * 64, MT_ROWS = 64;
 
 // query rows r0 .. r1 - 1 that see a key of the 256 from base on
@@ -235,8 +236,8 @@ __global__ __launch_bounds__(256) void k_attend_mass_add(const AttendArgs a, con
   if (ranges > 0) ms.mass[(size_t)s * k.sample_rows + (size_t)h * k.stride + j] += v;
 }
 
-// Steps of a range: three rounds of workgroups, two per compute unit, where half of a causal call's steps are not taken; not less than 8, beside which the
-// operands of the keys and the sums at the end cost little.  (2 x 8 heads, 2048 queries of 5 heads, us of the whole call: one round 263, two 245, three 240,
+// Steps of a range: three rounds of workgroups, two per compute unit, where half of a causal call's steps are not taken; not less than 8, beside whose 2400
+// vector instructions a wave's fixed 500 (operands of the keys, addresses, the sums over lanes at the end) still count.  (2 x 8 heads, 2048 queries of 5 heads, us of the whole call: one round 263, two 245, three 240,
 // four with 4 steps at least 243.)
 AttendMass plan_attend_mass(const AttendArgs& a, int dtype) {
   const AttendKeys& k = a.keys[a.n_keys - 1];

@@ -14,9 +14,10 @@
 //
 // Two workgroups share a compute unit, so that one's products run beside the other's exponentials.  32 query heads of 8192 queries over 9421 rows: 710 us,
 // 1.01 PFLOP/s (the library's largest product reaches 1.22), the matrix pipe busy half the time at a clock that its power holds at 1.7 to 1.95 GHz.  Two
-// samples of 40 heads and 2048 queries 125 us, 0.77: 1280 workgroups are two and a half rounds, the masked tiles an eighth.  head_dim 64, 16384 queries, window
-// of 1024: 190 us, 0.70 PFLOP/s, the vector work (a multiply-add, an exponential, an addition and a half of a maximum and a rounding per weight) takes 0.86 of
-// the cycles.  A raised wave priority during the products, operands of V read ahead of the exponentials: within 1 %.  The check for
+// samples of 40 heads and 2048 queries 125 us, 0.77, the matrix pipe busy 0.34 of the cycles: 7.5 vector instructions beside the products per exponential, where
+// the long prompt has 6.1 (starts and ends of the workgroups, rescaling, masked tiles), and a last round of workgroups that is not full.  head_dim 64, 16384
+// queries, window of 1024: 190 us, 0.70 PFLOP/s, the vector work (a multiply-add, an exponential, an addition and a half of a maximum and a rounding per weight)
+// takes 0.69 of the cycles, it or the products 0.84.  A raised wave priority during the products, operands of V read ahead of the exponentials: within 1 %.  The check for
 // values that are not finite in every tile with masks, before it came to be made only where a result is none: 1 to 3 % more.
 #include "attend_few.hpp"
 #include "attend_tile.hpp"
