@@ -633,8 +633,9 @@ def _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out, pref
 def attend(Q, K, V, kv_len=None, causal=True, window=0, sink=0, sink_len=None, mass=None, out=None):
     """obf_attend: Q [S,H*g,T,d] (any strides of 16 bytes, last dimension contiguous) over the caches K, V [S,H,rows,d] (samples any whole number of rows
     apart) with kv_len int32 [S,H] rows per head (None: all).  sink_len int32 [S,H]: first rows that stay visible behind a window, per head, in place of
-    `sink`, which then says about how many they are, if that is known (for the launch alone).  mass float32 [S,H,rows], in place: accumulated attention weight.  out: a dict returned by an earlier call of the same shape, whose buffers and
-    workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws.  Forward only: tensors that require a gradient are refused while gradients are recorded."""
+    `sink`, which then says about how many they are, if that is known (for the launch alone).  mass float32 [S,H,rows], in place: accumulated attention weight.
+    out: a dict returned by an earlier call of the same shape, whose buffers and workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws.
+    Forward only: tensors that require a gradient are refused while gradients are recorded."""
     return _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out)
 
 

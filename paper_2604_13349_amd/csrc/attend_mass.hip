@@ -72,7 +72,8 @@ __global__ __launch_bounds__(AM_WAVES * 64) void k_attend_mass(const AttendArgs 
 // added in their order by k_attend_mass_add.
 // Two samples of 40 heads and 2048 queries: 100 us; vector work takes 0.38 of the cycles, the products 0.19, a quarter of that beside it.  Of 6.4 vector
 // instructions per exponential three are the weights' (a multiply-add, the exponential, an addition): the rows' addresses take some 80 a step of about 300, the
-// fixed part of a range some 500, and the masked blocks bring scalars back that have no register.  Loads three steps ahead, both keys' products before their weights: no faster.
+// fixed part of a range some 500, and the masked blocks bring scalars back that have no register.  Loads three steps ahead, both keys' products before their
+// weights: no faster.
 constexpr int MT_WAVES = 4, MT_THREADS = MT_WAVES * 64, MT_KEYS = MT_WAVES * 64, MT_ROWS = 64;
 
 // query rows r0 .. r1 - 1 that see a key of the 256 from base on
@@ -237,8 +238,8 @@ __global__ __launch_bounds__(256) void k_attend_mass_add(const AttendArgs a, con
 }
 
 // Steps of a range: three rounds of workgroups, two per compute unit, where half of a causal call's steps are not taken; not less than 8, beside whose 2400
-// vector instructions a wave's fixed 500 (operands of the keys, addresses, the sums over lanes at the end) still count.  (2 x 8 heads, 2048 queries of 5 heads, us of the whole call: one round 263, two 245, three 240,
-// four with 4 steps at least 243.)
+// vector instructions a wave's fixed 500 (operands of the keys, addresses, the sums over lanes at the end) still count.  (2 x 8 heads, 2048 queries of 5 heads, us of the
+// whole call: one round 263, two 245, three 240, four with 4 steps at least 243.)
 AttendMass plan_attend_mass(const AttendArgs& a, int dtype) {
   const AttendKeys& k = a.keys[a.n_keys - 1];
   AttendMass ms = {nullptr, nullptr, 1, 0, 0};
