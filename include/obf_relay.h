@@ -422,6 +422,63 @@ obf_status_t obf_evict(int32_t n_heads, int32_t head_dim, int32_t dtype, const v
                        int32_t recent, const int32_t* sink_len, int32_t sink, void* K_out, void* V_out, float* mass_out,
                        int32_t* pos_out, int32_t* idx, int32_t* len_out, int32_t out_stride, void* stream);
 
+/* ---- a cache held in codes of 4 or 8 bits -----------------------------------------------------------------------------
+ * Keys and values as the row codes of obf_quantize_rows, at the row numbers of a cache of obf_attend: row r has head_dim * bits / 8
+ * bytes of codes, a scale and a zero, and stands for zero + scale * q.  obf_cache_write puts new rows behind what a head holds,
+ * obf_cache_read gives rows back, obf_attend_codes attends over them. */
+typedef struct {
+  uint8_t* codes;         /* [rows][head_dim * bits / 8], 16-byte aligned */
+  uint16_t* scale_f16;    /* half-precision bit patterns, [rows] each */
+  uint16_t* zero_f16;
+} obf_codes_t;
+
+/* Rows that go into or come out of such a cache, one layer of a batch:
+ *   K, V      element (s, h, t, c) of n_rows rows per head at s * stride[0] + h * stride[1] + t * stride[2] + c; all three strides
+ *             0: contiguous [n_samples][n_kv_heads][n_rows][head_dim]
+ *   cache     row (s, h, j) at s * sample_stride + h * token_stride + j (sample_stride 0: n_kv_heads * token_stride)
+ *   kv_len    rows per (sample, head), DEVICE int32, entry s * len_stride + h (len_stride 0: n_kv_heads); NULL: kv_len_all in all.
+ *             A length below 0 or above token_stride counts as a head without rows.
+ * Limits: head_dim 64 or 128; token_stride, n_rows <= 2^24; n_samples*n_kv_heads <= 65535; at most 2^30 cache rows and 2^30 rows in
+ * K; K, V and codes 16-byte aligned, strides of K and V multiples of 16 bytes.  Values must lie in the half-precision range (an
+ * infinity or no number among a row's values may spoil that row, and no other).  Outputs may not overlap inputs or one another (what
+ * the host can see of it is OBF_ERR_INVALID_ARG). */
+typedef struct {
+  int32_t n_samples;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t bits;           /* 4 or 8 */
+  int32_t dtype;          /* obf_dtype_t of K, V */
+  int32_t n_rows;
+  int32_t token_stride;
+  int32_t kv_len_all;
+  int32_t len_stride;
+  int64_t sample_stride;
+  int64_t k_stride[3];
+  int64_t v_stride[3];
+} obf_cache_rows_t;
+
+/* Writes the newest rows of every head: kv_len counts them already (as obf_attend's lengths count the queries' rows), so that of a
+ * head of n rows, m of them new (n_new, DEVICE int32 laid out as kv_len; NULL: n_rows in all), row t < m of K and V becomes row
+ * n - m + t of the cache, by the arithmetic of obf_quantize_rows.  A row whose place would lie before row 0 is left out; a head whose
+ * m lies outside [0, n_rows] gets none.  All other rows of the cache stay as they are; the call may be repeated. */
+obf_status_t obf_cache_write(const obf_cache_rows_t* call, const void* K, const void* V, const int32_t* kv_len, const int32_t* n_new,
+                             const obf_codes_t* K_cache, const obf_codes_t* V_cache, void* stream);
+
+/* Row t of K and V becomes row idx[s][h][t] of the cache (DEVICE int32 [n_samples][n_kv_heads][n_rows]; NULL: row t), zero + scale * q
+ * rounded to single precision and then to dtype.  Where a head has no such row (a number outside [0, its length), the -1 behind an
+ * index list among them) K and V stay as they are. */
+obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_cache, const obf_codes_t* V_cache, const int32_t* kv_len,
+                            const int32_t* idx, void* K, void* V, void* stream);
+
+/* obf_attend over a cache held in codes (without accumulated weights); call->dtype is that of Q and O.  The rows enter as zero + scale * q:
+ * fp32, and bf16 up to 32 query rows (n_queries * group) per KV head, unrounded, with softmax weights times scale of 22 and 11 bits; bf16
+ * above 32 query rows: rounded to half precision (values past its range to the largest one), with weights of 11 bits.
+ * Rows at and behind a head's length are not read.  K and V name the codes' arrays, which are inputs. */
+size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits);
+obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V,
+                              const int32_t* kv_len, const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes,
+                              void* stream);
+
 /* Profiling aid (tracing of the path's own kernels with HIP events on the caller's stream).
  * obf_profile_enable(stage) makes every later call on this thread bracket the launch of that
  * internal stage's kernel with a pair of events; stage -1 switches it off.  obf_profile_read

@@ -33,6 +33,18 @@ class _Shape(C.Structure):
                 ("n_tokens", C.c_int32), ("window", C.c_int32), ("dtype", C.c_int32)]
 
 
+class _Codes(C.Structure):
+    """obf_codes_t."""
+    _fields_ = [("codes", C.c_void_p), ("scale_f16", C.c_void_p), ("zero_f16", C.c_void_p)]
+
+
+class _CacheRows(C.Structure):
+    """obf_cache_rows_t."""
+    _fields_ = [("n_samples", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("bits", C.c_int32), ("dtype", C.c_int32), ("n_rows", C.c_int32),
+                ("token_stride", C.c_int32), ("kv_len_all", C.c_int32), ("len_stride", C.c_int32), ("sample_stride", C.c_int64), ("k_stride", C.c_int64 * 3),
+                ("v_stride", C.c_int64 * 3)]
+
+
 class _Variant(C.Structure):
     """obf_variant_t."""
     _fields_ = [("no_projection", C.c_int32), ("subspace", C.c_int32), ("evr_tau", C.c_float),
@@ -134,6 +146,15 @@ def load_library():
     lib.obf_attend_mass.argtypes = [ap, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.obf_evict.restype = C.c_int
     lib.obf_evict.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp]
+    rp, cp = C.POINTER(_CacheRows), C.POINTER(_Codes)
+    lib.obf_cache_write.restype = C.c_int
+    lib.obf_cache_write.argtypes = [rp, vp, vp, vp, vp, cp, cp, vp]
+    lib.obf_cache_read.restype = C.c_int
+    lib.obf_cache_read.argtypes = [rp, cp, cp, vp, vp, vp, vp, vp]
+    lib.obf_attend_codes_workspace_bytes.restype = sz
+    lib.obf_attend_codes_workspace_bytes.argtypes = [ap, i32]
+    lib.obf_attend_codes.restype = C.c_int
+    lib.obf_attend_codes.argtypes = [ap, i32, vp, cp, cp, vp, vp, vp, vp, vp, sz, vp]
     lib.obf_profile_enable.restype = C.c_int
     lib.obf_profile_enable.argtypes = [i32]
     lib.obf_profile_read.restype = C.c_int
@@ -491,6 +512,18 @@ def _want(name: str, m, shape, dtype, contiguous=True):
         raise ValueError(f"{name} must be {'contiguous ' if contiguous else ''}{dtype} {list(shape)}")
 
 
+def _between_samples(name: str, shape, stride, width: int) -> int:
+    """Rows between the samples of a cache [samples, heads, rows, width] (or without the last dimension, where width is 1), whose heads are contiguous."""
+    S, H, rows = shape[:3]
+    if any(n > 1 and w != x for n, w, x in zip(shape[1:], stride[1:], (rows * width, width, 1))):
+        raise ValueError(f"{name}: the heads of a sample must be contiguous")
+    if S == 1:
+        return H * rows
+    if stride[0] % width or stride[0] < H * rows * width:
+        raise ValueError(f"{name}: samples must be whole rows apart and not overlap")
+    return stride[0] // width
+
+
 def _row_strides(name: str, m, d: int):
     """Strides of a [samples, heads, queries, d] tensor; those of dimensions of one are made up."""
     shape, stride = m[0], m[1]
@@ -518,18 +551,8 @@ def _attend_plan(Q, K, V, O, lse, mass, kv_len, sink_len, prefix_K, prefix_V, pr
         raise ValueError("Q and K must both be float32 or bfloat16")
     _want("V", V, K[0], dtype, contiguous=False)
 
-    def apart(name, m):
-        """Rows between the samples of a cache, whose heads are contiguous."""
-        if any(n > 1 and w != x for n, w, x in zip(m[0][1:], m[1][1:], (rows * d, d, 1))):
-            raise ValueError(f"{name}: the heads of a sample must be contiguous")
-        if S == 1:
-            return H * rows
-        if m[1][0] % d or m[1][0] < H * rows * d:
-            raise ValueError(f"{name}: samples must be whole rows apart and not overlap")
-        return m[1][0] // d
-
-    between = apart("K", K)
-    if V is not None and apart("V", V) != between:
+    between = _between_samples("K", K[0], K[1], d)
+    if V is not None and _between_samples("V", V[0], V[1], d) != between:
         raise ValueError("K and V must have the same strides")
     if mass is not None:
         _want("mass", mass, (S, H, rows), torch.float32, contiguous=False)
@@ -720,6 +743,165 @@ def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, 
             heads, d, dtype, K.data_ptr(), V.data_ptr(), mass.data_ptr(), _addr(pos), _addr(kv_len), rows, rows, budget, recent, _addr(sink_len), sink,
             o["K_out"].data_ptr(), o["V_out"].data_ptr(), o["mass_out"].data_ptr(), o["pos_out"].data_ptr() if pos is not None else None, o["idx"].data_ptr(),
             o["len_out"].data_ptr(), out_stride, stream))
+    return o
+
+
+class CodeCache:
+    """A cache held in codes of 4 or 8 bits (obf_codes_t): K_codes, V_codes uint8 [S,H,rows,d*bits/8], K_scale, K_zero, V_scale, V_zero float16 [S,H,rows];
+    samples any whole number of rows apart, the same in all six, the heads of a sample contiguous (a layer of [S,L,H,...] tensors is a cache as it lies).  Rows
+    are what quantize_rows makes of them.  Shapes, strides and devices are checked here, once: the tensors keep them."""
+
+    __slots__ = ("K_codes", "K_scale", "K_zero", "V_codes", "V_scale", "V_zero", "d", "bits", "shape", "between", "device")
+
+    def __init__(self, K_codes, K_scale, K_zero, V_codes, V_scale, V_zero, d: int, bits: int):
+        d, bits = _int("d", d), _int("bits", bits)
+        if bits not in (4, 8):
+            raise ValueError("bits must be 4 or 8")
+        if d not in (64, 128):
+            raise ValueError("d must be 64 or 128")
+        if K_codes.dim() != 4:
+            raise ValueError("K_codes must be [samples, heads, rows, d * bits / 8]")
+        S, H, rows = K_codes.shape[:3]
+        if K_codes.device.type != "cuda":
+            raise ValueError("tensors must be on a GPU")
+        between = None
+        for name, t, dtype, tail in (("K_codes", K_codes, torch.uint8, (d * bits // 8,)), ("K_scale", K_scale, torch.float16, ()), ("K_zero", K_zero, torch.float16, ()),
+                                     ("V_codes", V_codes, torch.uint8, (d * bits // 8,)), ("V_scale", V_scale, torch.float16, ()), ("V_zero", V_zero, torch.float16, ())):
+            if t.dtype != dtype or tuple(t.shape) != (S, H, rows) + tail:
+                raise ValueError(f"{name} must be {dtype} {[S, H, rows] + list(tail)}")
+            if t.device != K_codes.device:
+                raise ValueError(f"{name} is on {t.device}, not on {K_codes.device}")
+            apart = _between_samples(name, t.shape, t.stride(), tail[0] if tail else 1)
+            if between is not None and apart != between:
+                raise ValueError(f"{name} must have the row strides of K_codes")
+            between = apart
+        self.K_codes, self.K_scale, self.K_zero, self.V_codes, self.V_scale, self.V_zero = K_codes, K_scale, K_zero, V_codes, V_scale, V_zero
+        self.d, self.bits, self.shape, self.between, self.device = d, bits, (S, H, rows), between, K_codes.device
+
+    def _layout(self):
+        return self.shape, self.between, self.d, self.bits, self.device
+
+    def _codes(self):
+        return (_Codes(self.K_codes.data_ptr(), self.K_scale.data_ptr(), self.K_zero.data_ptr()),
+                _Codes(self.V_codes.data_ptr(), self.V_scale.data_ptr(), self.V_zero.data_ptr()))
+
+
+def code_cache(samples: int, heads: int, rows: int, d: int, bits: int = 4, device="cuda") -> CodeCache:
+    """An empty cache held in codes: room for `rows` rows per head."""
+    both = [[torch.zeros((samples, heads, rows, d * bits // 8), dtype=torch.uint8, device=device)] +
+            [torch.zeros((samples, heads, rows), dtype=torch.float16, device=device) for _ in range(2)] for _ in range(2)]
+    return CodeCache(*both[0], *both[1], d=d, bits=bits)
+
+
+def _lens_layout(S: int, H: int, metas):
+    """(entries between samples, 0: heads of all samples contiguous, or one sample; whether the lengths have to be made contiguous) of int32 [S, H] tensors."""
+    copy = any(H > 1 and m[1][1] != 1 or S > 1 and m[1][0] < H for m in metas) or len({m[1][0] for m in metas if S > 1}) > 1
+    return (metas[0][1][0] if metas and S > 1 and not copy else 0), copy
+
+
+@functools.lru_cache(maxsize=1024)
+def _rows_plan(cache, K, V, kv_len, per_head, idx):
+    """The descriptor of a cache_write (per_head: n_new) or cache_read (idx) from the tensors' metadata, which is checked: (obf_cache_rows_t, whether the
+    lengths have to be made contiguous)."""
+    (S, H, rows), between, d, bits, device = cache
+    for name, m in (("K", K), ("V", V), ("kv_len", kv_len), ("n_new", per_head), ("idx", idx)):
+        if m is not None and m[3] != device:
+            raise ValueError(f"{name} is on {m[3]}, not on {device}")
+    if len(K[0]) != 4 or tuple(K[0][:2]) != (S, H) or K[0][3] != d or K[2] not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"K must be float32 or bfloat16 [{S}, {H}, rows, {d}]")
+    _want("V", V, K[0], K[2], contiguous=False)
+    _want("kv_len", kv_len, (S, H), torch.int32, contiguous=False)
+    _want("n_new", per_head, (S, H), torch.int32, contiguous=False)
+    _want("idx", idx, K[0][:3], torch.int32)
+    len_stride, copy_lens = _lens_layout(S, H, [m for m in (kv_len, per_head) if m is not None])
+    c = _CacheRows(S, H, d, bits, OBF_F32 if K[2] == torch.float32 else OBF_BF16, K[0][2], rows, rows, len_stride, between)
+    c.k_stride = (C.c_int64 * 3)(*_row_strides("K", K, d))
+    c.v_stride = (C.c_int64 * 3)(*_row_strides("V", V, d))
+    return c, copy_lens
+
+
+def cache_write(cache: CodeCache, K, V, kv_len=None, n_new=None):
+    """obf_cache_write: K, V [S,H,T,d] (any strides of 16 bytes, last dimension contiguous) become the newest rows of the cache's heads.  kv_len int32 [S,H]:
+    rows per head with the new ones (None: the cache is full then); n_new int32 [S,H]: how many of the T rows are a head's (None: all), the first of them.
+    Returns the cache."""
+    _forward_only(K, V, K)
+    c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), _meta(n_new), None)
+    with _on(cache.device) as stream:
+        if copy_lens:
+            kv_len, n_new = (None if t is None else t.contiguous() for t in (kv_len, n_new))
+        kc, vc = cache._codes()
+        _check(load_library().obf_cache_write(C.byref(c), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(n_new), C.byref(kc), C.byref(vc), stream))
+    return cache
+
+
+def cache_read(cache: CodeCache, dtype: torch.dtype, kv_len=None, idx=None, out=None):
+    """obf_cache_read: rows idx int32 [S,H,n] of every head, or (None) all of its rows, as dtype.  out: a dict whose K_out, V_out [S,H,n,d] are filled; where a
+    head has no such row they stay as they are.  Without it they are made, with zeros in such places.  Returns the dict."""
+    o = out if out is not None else {}
+    S, H, rows = cache.shape
+    for name in ("K_out", "V_out"):
+        if name not in o:
+            o[name] = torch.zeros((S, H, rows if idx is None else idx.shape[-1], cache.d), dtype=dtype, device=cache.device)
+    K, V = o["K_out"], o["V_out"]
+    if K.dtype != dtype:
+        raise ValueError(f"K_out is {K.dtype}, not {dtype}")
+    _forward_only(K, V, K)
+    c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), None, _meta(idx))
+    with _on(cache.device) as stream:
+        if copy_lens:
+            kv_len = kv_len.contiguous()
+        kc, vc = cache._codes()
+        _check(load_library().obf_cache_read(C.byref(c), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(idx), K.data_ptr(), V.data_ptr(), stream))
+    return o
+
+
+@functools.lru_cache(maxsize=1024)
+def _attend_codes_plan(cache, Q, O, lse, kv_len, sink_len, causal, window, sink):
+    """As _attend_plan: (obf_attend_t, bytes of workspace, whether the lengths have to be made contiguous)."""
+    (S, H, rows), between, d, bits, device = cache
+    for name, m in (("Q", Q), ("O", O), ("lse", lse), ("kv_len", kv_len), ("sink_len", sink_len)):
+        if m is not None and m[3] != device:
+            raise ValueError(f"{name} is on {m[3]}, not on {device}")
+    if len(Q[0]) != 4 or Q[0][0] != S or Q[0][3] != d or H < 1 or Q[0][1] % H != 0:
+        raise ValueError("Q must be [samples, query heads, queries, d] and match the cache")
+    if Q[2] not in (torch.float32, torch.bfloat16):
+        raise ValueError("Q must be float32 or bfloat16")
+    _want("kv_len", kv_len, (S, H), torch.int32, contiguous=False)
+    _want("sink_len", sink_len, (S, H), torch.int32, contiguous=False)
+    _want("O", O, Q[0], Q[2], contiguous=False)
+    _want("lse", lse, Q[0][:3], torch.float32)
+    len_stride, copy_lens = _lens_layout(S, H, [m for m in (kv_len, sink_len) if m is not None])
+    c = _Attend(S, H, Q[0][1] // H, d, Q[0][2], rows, OBF_F32 if Q[2] == torch.float32 else OBF_BF16, int(causal), window, sink, rows, len_stride, between)
+    c.q_stride = (C.c_int64 * 3)(*_row_strides("Q", Q, d))
+    so = _row_strides("O", O, d)
+    if any(n > 1 and w < d for n, w in zip(O[0][:3], so)):
+        raise ValueError("O: rows must not overlap")
+    c.o_stride = (C.c_int64 * 3)(*so)
+    lib = load_library()
+    need = int(lib.obf_attend_codes_workspace_bytes(C.byref(c), bits))
+    if need == 0:
+        raise ObfError(2, lib.obf_last_error().decode())
+    return c, need, copy_lens
+
+
+def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0, sink_len=None, out=None):
+    """obf_attend_codes: attend, over a cache held in codes, without accumulated weights.  Returns a dict as attend does: O [S,H*g,T,d], lse [S,H*g,T], ws."""
+    _forward_only(Q, Q, Q)
+    o = out if out is not None else {}
+    if "O" not in o:
+        o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
+    if "lse" not in o:
+        o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+    O, lse = o["O"], o["lse"]
+    c, need, copy_lens = _attend_codes_plan(cache._layout(), _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
+                                            _int("sink", sink))
+    with _on(cache.device) as stream:
+        ws = o["ws"] = _workspace(o.get("ws"), need, cache.device)
+        if copy_lens:
+            kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
+        kc, vc = cache._codes()
+        _check(load_library().obf_attend_codes(C.byref(c), cache.bits, Q.data_ptr(), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(sink_len), O.data_ptr(),
+                                               lse.data_ptr(), ws.data_ptr(), ws.nbytes, stream))
     return o
 
 

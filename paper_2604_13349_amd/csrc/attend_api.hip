@@ -1,19 +1,13 @@
 // Entry points of the operators that read and thin out a relayed cache: argument checks, workspace, launches.
-#include "attend.hpp"
+#include "attend_check.hpp"
 
 namespace obf {
-
-constexpr int kAttendMaxStride = 1 << 24;     // rows between heads
-constexpr int kAttendMaxQueries = 1 << 20;
-constexpr int kAttendMaxGroup = 128;
 
 static bool attend_overlap(const void* a, size_t an, const void* b, size_t bn) {
   return a && b && (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
 }
 
-// Whether rows of `row` elements meet, at strides[i] between the counts[i] of each of three dimensions: from the smallest stride up, each has to pass what lies
-// below it.
-static bool rows_meet(const int64_t (&strides)[3], const int64_t (&counts)[3], const int64_t row) {
+bool rows_meet(const int64_t (&strides)[3], const int64_t (&counts)[3], const int64_t row) {
   __int128 span = row;                                 // (before the limits of the numbers are checked)
   bool done[3] = {counts[0] == 1, counts[1] == 1, counts[2] == 1};
   for (;;) {
@@ -26,7 +20,7 @@ static bool rows_meet(const int64_t (&strides)[3], const int64_t (&counts)[3], c
   }
 }
 
-static obf_status_t check_attend(const obf_attend_t* c) {
+obf_status_t check_attend(const obf_attend_t* c) {
   if (!c) { set_error("attend: descriptor is NULL"); return OBF_ERR_INVALID_ARG; }
   if (c->n_samples < 1 || c->n_kv_heads < 1 || c->group < 1 || c->n_queries < 1 || c->token_stride < 1) {
     set_error("attend: n_samples, n_kv_heads, group, n_queries, token_stride must all be >= 1");
@@ -67,10 +61,34 @@ static obf_status_t check_attend(const obf_attend_t* c) {
   return OBF_OK;
 }
 
-static obf_status_t check_aligned(const char* name, const void* p) {
+obf_status_t check_aligned(const char* name, const void* p) {
   if (!p) { set_error("%s is NULL", name); return OBF_ERR_INVALID_ARG; }
   if ((uintptr_t)p & 15) { set_error("%s must be 16-byte aligned", name); return OBF_ERR_INVALID_ARG; }
   return OBF_OK;
+}
+
+AttendArgs attend_args(const obf_attend_t* c) {
+  AttendArgs a = AttendArgs();
+  a.S = c->n_samples; a.H = c->n_kv_heads; a.g = c->group; a.T = c->n_queries;
+  a.g_inv = ((1u << 23) + a.g - 1) / a.g;
+  const long d = c->head_dim, hq = (long)a.H * a.g;
+  const bool qd = c->q_stride[0] || c->q_stride[1] || c->q_stride[2], od = c->o_stride[0] || c->o_stride[1] || c->o_stride[2];
+  a.qs = qd ? c->q_stride[0] : hq * a.T * d; a.qh = qd ? c->q_stride[1] : a.T * d; a.qt = qd ? c->q_stride[2] : d;
+  a.os = od ? c->o_stride[0] : hq * a.T * d; a.oh = od ? c->o_stride[1] : a.T * d; a.ot = od ? c->o_stride[2] : d;
+  a.scale2 = (float)(1.4426950408889634 / (d == 128 ? 11.313708498984761 : 8.0));
+  a.rows = (long)a.S * hq * a.T;
+  return a;
+}
+
+AttendKeys attend_own(const obf_attend_t* c) {
+  AttendKeys k = AttendKeys();
+  k.len_all = c->kv_len_all; k.len_stride = c->len_stride ? c->len_stride : c->n_kv_heads;
+  k.stride = c->token_stride; k.sample_rows = c->sample_stride ? c->sample_stride : (long)c->n_kv_heads * c->token_stride;
+  k.sink = c->sink;
+  k.window = c->window < c->token_stride ? c->window : 0;      // (positions lie below the stride: the others hide nothing)
+  k.causal = c->causal != 0;
+  k.samples = c->n_samples; k.row_samples = 1;
+  return k;
 }
 
 // The launch of one call: which kernel goes over which set of keys, tiles, ranges; and the workspace, in the order partial sums, partial normalisers, row
@@ -87,15 +105,8 @@ struct AttendPlan {
 static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride, bool with_mass, bool sinks_per_head) {
   AttendPlan p;
   AttendArgs& a = p.a;
-  a = AttendArgs();
-  a.S = c->n_samples; a.H = c->n_kv_heads; a.g = c->group; a.T = c->n_queries;
-  a.g_inv = ((1u << 23) + a.g - 1) / a.g;
-  const long d = c->head_dim, hq = (long)a.H * a.g;
-  const bool qd = c->q_stride[0] || c->q_stride[1] || c->q_stride[2], od = c->o_stride[0] || c->o_stride[1] || c->o_stride[2];
-  a.qs = qd ? c->q_stride[0] : hq * a.T * d; a.qh = qd ? c->q_stride[1] : a.T * d; a.qt = qd ? c->q_stride[2] : d;
-  a.os = od ? c->o_stride[0] : hq * a.T * d; a.oh = od ? c->o_stride[1] : a.T * d; a.ot = od ? c->o_stride[2] : d;
-  a.scale2 = (float)(1.4426950408889634 / (d == 128 ? 11.313708498984761 : 8.0));
-  a.rows = (long)a.S * hq * a.T;
+  a = attend_args(c);
+  const long d = c->head_dim;
   a.n_keys = 0;
   if (prefix_stride > 0) {
     AttendKeys& k = a.keys[a.n_keys++];
@@ -103,13 +114,7 @@ static AttendPlan plan_attend(const obf_attend_t* c, int prefix_stride, bool wit
     k.stride = prefix_stride; k.samples = 1; k.row_samples = a.S;
   }
   AttendKeys& k = a.keys[a.n_keys++];
-  k = AttendKeys();
-  k.len_all = c->kv_len_all; k.len_stride = c->len_stride ? c->len_stride : a.H;
-  k.stride = c->token_stride; k.sample_rows = c->sample_stride ? c->sample_stride : (long)a.H * c->token_stride;
-  k.sink = c->sink;
-  k.window = c->window < c->token_stride ? c->window : 0;      // (positions lie below the stride: the others hide nothing)
-  k.causal = c->causal != 0;
-  k.samples = a.S; k.row_samples = 1;
+  k = attend_own(c);
   const long own_rows = (long)a.T * a.g;
   // A sample's queries fill tiles of many rows by themselves: one pass over the message and the own rows, no partial results of the message.
   a.fused = a.n_keys > 1 && c->dtype == OBF_BF16 && own_rows > kAttendFewRows;
@@ -168,17 +173,14 @@ static obf_status_t launch_plan(const AttendPlan& p, int d, int dtype, hipStream
   return p.a.n_keys == 1 || p.a.fused ? launch_attend_tile(p.a, d, st) : launch_attend_tile_few(p.a, d, st);
 }
 
-static obf_status_t check_attend_ws(const AttendPlan& p, const void* ws, size_t ws_bytes) {
+obf_status_t check_attend_ws(const size_t need, const void* ws, size_t ws_bytes) {
   if (!ws) { set_error("workspace is NULL"); return OBF_ERR_INVALID_ARG; }
   if (((uintptr_t)ws & 255) != 0) { set_error("workspace must be 256-byte aligned"); return OBF_ERR_INVALID_ARG; }
-  if (ws_bytes < p.total) { set_error("workspace too small: %zu bytes given, %zu needed", ws_bytes, p.total); return OBF_ERR_WORKSPACE_TOO_SMALL; }
+  if (ws_bytes < need) { set_error("workspace too small: %zu bytes given, %zu needed", ws_bytes, need); return OBF_ERR_WORKSPACE_TOO_SMALL; }
   return OBF_OK;
 }
 
-// Memory that a call certainly reads or writes: all of a tensor without gaps, the first run of one with gaps (whose gaps may hold another).
-struct Region { const char* name; const void* p; size_t bytes; };
-
-static obf_status_t check_apart(const Region* outs, const int n_outs, const Region* ins, const int n_ins) {
+obf_status_t check_apart(const Region* outs, const int n_outs, const Region* ins, const int n_ins) {
   for (int i = 0; i < n_outs; ++i) {
     const auto meets = [&](const Region& r) {
       if (!attend_overlap(outs[i].p, outs[i].bytes, r.p, r.bytes)) return false;
@@ -191,20 +193,18 @@ static obf_status_t check_apart(const Region* outs, const int n_outs, const Regi
   return OBF_OK;
 }
 
-// Elements of a Q or O.
-static size_t region_rows(const AttendArgs& a, const long d, const long s, const long h, const long t) {
-  const long heads = (long)a.H * a.g, all = a.S * heads * a.T * d;
-  if ((a.S - 1) * s + (heads - 1) * h + (a.T - 1) * t + d == all) return (size_t)all;
-  if (a.T > 1 && t != d) return (size_t)d;
-  if (heads > 1 && h != a.T * d) return (size_t)(a.T * d);
-  return (size_t)(heads * a.T * d);
+size_t region_rows(const long S, const long heads, const long T, const long d, const long s, const long h, const long t) {
+  const long all = S * heads * T * d;
+  if ((S - 1) * s + (heads - 1) * h + (T - 1) * t + d == all) return (size_t)all;
+  if (T > 1 && t != d) return (size_t)d;
+  if (heads > 1 && h != T * d) return (size_t)(T * d);
+  return (size_t)(heads * T * d);
 }
-// Rows of a cache, entries of its lengths.
-static size_t region_cache(const AttendArgs& a, const AttendKeys& k) {
+size_t region_cache(const AttendArgs& a, const AttendKeys& k) {
   const size_t one = (size_t)a.H * k.stride;
   return k.samples > 1 && (size_t)k.sample_rows == one ? one * k.samples : one;
 }
-static size_t region_lens(const AttendArgs& a, const AttendKeys& k) { return (size_t)a.H * (k.samples > 1 && k.len_stride == a.H ? k.samples : 1); }
+size_t region_lens(const AttendArgs& a, const AttendKeys& k) { return (size_t)a.H * (k.samples > 1 && k.len_stride == a.H ? k.samples : 1); }
 
 static obf_status_t check_attend_apart(const obf_attend_t* c, const AttendPlan& p, const float* lse, const bool lse_out, const float* mass, const void* ws) {
   const AttendArgs& a = p.a;
@@ -213,9 +213,10 @@ static obf_status_t check_attend_apart(const obf_attend_t* c, const AttendPlan& 
   const AttendKeys& front = a.keys[0];
   const bool shared = a.n_keys > 1;
   const Region first = {"lse", lse, (size_t)a.rows * 4}, none = {"", nullptr, 0};
-  const Region outs[] = {{"O", a.O, a.O ? region_rows(a, c->head_dim, a.os, a.oh, a.ot) * es : 0}, lse_out ? first : none,
+  const long hq = (long)a.H * a.g;
+  const Region outs[] = {{"O", a.O, a.O ? region_rows(a.S, hq, a.T, c->head_dim, a.os, a.oh, a.ot) * es : 0}, lse_out ? first : none,
                          {"mass", mass, region_cache(a, own) * 4}, {"the workspace", ws, p.total}};
-  const Region ins[] = {{"Q", a.Q, region_rows(a, c->head_dim, a.qs, a.qh, a.qt) * es}, {"K", own.K, region_cache(a, own) * row},
+  const Region ins[] = {{"Q", a.Q, region_rows(a.S, hq, a.T, c->head_dim, a.qs, a.qh, a.qt) * es}, {"K", own.K, region_cache(a, own) * row},
                         {"V", own.V, region_cache(a, own) * row}, {"kv_len", own.len, region_lens(a, own) * 4},
                         {"sink_len", own.sink_len, region_lens(a, own) * 4}, lse_out ? none : first,
                         {"prefix_K", shared ? front.K : nullptr, region_cache(a, front) * row}, {"prefix_V", shared ? front.V : nullptr, region_cache(a, front) * row},
@@ -227,7 +228,7 @@ static obf_status_t run_attend(const obf_attend_t* c, const void* Q, const void*
                                int32_t prefix_len_all, int32_t prefix_stride, const void* K, const void* V, const int32_t* kv_len,
                                const int32_t* sink_len, void* O, float* lse, float* mass, void* ws, size_t ws_bytes, hipStream_t st) {
   AttendPlan p = plan_attend(c, prefix_stride, mass != nullptr, sink_len != nullptr);
-  OBF_TRY(check_attend_ws(p, ws, ws_bytes));
+  OBF_TRY(check_attend_ws(p.total, ws, ws_bytes));
   AttendArgs& a = p.a;
   char* base = (char*)ws;
   a.Q = Q; a.O = O;
@@ -288,7 +289,7 @@ obf_status_t obf_attend_mass(const obf_attend_t* call, const void* Q, const void
   OBF_TRY(check_attend(call));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("K", K)); OBF_NONNULL(lse); OBF_NONNULL(mass);
   AttendPlan p = plan_attend(call, 0, true, sink_len != nullptr);
-  OBF_TRY(check_attend_ws(p, ws, ws_bytes));
+  OBF_TRY(check_attend_ws(p.total, ws, ws_bytes));
   p.a.Q = Q;
   p.a.keys[0].K = K; p.a.keys[0].len = kv_len; p.a.keys[0].sink_len = sink_len;
   OBF_TRY(check_attend_apart(call, p, lse, false, mass, ws));

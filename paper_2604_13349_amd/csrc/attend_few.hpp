@@ -168,6 +168,44 @@ __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { *(float4
 // What the waves of a workgroup leave for their join.
 template <int D, int NB, int NW> struct FewShared { float o[NW][16 * NB][D]; float m[NW][16 * NB], l[NW][16 * NB]; };
 
+// The waves' parts of the rows row0 .. of set (ks, h), to O and lse or to the range's place among the partial results.
+template <typename ET, int D, int NB, int NW>
+__device__ __forceinline__ void few_join(const AttendArgs& a, const AttendKeys& k, const int ks, const int h, const int row0, const int split, const FewShared<D, NB, NW>& sm) {
+  constexpr int ROWS = 16 * NB;
+  constexpr int PIECES = D / 4;
+  for (int e = threadIdx.x; e < ROWS * PIECES; e += NW * 64) {
+    const int r = e / PIECES, c = (e % PIECES) * 4;
+    if (row0 + r >= k.row_samples * a.T * a.g) break;
+    float top = sm.m[0][r];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm.m[w][r]);
+    const float ref = top > -INFINITY ? top : 0.f;
+    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = attend_exp2(sm.m[w][r] - ref);
+      sum = fmaf(f, sm.l[w][r], sum);
+      const float4 x = *(const float4*)&sm.o[w][r][c];
+      v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
+    }
+    // (a sum of 0: no key is visible; a sum that is no number: some visible logit is none, whatever `top` is)
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] *= inv;
+    const float lse2 = sum != 0.f ? top + attend_log2(sum) : -INFINITY;
+    const AttendRow w = attend_row(a, k, ks, row0 + r);
+    const size_t number = attend_row_number(a, h, w);
+    if (a.ranges > 1) {
+      const size_t at = (size_t)(k.split0 + split) * a.rows + number;
+      if (c == 0) a.part_lse[at] = lse2;
+      if (sum != 0.f) *(float4*)(a.part_O + at * D + c) = make_float4(v[0], v[1], v[2], v[3]);   // (nobody reads the others)
+    } else {
+      if (c == 0 && a.lse) a.lse[number] = lse2 * 0.69314718055994531f;
+      store4((ET*)a.O + (size_t)w.s * a.os + (size_t)(h * a.g + w.gi) * a.oh + (size_t)w.t * a.ot + c, v);
+    }
+  }
+}
+
 // Workgroup `block` of those of one set of keys; with_logits: the logits are kept if a.logits asks for it.
 template <typename ET, int D, int NB, int NW>
 __device__ __forceinline__ void attend_few(const AttendArgs& a, const AttendKeys& k, int block, const bool with_logits, FewShared<D, NB, NW>& sm) {
@@ -187,7 +225,6 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const AttendKeys
   const AttendSpan span = attend_span(k, n, sink, pmin, pmax);
   const int tiles = (span.count + 31) / 32, per = max(NW, (tiles + k.nsplit - 1) / k.nsplit);   // (a short head does not use all its ranges)
   const int first = split * per, behind = min(tiles, first + per);
-  const bool joined = a.ranges > 1;
   const ET* K = (const ET*)k.K + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
   const ET* V = (const ET*)k.V + ((size_t)ks * k.sample_rows + (size_t)h * k.stride) * D;
 
@@ -304,38 +341,7 @@ __device__ __forceinline__ void attend_few(const AttendArgs& a, const AttendKeys
       for (int c = 0; c < 4; ++c) sm.o[wave][r][Tile::channel(quad, db, c)] = o[nb][db][c];
   }
   __syncthreads();
-  constexpr int PIECES = D / 4;
-  for (int e = threadIdx.x; e < ROWS * PIECES; e += NW * 64) {
-    const int r = e / PIECES, c = (e % PIECES) * 4;
-    if (row0 + r >= set_rows) break;
-    float top = sm.m[0][r];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) top = fmaxf(top, sm.m[w][r]);
-    const float ref = top > -INFINITY ? top : 0.f;
-    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = attend_exp2(sm.m[w][r] - ref);
-      sum = fmaf(f, sm.l[w][r], sum);
-      const float4 x = *(const float4*)&sm.o[w][r][c];
-      v[0] = fmaf(f, x.x, v[0]); v[1] = fmaf(f, x.y, v[1]); v[2] = fmaf(f, x.z, v[2]); v[3] = fmaf(f, x.w, v[3]);
-    }
-    // (a sum of 0: no key is visible; a sum that is no number: some visible logit is none, whatever `top` is)
-    const float inv = sum != 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= inv;
-    const float lse2 = sum != 0.f ? top + attend_log2(sum) : -INFINITY;
-    const AttendRow w = attend_row(a, k, ks, row0 + r);
-    const size_t number = attend_row_number(a, h, w);
-    if (joined) {
-      const size_t at = (size_t)(k.split0 + split) * a.rows + number;
-      if (c == 0) a.part_lse[at] = lse2;
-      if (sum != 0.f) *(float4*)(a.part_O + at * D + c) = make_float4(v[0], v[1], v[2], v[3]);   // (nobody reads the others)
-    } else {
-      if (c == 0 && a.lse) a.lse[number] = lse2 * 0.69314718055994531f;
-      store4((ET*)a.O + (size_t)w.s * a.os + (size_t)(h * a.g + w.gi) * a.oh + (size_t)w.t * a.ot + c, v);
-    }
-  }
+  few_join<ET, D, NB, NW>(a, k, ks, h, row0, split, sm);
 }
 
 }  // namespace obf

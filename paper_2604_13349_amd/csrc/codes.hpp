@@ -1,0 +1,97 @@
+// The row code: a lane's part of a row, 16 consecutive columns, to codes and back.
+//
+// Every row carries an asymmetric code of its own and two half-precision numbers, zero = fp16(min x), scale = fp16((max x - min x) / L), L = 2^bits - 1,
+// q = clamp(rint((x - zero) / scale), 0, L), and stands for zero + scale q.  The integer decision is taken in single precision with individually rounded
+// subtract, divide and round-to-even.
+#pragma once
+#include <hip/hip_fp16.h>
+#include "common.hpp"
+
+namespace obf {
+
+constexpr int QT_THREADS = 256;
+constexpr int QT_COLS = 16;              // columns per lane
+
+// 16 consecutive elements (16-byte aligned) as floats, and back
+__device__ __forceinline__ void load16(const uint16_t* __restrict__ p, float (&o)[QT_COLS]) {
+  const uint4 v[2] = {((const uint4*)p)[0], ((const uint4*)p)[1]};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { o[8 * i + 2 * k] = __uint_as_float(w[k] << 16); o[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+  }
+}
+__device__ __forceinline__ void load16(const float* __restrict__ p, float (&o)[QT_COLS]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float4 v = ((const float4*)p)[i]; o[4 * i] = v.x; o[4 * i + 1] = v.y; o[4 * i + 2] = v.z; o[4 * i + 3] = v.w; }
+}
+__device__ __forceinline__ void store16(uint16_t* __restrict__ p, const float (&x)[QT_COLS]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = (uint32_t)float_to_bf16_bits(x[8 * i + 2 * k]) | ((uint32_t)float_to_bf16_bits(x[8 * i + 2 * k + 1]) << 16);
+    ((uint4*)p)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+__device__ __forceinline__ void store16(float* __restrict__ p, const float (&x)[QT_COLS]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ((float4*)p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+}
+
+// Codes of the 16 columns x of a row that LPR neighbouring lanes share, scale and zero as half-precision bits (the same in all of them).
+template <int LPR, int BITS>
+__device__ __forceinline__ void encode16(const float (&x)[QT_COLS], uint32_t (&w)[QT_COLS * BITS / 32], uint16_t& scale, uint16_t& zero) {
+  float lo = x[0], hi = x[0];
+#pragma unroll
+  for (int i = 1; i < QT_COLS; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
+#pragma unroll
+  for (int off = LPR / 2; off > 0; off >>= 1) { lo = fminf(lo, __shfl_xor(lo, off)); hi = fmaxf(hi, __shfl_xor(hi, off)); }
+  constexpr float L = (float)((1 << BITS) - 1);
+  const __half zh = __float2half_rn(lo), sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), L));
+  const float z = __half2float(zh), s = __half2float(sh);
+  uint32_t q[QT_COLS];
+  if (s > 0.f && s < INFINITY && fabsf(z) < INFINITY) {
+    // The correctly rounded quotient from the row's reciprocal (Markstein): with r = RN(1/s), s of eleven significant bits, a quotient
+    // within an ulp becomes the correctly rounded one by one residual step; the first step only brings it there.
+    const float r = __frcp_rn(s);
+#pragma unroll
+    for (int i = 0; i < QT_COLS; ++i) {
+      const float t = __fsub_rn(x[i], z);
+      float y = __fmul_rn(t, r);
+      y = __fmaf_rn(__fmaf_rn(-y, s, t), r, y);
+      y = __fmaf_rn(__fmaf_rn(-y, s, t), r, y);
+      q[i] = (uint32_t)fminf(fmaxf(rintf(y), 0.f), L);
+    }
+  } else {                                                     // a constant row, or values past the half-precision range
+#pragma unroll
+    for (int i = 0; i < QT_COLS; ++i)
+      q[i] = (s > 0.f) ? (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], z), s)), 0.f), L) : 0u;
+  }
+#pragma unroll
+  for (int k = 0; k < QT_COLS * BITS / 32; ++k) {              // little-endian: the even column of an int4 pair in the low half
+    w[k] = 0u;
+#pragma unroll
+    for (int i = 0; i < 32 / BITS; ++i) w[k] |= q[k * (32 / BITS) + i] << (i * BITS);
+  }
+  scale = __half_as_ushort(sh); zero = __half_as_ushort(zh);
+}
+template <int BITS>
+__device__ __forceinline__ void decode16(const uint32_t (&w)[QT_COLS * BITS / 32], const uint16_t scale, const uint16_t zero, float (&x)[QT_COLS]) {
+  const float s = __half2float(__ushort_as_half(scale)), z = __half2float(__ushort_as_half(zero));
+#pragma unroll
+  for (int i = 0; i < QT_COLS; ++i) x[i] = fmaf(s, (float)((w[i * BITS / 32] >> (i * BITS % 32)) & ((1u << BITS) - 1u)), z);
+}
+
+// A lane's codes, in one piece of 16 (8 bits) or 8 bytes.
+template <int BITS> __device__ __forceinline__ void load_codes16(const uint8_t* __restrict__ p, uint32_t (&w)[QT_COLS * BITS / 32]) {
+  if constexpr (BITS == 8) { const uint4 v = *(const uint4*)p; w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+  else { const uint2 v = *(const uint2*)p; w[0] = v.x; w[1] = v.y; }
+}
+template <int BITS> __device__ __forceinline__ void store_codes16(uint8_t* __restrict__ p, const uint32_t (&w)[QT_COLS * BITS / 32]) {
+  if constexpr (BITS == 8) *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+  else *(uint2*)p = make_uint2(w[0], w[1]);
+}
+
+}  // namespace obf

@@ -1,0 +1,191 @@
+// Entry points of the operators of a cache held in codes: argument checks, workspace, launches.
+#include "attend_check.hpp"
+#include "attend_codes.hpp"
+
+namespace obf {
+
+static obf_status_t check_codes(const char* name, const obf_codes_t* c) {
+  if (!c || !c->codes || !c->scale_f16 || !c->zero_f16) { set_error("%s: codes, scale and zero are needed", name); return OBF_ERR_INVALID_ARG; }
+  if ((uintptr_t)c->codes & 15) { set_error("%s: codes must be 16-byte aligned", name); return OBF_ERR_INVALID_ARG; }
+  if (((uintptr_t)c->scale_f16 | (uintptr_t)c->zero_f16) & 1) { set_error("%s: scale and zero must be 2-byte aligned", name); return OBF_ERR_INVALID_ARG; }
+  return OBF_OK;
+}
+
+static obf_status_t check_bits(int32_t bits) {
+  if (bits != 4 && bits != 8) { set_error("bits must be 4 or 8"); return OBF_ERR_INVALID_ARG; }
+  return OBF_OK;
+}
+
+static obf_status_t check_rows(const obf_cache_rows_t* c) {
+  if (!c) { set_error("cache rows: descriptor is NULL"); return OBF_ERR_INVALID_ARG; }
+  if (c->n_samples < 1 || c->n_kv_heads < 1 || c->n_rows < 1 || c->token_stride < 1) {
+    set_error("cache rows: n_samples, n_kv_heads, n_rows, token_stride must all be >= 1");
+    return OBF_ERR_INVALID_ARG;
+  }
+  OBF_TRY(check_bits(c->bits));
+  if (c->dtype != OBF_F32 && c->dtype != OBF_BF16) { set_error("cache rows: unknown dtype %d", c->dtype); return OBF_ERR_INVALID_ARG; }
+  if (c->kv_len_all < 0 || c->kv_len_all > c->token_stride) { set_error("cache rows: kv_len_all outside [0, token_stride]"); return OBF_ERR_INVALID_ARG; }
+  if (c->len_stride < 0 || (c->len_stride > 0 && c->len_stride < c->n_kv_heads)) { set_error("cache rows: len_stride below n_kv_heads"); return OBF_ERR_INVALID_ARG; }
+  if (c->sample_stride < 0 || (c->sample_stride > 0 && c->sample_stride < (int64_t)c->n_kv_heads * c->token_stride)) {
+    set_error("cache rows: sample_stride below n_kv_heads * token_stride");
+    return OBF_ERR_INVALID_ARG;
+  }
+  const int unit = c->dtype == OBF_BF16 ? 8 : 4;
+  for (int i = 0; i < 3; ++i)
+    if (c->k_stride[i] < 0 || c->k_stride[i] % unit || c->v_stride[i] < 0 || c->v_stride[i] % unit) {
+      set_error("cache rows: strides of K and V must be multiples of 16 bytes and not negative");
+      return OBF_ERR_INVALID_ARG;
+    }
+  if (c->head_dim != 64 && c->head_dim != 128) { set_error("head_dim %d unsupported (64 or 128)", c->head_dim); return OBF_ERR_UNSUPPORTED; }
+  if (c->token_stride > kAttendMaxStride || c->n_rows > kAttendMaxStride) {
+    set_error("cache rows: token_stride or n_rows above the supported %d", kAttendMaxStride);
+    return OBF_ERR_UNSUPPORTED;
+  }
+  if ((int64_t)c->n_samples * c->n_kv_heads > 65535) { set_error("cache rows: more than 65535 heads in one call"); return OBF_ERR_UNSUPPORTED; }
+  if ((int64_t)c->n_samples * c->n_kv_heads * c->token_stride > ((int64_t)1 << 30) || (int64_t)c->n_samples * c->n_kv_heads * c->n_rows > ((int64_t)1 << 30)) {
+    set_error("cache rows: more than 2^30 rows in one call");
+    return OBF_ERR_UNSUPPORTED;
+  }
+  return OBF_OK;
+}
+
+// Strides of a tensor of rows; all three 0: contiguous.
+static void row_strides(const int64_t (&given)[3], const obf_cache_rows_t* c, long (&out)[3]) {
+  const bool any = given[0] || given[1] || given[2];
+  const long row = c->head_dim, head = row * c->n_rows;
+  out[0] = any ? given[0] : head * c->n_kv_heads; out[1] = any ? given[1] : head; out[2] = any ? given[2] : row;
+}
+
+static CacheRowsArgs rows_args(const obf_cache_rows_t* c, const void* K, const void* V, const int32_t* kv_len, const int32_t* count, const obf_codes_t* kc,
+                               const obf_codes_t* vc) {
+  CacheRowsArgs a;
+  a.x[0] = const_cast<void*>(K); a.x[1] = const_cast<void*>(V);
+  row_strides(c->k_stride, c, a.stride[0]);
+  row_strides(c->v_stride, c, a.stride[1]);
+  a.rows[0] = {kc->codes, kc->scale_f16, kc->zero_f16};
+  a.rows[1] = {vc->codes, vc->scale_f16, vc->zero_f16};
+  a.len = kv_len; a.count = count;
+  a.len_all = c->kv_len_all; a.len_stride = c->len_stride ? c->len_stride : c->n_kv_heads;
+  a.S = c->n_samples; a.H = c->n_kv_heads; a.n_rows = c->n_rows; a.token_stride = c->token_stride;
+  a.sample_rows = c->sample_stride ? c->sample_stride : (long)c->n_kv_heads * c->token_stride;
+  return a;
+}
+
+// The six arrays of a cache, of `rows` rows that certainly belong to it.
+static void code_regions(Region (&out)[6], const obf_codes_t* k, const obf_codes_t* v, const size_t rows, const size_t bytes) {
+  out[0] = {"K's codes", k->codes, rows * bytes}; out[1] = {"K's scale", k->scale_f16, rows * 2}; out[2] = {"K's zero", k->zero_f16, rows * 2};
+  out[3] = {"V's codes", v->codes, rows * bytes}; out[4] = {"V's scale", v->scale_f16, rows * 2}; out[5] = {"V's zero", v->zero_f16, rows * 2};
+}
+
+static obf_status_t check_rows_apart(const obf_cache_rows_t* c, const CacheRowsArgs& a, const obf_codes_t* kc, const obf_codes_t* vc, const bool write) {
+  const size_t es = c->dtype == OBF_BF16 ? 2 : 4, one = (size_t)a.H * a.token_stride;
+  const bool whole = a.S == 1 || (size_t)a.sample_rows == one, lens_whole = a.S == 1 || a.len_stride == a.H;
+  Region codes[6];
+  code_regions(codes, kc, vc, whole ? one * a.S : one, (size_t)c->head_dim * c->bits / 8);
+  const auto rows = [&](const int i) { return region_rows(a.S, a.H, a.n_rows, c->head_dim, a.stride[i][0], a.stride[i][1], a.stride[i][2]) * es; };
+  const size_t lens = (size_t)a.H * (lens_whole ? a.S : 1) * 4;
+  const Region k = {"K", a.x[0], rows(0)}, v = {"V", a.x[1], rows(1)}, len = {"kv_len", a.len, lens},
+               count = {write ? "n_new" : "idx", a.count, write ? lens : (size_t)a.S * a.H * a.n_rows * 4};
+  if (write) {
+    const Region ins[] = {k, v, len, count};
+    return check_apart(codes, 6, ins, 4);
+  }
+  const Region outs[] = {k, v}, ins[] = {codes[0], codes[1], codes[2], codes[3], codes[4], codes[5], len, count};
+  return check_apart(outs, 2, ins, 8);
+}
+
+struct AttendCodesPlan { AttendCodesArgs c; int tile_rows; size_t part_O, part_lse, total; };
+
+static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, bool sinks_per_head) {
+  AttendCodesPlan p;
+  AttendArgs& a = p.c.a;
+  a = attend_args(c);
+  a.n_keys = 1;
+  AttendKeys& k = a.keys[0];
+  k = attend_own(c);
+  const long own_rows = (long)a.T * a.g, d = c->head_dim;
+  p.tile_rows = 16;
+  k.row_tiles = (int)((own_rows + p.tile_rows - 1) / p.tile_rows);
+  const bool few_seen = k.window > 0 && (k.sink > 0 || !sinks_per_head);
+  const long blocks = (long)k.row_tiles * a.S * a.H, seen = few_seen ? (long)k.window + k.sink + p.tile_rows / a.g + 1 : k.stride;
+  const long rows = seen < k.stride ? seen : k.stride;
+  const bool none = rows <= 512 || (blocks >= 128 && rows <= 8 * blocks && rows <= 2048);
+  const long most_ranges = none ? 1 : (rows + 255) / 256, want = (2 * kNumCU + blocks - 1) / blocks;
+  k.nsplit = (int)(want < most_ranges ? want : most_ranges);
+  k.split0 = 0;
+  a.ranges = k.nsplit;
+  k.blocks = (int)(blocks * k.nsplit);
+  size_t at = 0;
+  p.part_O = at;
+  if (a.ranges > 1) at += (size_t)a.ranges * a.rows * d * sizeof(float);
+  p.part_lse = at;
+  if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
+  p.total = at ? at : 256;
+  return p;
+}
+
+}  // namespace obf
+
+using namespace obf;
+
+extern "C" {
+
+obf_status_t obf_cache_write(const obf_cache_rows_t* call, const void* K, const void* V, const int32_t* kv_len, const int32_t* n_new,
+                             const obf_codes_t* K_cache, const obf_codes_t* V_cache, void* stream) {
+  OBF_TRY(check_rows(call));
+  OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V));
+  OBF_TRY(check_codes("K_cache", K_cache)); OBF_TRY(check_codes("V_cache", V_cache));
+  const CacheRowsArgs a = rows_args(call, K, V, kv_len, n_new, K_cache, V_cache);
+  OBF_TRY(check_rows_apart(call, a, K_cache, V_cache, true));
+  return launch_cache_write(a, call->head_dim, call->dtype, call->bits, (hipStream_t)stream);
+}
+
+obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_cache, const obf_codes_t* V_cache, const int32_t* kv_len,
+                            const int32_t* idx, void* K, void* V, void* stream) {
+  OBF_TRY(check_rows(call));
+  OBF_TRY(check_aligned("K", K)); OBF_TRY(check_aligned("V", V));
+  OBF_TRY(check_codes("K_cache", K_cache)); OBF_TRY(check_codes("V_cache", V_cache));
+  const CacheRowsArgs a = rows_args(call, K, V, kv_len, idx, K_cache, V_cache);
+  for (int i = 0; i < 2; ++i) {
+    const int64_t strides[3] = {a.stride[i][0], a.stride[i][1], a.stride[i][2]};
+    if (rows_meet(strides, {a.S, a.H, a.n_rows}, call->head_dim)) { set_error("cache rows: rows of K and V must not overlap"); return OBF_ERR_INVALID_ARG; }
+  }
+  OBF_TRY(check_rows_apart(call, a, K_cache, V_cache, false));
+  return launch_cache_read(a, call->head_dim, call->dtype, call->bits, (hipStream_t)stream);
+}
+
+size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits) {
+  if (check_attend(call) != OBF_OK || check_bits(bits) != OBF_OK) return 0;
+  return plan_attend_codes(call, true).total;
+}
+
+obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V, const int32_t* kv_len,
+                              const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  OBF_TRY(check_attend(call));
+  OBF_TRY(check_bits(bits));
+  OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("O", O));
+  OBF_TRY(check_codes("K", K)); OBF_TRY(check_codes("V", V));
+  AttendCodesPlan p = plan_attend_codes(call, sink_len != nullptr);
+  OBF_TRY(check_attend_ws(p.total, ws, ws_bytes));
+  AttendArgs& a = p.c.a;
+  a.Q = Q; a.O = O; a.lse = lse;
+  a.part_O = (float*)((char*)ws + p.part_O);
+  a.part_lse = (float*)((char*)ws + p.part_lse);
+  AttendKeys& k = a.keys[0];
+  k.len = kv_len; k.sink_len = sink_len;
+  p.c.k = {K->codes, K->scale_f16, K->zero_f16};
+  p.c.v = {V->codes, V->scale_f16, V->zero_f16};
+  const size_t es = call->dtype == OBF_BF16 ? 2 : 4;
+  const long hq = (long)a.H * a.g;
+  Region codes[6];
+  code_regions(codes, K, V, region_cache(a, k), (size_t)call->head_dim * bits / 8);
+  const Region outs[] = {{"O", O, region_rows(a.S, hq, a.T, call->head_dim, a.os, a.oh, a.ot) * es}, {"lse", lse, (size_t)a.rows * 4}, {"the workspace", ws, p.total}};
+  const Region ins[] = {{"Q", Q, region_rows(a.S, hq, a.T, call->head_dim, a.qs, a.qh, a.qt) * es}, codes[0], codes[1], codes[2], codes[3], codes[4], codes[5],
+                        {"kv_len", kv_len, region_lens(a, k) * 4}, {"sink_len", sink_len, region_lens(a, k) * 4}};
+  OBF_TRY(check_apart(outs, 3, ins, 9));
+  const hipStream_t st = (hipStream_t)stream;
+  OBF_TRY(launch_attend_codes_few(p.c, p.tile_rows, call->head_dim, call->dtype, bits, st));
+  return a.ranges > 1 ? launch_attend_join(a, call->head_dim, call->dtype, st) : OBF_OK;
+}
+
+}  // extern "C"

@@ -238,7 +238,7 @@ inline Workspace carve(const Dims& m, int max_budget, int rank) {
 
 enum Stage {
   ST_SCORE_STATS = 0, ST_SCORE_LSE, ST_SCORE_MASS, ST_SELECT, ST_REFINE, ST_GATHER, ST_KEEP_CERT, ST_KEEP_BASIS, ST_DEL_STATS,
-  ST_FINALIZE, ST_BASIS_STATS, ST_ATTEND, ST_ATTEND_JOIN, ST_ATTEND_MASS, ST_EVICT, ST_COUNT
+  ST_FINALIZE, ST_BASIS_STATS, ST_ATTEND, ST_ATTEND_JOIN, ST_ATTEND_MASS, ST_EVICT, ST_CACHE_WRITE, ST_CACHE_READ, ST_COUNT
 };
 
 // Entry points (inside namespace obf, or with it opened): leave with the status of a failed step; refuse a NULL argument.

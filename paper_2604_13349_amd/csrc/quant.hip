@@ -1,47 +1,14 @@
 // Post-hoc int8 / int4 codes for relay rows (the "+ int8" rows of App. E's comparison table).  The paper names no
 // scheme; the one taken here reproduces its ratios: every row carries its own asymmetric code and two half-precision
 // numbers, zero = fp16(min x), scale = fp16((max x - min x) / L), L = 2^bits - 1, q = clamp(rint((x - zero) / scale), 0, L).
-// The integer decision is taken in single precision with individually rounded subtract, divide and round-to-even.
 //
 // Both directions are bound by memory: a lane handles 16 consecutive columns, so that a row of 128 is eight lanes and a wave moves
 // eight rows (sixteen at head_dim 64); rows come and go in 16-byte pieces, the codes of a lane in one piece of 16 (int8) or 8 bytes.
 // A lane of 16 columns also pays for the row's minimum, maximum, scale and zero once per 16 values.  366k rows of 128 bf16 values, int8:
 // 25 us to codes and 29 back (5.4 and 4.9 TB/s; 97 and 108 us with a wave per row and a thread per value).
-#include <hip/hip_fp16.h>
-#include "common.hpp"
+#include "codes.hpp"
 
 namespace obf {
-
-constexpr int QT_THREADS = 256;
-constexpr int QT_COLS = 16;              // columns per lane
-
-// 16 consecutive elements (16-byte aligned) as floats, and back
-__device__ __forceinline__ void load16(const uint16_t* __restrict__ p, float (&o)[QT_COLS]) {
-  const uint4 v[2] = {((const uint4*)p)[0], ((const uint4*)p)[1]};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) { o[8 * i + 2 * k] = __uint_as_float(w[k] << 16); o[8 * i + 2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
-  }
-}
-__device__ __forceinline__ void load16(const float* __restrict__ p, float (&o)[QT_COLS]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { const float4 v = ((const float4*)p)[i]; o[4 * i] = v.x; o[4 * i + 1] = v.y; o[4 * i + 2] = v.z; o[4 * i + 3] = v.w; }
-}
-__device__ __forceinline__ void store16(uint16_t* __restrict__ p, const float (&x)[QT_COLS]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    uint32_t w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = (uint32_t)float_to_bf16_bits(x[8 * i + 2 * k]) | ((uint32_t)float_to_bf16_bits(x[8 * i + 2 * k + 1]) << 16);
-    ((uint4*)p)[i] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
-__device__ __forceinline__ void store16(float* __restrict__ p, const float (&x)[QT_COLS]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) ((float4*)p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-}
 
 template <typename T, int D, int BITS>
 __global__ __launch_bounds__(QT_THREADS) void k_quant_rows(const T* __restrict__ X, long n_rows, uint8_t* __restrict__ codes,
@@ -52,43 +19,11 @@ __global__ __launch_bounds__(QT_THREADS) void k_quant_rows(const T* __restrict__
   if (row >= n_rows) return;                                   // all lanes of a row together
   float x[QT_COLS];
   load16(X + row * D + part * QT_COLS, x);
-  float lo = x[0], hi = x[0];
-#pragma unroll
-  for (int i = 1; i < QT_COLS; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
-#pragma unroll
-  for (int off = LPR / 2; off > 0; off >>= 1) { lo = fminf(lo, __shfl_xor(lo, off)); hi = fmaxf(hi, __shfl_xor(hi, off)); }
-  constexpr float L = (float)((1 << BITS) - 1);
-  const __half zh = __float2half_rn(lo), sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), L));
-  const float z = __half2float(zh), s = __half2float(sh);
-  uint32_t q[QT_COLS];
-  if (s > 0.f && s < INFINITY && fabsf(z) < INFINITY) {
-    // The correctly rounded quotient from the row's reciprocal (Markstein): with r = RN(1/s), s of eleven significant bits, a quotient
-    // within an ulp becomes the correctly rounded one by one residual step; the first step only brings it there.
-    const float r = __frcp_rn(s);
-#pragma unroll
-    for (int i = 0; i < QT_COLS; ++i) {
-      const float t = __fsub_rn(x[i], z);
-      float y = __fmul_rn(t, r);
-      y = __fmaf_rn(__fmaf_rn(-y, s, t), r, y);
-      y = __fmaf_rn(__fmaf_rn(-y, s, t), r, y);
-      q[i] = (uint32_t)fminf(fmaxf(rintf(y), 0.f), L);
-    }
-  } else {                                                     // a constant row, or values past the half-precision range
-#pragma unroll
-    for (int i = 0; i < QT_COLS; ++i)
-      q[i] = (s > 0.f) ? (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], z), s)), 0.f), L) : 0u;
-  }
   uint32_t w[QT_COLS * BITS / 32];
-#pragma unroll
-  for (int k = 0; k < QT_COLS * BITS / 32; ++k) {              // little-endian: the even column of an int4 pair in the low half
-    w[k] = 0u;
-#pragma unroll
-    for (int i = 0; i < 32 / BITS; ++i) w[k] |= q[k * (32 / BITS) + i] << (i * BITS);
-  }
-  uint8_t* o = codes + row * (D * BITS / 8) + part * (QT_COLS * BITS / 8);
-  if constexpr (BITS == 8) *(uint4*)o = make_uint4(w[0], w[1], w[2], w[3]);
-  else *(uint2*)o = make_uint2(w[0], w[1]);
-  if (part == 0) { scale[row] = __half_as_ushort(sh); zero[row] = __half_as_ushort(zh); }
+  uint16_t sh, zh;
+  encode16<LPR, BITS>(x, w, sh, zh);
+  store_codes16<BITS>(codes + row * (D * BITS / 8) + part * (QT_COLS * BITS / 8), w);
+  if (part == 0) { scale[row] = sh; zero[row] = zh; }
 }
 
 template <typename T, int D, int BITS>
@@ -98,14 +33,10 @@ __global__ __launch_bounds__(QT_THREADS) void k_dequant_rows(const uint8_t* __re
   const long row = (long)blockIdx.x * (QT_THREADS / LPR) + threadIdx.x / LPR;
   const int part = threadIdx.x % LPR;
   if (row >= n_rows) return;
-  const uint8_t* c = codes + row * (D * BITS / 8) + part * (QT_COLS * BITS / 8);
   uint32_t w[QT_COLS * BITS / 32];
-  if constexpr (BITS == 8) { const uint4 v = *(const uint4*)c; w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
-  else { const uint2 v = *(const uint2*)c; w[0] = v.x; w[1] = v.y; }
-  const float s = __half2float(__ushort_as_half(scale[row])), z = __half2float(__ushort_as_half(zero[row]));
+  load_codes16<BITS>(codes + row * (D * BITS / 8) + part * (QT_COLS * BITS / 8), w);
   float x[QT_COLS];
-#pragma unroll
-  for (int i = 0; i < QT_COLS; ++i) x[i] = fmaf(s, (float)((w[i * BITS / 32] >> (i * BITS % 32)) & ((1u << BITS) - 1u)), z);
+  decode16<BITS>(w, scale[row], zero[row], x);
   store16(X + row * D + part * QT_COLS, x);
 }
 

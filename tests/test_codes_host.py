@@ -1,0 +1,156 @@
+"""Host side of the operators of a cache held in codes, without a GPU: refusals before anything is enqueued; the 64-bit definitions on cases with a known answer."""
+import ctypes as C
+import math
+import os
+
+import pytest
+import torch
+
+from paper_2604_13349_amd import binding as B
+from tests import attend_ref
+from tests import codes_ref as R
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.lib_path()):
+        from paper_2604_13349_amd import build
+        build.build(verbose=False)
+    return B.load_library()
+
+
+SIZE = {"n_samples": 2, "n_kv_heads": 3, "head_dim": 128, "bits": 4, "dtype": B.OBF_BF16, "n_rows": 5, "token_stride": 40, "kv_len_all": 40}
+CODES = ("K.codes", "K.scale", "K.zero", "V.codes", "V.scale", "V.zero")
+# addresses that are never dereferenced: every call below fails on the host
+AT = {name: (i + 1) << 30 for i, name in enumerate(("K", "V", "kv_len", "per_head") + CODES)}
+
+
+def _rows(**kw):
+    c = B._CacheRows(*[SIZE[k] for k in SIZE])
+    for k, v in kw.items():
+        setattr(c, k, (C.c_int64 * 3)(*v) if isinstance(v, tuple) else v)
+    return c
+
+
+def _codes(at, which):
+    return B._Codes(*[at[f"{which}.{x}"] for x in ("codes", "scale", "zero")])
+
+
+def _call(lib, kind, c, at=AT):
+    k, v = _codes(at, "K"), _codes(at, "V")
+    p = {n: C.c_void_p(a) if a else None for n, a in at.items()}
+    d = C.byref(c) if c is not None else None
+    if kind == "write":
+        rc = lib.obf_cache_write(d, p["K"], p["V"], p["kv_len"], p["per_head"], C.byref(k), C.byref(v), None)
+    else:
+        rc = lib.obf_cache_read(d, C.byref(k), C.byref(v), p["kv_len"], p["per_head"], p["K"], p["V"], None)
+    return rc, lib.obf_last_error().decode()
+
+
+REFUSED = [
+    (dict(n_samples=0), 1, "n_samples"), (dict(n_kv_heads=0), 1, "n_kv_heads"), (dict(n_rows=0), 1, "n_rows"), (dict(token_stride=0, kv_len_all=0), 1, "token_stride"),
+    (dict(bits=3), 1, "bits"), (dict(dtype=2), 1, "dtype"), (dict(kv_len_all=41), 1, "kv_len_all"), (dict(kv_len_all=-1), 1, "kv_len_all"),
+    (dict(len_stride=2), 1, "len_stride"), (dict(len_stride=-1), 1, "len_stride"), (dict(sample_stride=119), 1, "sample_stride"),
+    (dict(k_stride=(1920, 640, 4)), 1, "16 bytes"), (dict(v_stride=(1920, -8, 128)), 1, "16 bytes"),
+    (dict(head_dim=96), 2, "head_dim"), (dict(token_stride=(1 << 24) + 1), 2, "token_stride"), (dict(n_rows=(1 << 24) + 1), 2, "n_rows"),
+    (dict(n_samples=21846), 2, "65535"), (dict(n_samples=1 << 14, token_stride=1 << 15, kv_len_all=0), 2, "2^30"), (dict(n_samples=1 << 14, n_rows=1 << 15), 2, "2^30"),
+]
+
+
+@pytest.mark.parametrize("kind", ["write", "read"])
+@pytest.mark.parametrize("change,status,word", REFUSED, ids=[f"{w}{i}" for i, (_, _, w) in enumerate(REFUSED)])
+def test_refused_descriptors(lib, kind, change, status, word):
+    rc, msg = _call(lib, kind, _rows(**change))
+    assert rc == status and word in msg
+
+
+@pytest.mark.parametrize("kind", ["write", "read"])
+def test_refused_pointers(lib, kind):
+    assert _call(lib, kind, None)[0] == 1
+    for name in ("K", "V") + CODES:
+        assert _call(lib, kind, _rows(), {**AT, name: 0})[0] == 1, name
+        assert _call(lib, kind, _rows(), {**AT, name: AT[name] + (8 if name in ("K", "V") or "codes" in name else 1)})[0] == 1, name
+    f = lib.obf_cache_write
+    k = _codes(AT, "K")
+    assert f(C.byref(_rows()), AT["K"], AT["V"], None, None, None, C.byref(k), None) == 1
+    assert f(C.byref(_rows()), AT["K"], AT["V"], None, None, C.byref(k), None, None) == 1
+
+
+def test_outputs_that_meet_inputs_or_one_another_are_refused(lib):
+    heads = 6
+    size = {"K": heads * 5 * 256, "V": heads * 5 * 256, "kv_len": heads * 4, "per_head": heads * 4}
+    size.update({x: heads * 40 * (64 if "codes" in x else 2) for x in CODES})
+    for kind, outs in (("write", CODES), ("read", ("K", "V"))):
+        if kind == "read":
+            size["per_head"] = heads * 5 * 4
+        for o in outs:
+            for other in AT:
+                if other == o:
+                    continue
+                for at in (AT[other], AT[other] + (size[other] - 1) // 16 * 16, AT[other] - (size[o] - 1) // 16 * 16):
+                    rc, msg = _call(lib, kind, _rows(), {**AT, o: at})
+                    assert rc == 1 and "overlap" in msg, (kind, o, other)
+
+
+def test_rows_read_into_rows_that_overlap_are_refused(lib):
+    for s in ((0, 640, 128), (1920, 632, 128), (1920, 640, 64), (128, 128, 128), (640, 1272, 128)):
+        for name in ("k_stride", "v_stride"):
+            rc, msg = _call(lib, "read", _rows(**{name: s}))
+            assert rc == 1 and "overlap" in msg, s
+
+
+def test_refused_attention(lib):
+    at = {**AT, "Q": 30 << 30, "O": 31 << 30, "lse": 32 << 30, "ws": 33 << 30, "sink_len": 34 << 30}
+
+    def call(bits=4, ws_bytes=1 << 29, c=None, K=True, **moved):
+        a = {**at, **moved}
+        d = c if c is not None else B._Attend(2, 3, 4, 128, 1, 40, B.OBF_BF16, 1, 0, 0, 40, 0, 0)
+        k, v = _codes(a, "K"), _codes(a, "V")
+        return lib.obf_attend_codes(C.byref(d), bits, a["Q"], C.byref(k) if K else None, C.byref(v), a["kv_len"], a["sink_len"], a["O"], a["lse"], a["ws"], ws_bytes, None)
+
+    for kw in [dict(bits=2), dict(K=False), dict(Q=0), dict(O=0), dict(ws=0), dict(Q=at["Q"] + 8), dict(O=at["O"] + 8), dict(ws=at["ws"] + 16)] + \
+              [{x: 0} for x in CODES] + [{x: at[x] + 1} for x in CODES]:
+        assert call(**kw) == 1, kw
+    for change, status in ((dict(n_samples=0), 1), (dict(window=5, causal=0), 1), (dict(head_dim=96), 2), (dict(group=129), 2), (dict(n_queries=(1 << 20) + 1), 2)):
+        d = B._Attend(2, 3, 4, 128, 1, 40, B.OBF_BF16, 1, 0, 0, 40, 0, 0)
+        for k, v in change.items():
+            setattr(d, k, v)
+        assert call(c=d) == status
+        assert lib.obf_attend_codes_workspace_bytes(C.byref(d), 4) == 0
+    long = B._Attend(1, 2, 4, 128, 1, 40000, B.OBF_BF16, 1, 0, 0, 40000, 0, 0)
+    need = lib.obf_attend_codes_workspace_bytes(C.byref(long), 4)
+    assert need > 256 and call(c=long, ws_bytes=need - 1) == 3 and lib.obf_attend_codes_workspace_bytes(C.byref(long), 5) == 0
+    for o in ("O", "lse", "ws"):
+        for other in at:
+            if other not in (o, "V", "per_head") and not (other == "K"):
+                assert call(**{o: at[other]}, ws_bytes=256) == 1, (o, other)
+                assert "overlap" in lib.obf_last_error().decode()
+
+
+def test_tensors_must_be_on_a_gpu_and_need_no_gradient():
+    u, f = torch.zeros((1, 1, 4, 32), dtype=torch.uint8), torch.zeros((1, 1, 4), dtype=torch.float16)
+    with pytest.raises(ValueError, match="GPU"):
+        B.CodeCache(u, f, f, u, f, f, d=64, bits=4)
+    x = torch.zeros((1, 1, 1, 64))
+    g = x.clone().requires_grad_()
+    for call in (lambda: B.attend_codes(g, None), lambda: B.cache_write(None, g, x), lambda: B.cache_write(None, x, g)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+
+
+def test_definition_on_known_answers():
+    """The code's values by hand; over exact codes the attention is that of the values."""
+    q, s, z = R.quantise(torch.tensor([[1.0, 2.0, 8.5, 16.0]]), 4)
+    assert q.tolist() == [[0, 1, 8, 15]] and s.item() == 1.0 and z.item() == 1.0          # (7.5: to even)
+    assert R.quantise(torch.full((1, 8), 1.5), 8)[0].eq(0).all()
+    codes = torch.arange(64, dtype=torch.uint8).view(1, 1, 1, 64) % 16
+    assert torch.equal(R.unpack(R.pack(codes, 4), 4), codes) and R.pack(codes, 4)[0, 0, 0, :2].tolist() == [0x10, 0x32]
+    gen = torch.Generator().manual_seed(0)
+    K, V = ((torch.randint(0, 16, (1, 2, 30, 64), generator=gen).to(torch.uint8), torch.rand((1, 2, 30), generator=gen).half(), torch.randn((1, 2, 30), generator=gen).half())
+            for _ in range(2))
+    Q = torch.randn((1, 4, 3, 64), generator=gen)
+    n = torch.tensor([[30, 2]])
+    O, lse, tO, tl = R.attend(Q, K, V, 4, n, window=9, sink=2)
+    O2, lse2, *_ = attend_ref.attend(Q, R.values(*K), R.values(*V), n, window=9, sink=2)
+    assert torch.allclose(O, O2) and torch.equal(lse == -math.inf, lse2 == -math.inf) and torch.allclose(lse[lse > -9e9], lse2[lse2 > -9e9])
+    assert (lse[0, 2:, 0] == -math.inf).all() and (tO >= 0).all() and (tl >= 0).all()
