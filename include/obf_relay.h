@@ -470,10 +470,12 @@ obf_status_t obf_cache_write(const obf_cache_rows_t* call, const void* K, const 
 obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_cache, const obf_codes_t* V_cache, const int32_t* kv_len,
                             const int32_t* idx, void* K, void* V, void* stream);
 
-/* obf_attend over a cache held in codes (without accumulated weights); call->dtype is that of Q and O.  The rows enter as zero + scale * q:
- * fp32, and bf16 up to 32 query rows (n_queries * group) per KV head, unrounded, with softmax weights times scale of 22 and 11 bits; bf16
- * above 32 query rows: rounded to half precision (values past its range to the largest one), with weights of 11 bits.
- * Rows at and behind a head's length are not read.  K and V name the codes' arrays, which are inputs. */
+/* obf_attend over a cache held in codes (without accumulated weights); call->dtype is that of Q and O.  A row stands for zero + scale * q,
+ * unrounded; sums and statistics are single precision, the codes, and the queries under a power of two per row, enter the products as half-precision
+ * numbers (fp32 queries as two, 22 bits).  The weights, times the rows' scales, have 11 bits, with fp32 22.  With bf16 and more than 32 query rows
+ * (n_queries * group) per KV head V's values enter rounded to half precision, those past its range as the largest ones.
+ * Rows at and behind a head's length are not read.  K and V name the codes' arrays, which are inputs.  The workspace holds half-precision copies
+ * of the cache's rows where there are 2^11 query rows per KV head or about as many. */
 size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits);
 obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V,
                               const int32_t* kv_len, const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes,

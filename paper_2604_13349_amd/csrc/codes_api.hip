@@ -94,9 +94,9 @@ static obf_status_t check_rows_apart(const obf_cache_rows_t* c, const CacheRowsA
   return check_apart(outs, 2, ins, 8);
 }
 
-struct AttendCodesPlan { AttendCodesArgs c; int tile_rows; size_t part_O, part_lse, total; };
+struct AttendCodesPlan { AttendCodesArgs c; bool tile, rows; int waves; size_t part_O, part_lse, rows_k, rows_v, numbers, bad, total; };
 
-static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, bool sinks_per_head) {
+static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool sinks_per_head) {
   AttendCodesPlan p;
   AttendArgs& a = p.c.a;
   a = attend_args(c);
@@ -104,14 +104,27 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, bool sinks_per_h
   AttendKeys& k = a.keys[0];
   k = attend_own(c);
   const long own_rows = (long)a.T * a.g, d = c->head_dim;
-  p.tile_rows = 16;
-  k.row_tiles = (int)((own_rows + p.tile_rows - 1) / p.tile_rows);
+  // bf16, more than 32 rows: the kernel whose rows share the values that it makes of the codes; 17 to 32: two workgroups read the codes (us, as one of 32 rows: 16 x 8
+  // heads of 4000 rows 30 - 33, 4 x 8 of 1000 13 - 15, 16 x 8 of 8192 to 32768 135 - 139).
+  p.tile = c->dtype == OBF_BF16 && own_rows > kAttendFewRows;
+  const int tile_rows = p.tile ? kAttendTileRows : kCodesFewRows;
+  k.row_tiles = (int)((own_rows + tile_rows - 1) / tile_rows);
   const bool few_seen = k.window > 0 && (k.sink > 0 || !sinks_per_head);
-  const long blocks = (long)k.row_tiles * a.S * a.H, seen = few_seen ? (long)k.window + k.sink + p.tile_rows / a.g + 1 : k.stride;
+  const long blocks = (long)k.row_tiles * a.S * a.H, seen = few_seen ? (long)k.window + k.sink + tile_rows / a.g + 1 : k.stride;
   const long rows = seen < k.stride ? seen : k.stride;
-  const bool none = rows <= 512 || (blocks >= 128 && rows <= 8 * blocks && rows <= 2048);
-  const long most_ranges = none ? 1 : (rows + 255) / 256, want = (2 * kNumCU + blocks - 1) / blocks;
-  k.nsplit = (int)(want < most_ranges ? want : most_ranges);
+  // Ranges where the sets do not fill the chip; none for short caches, and where there is a workgroup per compute unit for caches that are not long: their join would take
+  // longer (us, ranges and none: 256 sets of 1000 to 2048 rows 22 - 18, of 1000 to 4096 in 8 bits 47 - 43, 24 x 20 tiles of many rows 64 - 51).
+  const bool none = rows <= 512 || (p.tile ? blocks >= kNumCU : (blocks >= 128 && rows <= 1024) || (blocks >= kNumCU && rows <= 4096));
+  const int per_cu = p.tile ? 2 : few_codes_per_cu(c->head_dim, c->dtype == OBF_F32, bits);
+  // At least 512 rows a range, 256 where there are few sets; 32 ranges at most, whose join takes as long as what more of them save (us, 8 heads of 32000 rows, 32, 64 and 128
+  // ranges 19 - 24 - 32; of 4000, 8 and 16 ranges 12.7 - 11.4; 64 heads of 2000, 4 and 8 ranges 14.1 - 16.9).
+  const long least = blocks * ((rows + 511) / 512) < kNumCU / 2 ? 256 : 512;
+  const long most = none ? 1 : (rows + least - 1) / least, want = (per_cu * kNumCU + blocks - 1) / blocks;
+  const long ranges = most < want ? most : want;
+  k.nsplit = (int)(p.tile || ranges < 32 ? ranges : 32);
+  p.waves = 8;
+  // Long ranges are twice as many of four waves, which even out heads of different lengths (16 x 8 heads of 8192 to 32768 rows: 84 us for 87).
+  if (!p.tile && k.nsplit > 1 && rows >= 4096L * k.nsplit) { p.waves = 4; k.nsplit *= 2; }
   k.split0 = 0;
   a.ranges = k.nsplit;
   k.blocks = (int)(blocks * k.nsplit);
@@ -120,6 +133,18 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, bool sinks_per_h
   if (a.ranges > 1) at += (size_t)a.ranges * a.rows * d * sizeof(float);
   p.part_lse = at;
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
+  // Values made once for all workgroups of a head
+  p.rows = p.tile && k.row_tiles >= 16;
+  p.c.flags = (k.stride + kCodeFlagRows - 1) / kCodeFlagRows;
+  const size_t values = ((size_t)a.S * a.H * k.stride * d * sizeof(uint16_t) + 255) & ~(size_t)255;
+  p.rows_k = at;
+  if (p.rows) at += values;
+  p.rows_v = at;
+  if (p.rows) at += values;
+  p.numbers = at;
+  if (p.rows) at += ((size_t)a.S * a.H * k.stride * sizeof(uint2) + 255) & ~(size_t)255;
+  p.bad = at;
+  if (p.rows) at += ((size_t)a.S * a.H * p.c.flags + 255) & ~(size_t)255;
   p.total = at ? at : 256;
   return p;
 }
@@ -156,7 +181,7 @@ obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_c
 
 size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits) {
   if (check_attend(call) != OBF_OK || check_bits(bits) != OBF_OK) return 0;
-  return plan_attend_codes(call, true).total;
+  return plan_attend_codes(call, bits, true).total;
 }
 
 obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V, const int32_t* kv_len,
@@ -165,12 +190,16 @@ obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void
   OBF_TRY(check_bits(bits));
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("O", O));
   OBF_TRY(check_codes("K", K)); OBF_TRY(check_codes("V", V));
-  AttendCodesPlan p = plan_attend_codes(call, sink_len != nullptr);
+  AttendCodesPlan p = plan_attend_codes(call, bits, sink_len != nullptr);
   OBF_TRY(check_attend_ws(p.total, ws, ws_bytes));
   AttendArgs& a = p.c.a;
   a.Q = Q; a.O = O; a.lse = lse;
   a.part_O = (float*)((char*)ws + p.part_O);
   a.part_lse = (float*)((char*)ws + p.part_lse);
+  p.c.rows_k = p.rows ? (uint16_t*)((char*)ws + p.rows_k) : nullptr;
+  p.c.rows_v = p.rows ? (uint16_t*)((char*)ws + p.rows_v) : nullptr;
+  p.c.numbers = p.rows ? (uint2*)((char*)ws + p.numbers) : nullptr;
+  p.c.bad = p.rows ? (uint8_t*)ws + p.bad : nullptr;
   AttendKeys& k = a.keys[0];
   k.len = kv_len; k.sink_len = sink_len;
   p.c.k = {K->codes, K->scale_f16, K->zero_f16};
@@ -184,7 +213,8 @@ obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void
                         {"kv_len", kv_len, region_lens(a, k) * 4}, {"sink_len", sink_len, region_lens(a, k) * 4}};
   OBF_TRY(check_apart(outs, 3, ins, 9));
   const hipStream_t st = (hipStream_t)stream;
-  OBF_TRY(launch_attend_codes_few(p.c, p.tile_rows, call->head_dim, call->dtype, bits, st));
+  if (p.tile) OBF_TRY(launch_attend_codes_tile(p.c, call->head_dim, bits, st));
+  else OBF_TRY(launch_attend_codes_few(p.c, p.waves, call->head_dim, call->dtype, bits, st));
   return a.ranges > 1 ? launch_attend_join(a, call->head_dim, call->dtype, st) : OBF_OK;
 }
 

@@ -2,10 +2,11 @@
 
 Bounds, as in attend_ref (u = 2^-24), with a row's two numbers taken apart, since the kernels sum scale times codes and zeros separately: a logit is off by at most
 dx = (d + 8) u sum_c |q_c| (|s| c + |z|) / sqrt(d), a weight by a factor of 1 + 2 dx + (n + 16) u.  Beside that
-  few rows    fp32 queries enter as two parts of 11 bits (2^-22 of an element), every element with 2^-25 beside a largest of 2^14 or more, 2^4 of that where its
-              code stands four bits higher (2^-35 of the largest); weights times scale with 2^-11 (bf16) or 2^-22 (fp32) and 2^-25 beside a largest of 2^7 or more
-              (2^-32 of the largest, in which a scale of 0 counts as 2^-24), times codes up to L
-  many rows   the row's values enter rounded to half precision, 2^-11 of the value and 2^-25, weights with 2^-11 and 2^-32 of the largest
+  few rows    fp32 queries enter as two parts of 11 bits (2^-22 of an element), every element with 2^-25 beside a largest of 2^14 or more (2^-39 of it); weights
+              times scale with 2^-11 (bf16) or 2^-22 (fp32) and 2^-25 beside a largest of 2^7 or more (2^-32 of the largest, in which a scale of 0 counts as
+              2^-24), times codes up to L; with bf16, sums of V's codes drop what lies 2^-20 below a largest product
+  many rows   queries with 2^-39 of the largest element, their sum with 2^-33 of it and 2^-25 beside one of up to 2^8 times 2^14 (2^-24 of the largest element, for
+              values up to |zero| + 2^(bits - 1) |scale|); V's values rounded to half precision, 2^-11 of the value and 2^-25, weights with 2^-11 and 2^-32 of the largest
 The result is then rounded once to its type."""
 import math
 
@@ -65,13 +66,15 @@ def attend(Q, K, V, bits, kv_len, causal=True, window=0, sink=0, sink_len=None):
                 qa = q.abs()
                 dx = (d + 8) * U * (qa @ k_abs.t())
                 if many:
-                    dx = dx + qa @ (2.0 ** -11 * k.abs() + 2.0 ** -25).t()
+                    middle = values(torch.full_like(K[0][s, h, at][:, :1], 1 << (bits - 1)), K[1][s, h, at].abs(), K[2][s, h, at].abs())[:, 0]
+                    dx = dx + (2.0 ** -39 * d + 2.0 ** -24) * qa.amax(dim=1)[:, None] * middle
+                    dx = dx + (d + 8) * U * qa.sum(dim=1)[:, None] * middle
                     p_eps, spare = 2.0 ** -11, 2.0 ** -32 * w.amax(dim=1)[:, None] * v.abs().sum(dim=0)
                     off = w @ (2.0 ** -11 * v.abs() + 2.0 ** -25)
                 else:
                     codes = values(K[0][s, h, at], K[1][s, h, at].abs(), torch.zeros_like(K[2][s, h, at]))
-                    dx = dx + (2.0 ** -22 if f32 else 0.0) * (qa @ codes.t()) + 2.0 ** -35 * qa.amax(dim=1)[:, None] * codes.sum(dim=1)
-                    p_eps = 2.0 ** -22 if f32 else 2.0 ** -11
+                    dx = dx + (2.0 ** -22 if f32 else 0.0) * (qa @ codes.t()) + 2.0 ** -39 * qa.amax(dim=1)[:, None] * codes.sum(dim=1)
+                    p_eps = 2.0 ** -22 if f32 else 2.0 ** -11 + 2.0 ** -20
                     vs = V[1][s, h, at].double().abs().clamp(min=2.0 ** -24)
                     spare, off = 2.0 ** -32 * L * at.numel() * (w * vs).amax(dim=1)[:, None], 0.0
                 dx = (dx.amax(dim=1) / math.sqrt(d))[:, None]

@@ -359,16 +359,27 @@ def test_scales_of_all_sizes_in_one_head(dtype, T, bits):
 
 
 @pytest.mark.parametrize("dtype,T", [(BF, 1), (BF, 40), (F32, 3)])
-def test_a_row_of_large_scale_that_no_query_looks_at(dtype, T):
-    """Values of 10^4 beside values of 10^-3, the large ones under logits 60 below the others: they must not take the others' precision."""
+@pytest.mark.parametrize("factor", [5e5, 1e7])
+def test_a_row_of_large_scale_that_no_query_looks_at(dtype, T, factor):
+    """Values of 10^4 beside values of 10^-3, the large ones under logits 60 below the others: they must not take the others' precision.  (With the larger factor
+    they lie past the half-precision range, zeros of -inf that every query sees: no finite number comes out.)"""
     Q, K, V = _make(14, dtype, 128, 1, 1, 2, T, 100)
     q = torch.randn(128, generator=torch.Generator().manual_seed(1))
     Q[:] = (q + 0.01 * torch.randn(Q.shape, generator=torch.Generator().manual_seed(2))).to(dtype)
     V = (V.float() * 1e-3).to(dtype)
     for j in (0, 31, 50):
         K[0, 0, j] = (-6.0 * q).to(dtype)
-        V[0, 0, j] = (V[0, 0, j].float() * 1e7).to(dtype)
-    _attend_and_check(Q, K, V, 4, torch.tensor([[100]], dtype=torch.int32), causal=False)
+        V[0, 0, j] = (V[0, 0, j].float() * factor).to(dtype)
+    kv_len = torch.tensor([[100]], dtype=torch.int32)
+    k, v = R.quantise(K, 4), R.quantise(V, 4)
+    if factor < 1e6:
+        _attend_and_check(Q, k, v, 4, kv_len, causal=False)
+    else:
+        assert torch.isinf(v[2]).any()
+        _, lse, _, tl = R.attend(Q, k, v, 4, kv_len, causal=False)
+        o = _b().attend_codes(Q.cuda(), _cache(k, v, 4, 128), causal=False)
+        assert not torch.isfinite(o["O"].float()).any()
+        _check("lse", o["lse"], lse, tl)
 
 
 def test_rows_at_the_ends_of_the_half_precision_range():
