@@ -2,16 +2,33 @@
 //
 // The arithmetic is that of the row code (codes.hpp); what these kernels add is the addressing: rows at the strides of a projection's output,
 // a number of them per head, behind what the head holds, and back by row numbers.  16 columns a lane, keys and values in one launch.
+//
+// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 32 (4.4 and 5.3 TB/s), the kept rows of 36 x 8 heads (800 to
+// 1229), 8 bits, in 50 and back in 50, 1229 of 8192 rows by their numbers in 60 (3.8: a row's 64 bytes come as the 128 of its line).  One row a lane, with lengths loaded
+// beside it: 46, 36, 54, 55 and 61; four rows: 40, 33, 52, 54 and 66.  Stores that bypass the caches double the time of the way back.
 #include "attend_codes.hpp"
 #include "codes.hpp"
 
 namespace obf {
 
-// Row `at` of the launch's rows: sample, head and number.
+// Head and rows of a lane: of PASSES rows, PER apart, the first.  CHUNKED, many rows per head: a workgroup takes PER * PASSES rows of one head, so that lengths and counts are
+// scalars and a lane has the loads of all its rows in flight; otherwise rows of all heads one after another, one a lane.
 struct CacheRow { int s, h, t; };
-__device__ __forceinline__ CacheRow cache_row(const CacheRowsArgs& a, const uint32_t at) {
-  const uint32_t set = at / (uint32_t)a.n_rows, s = set / (uint32_t)a.H;
-  return {(int)s, (int)(set - s * a.H), (int)(at - set * a.n_rows)};
+template <bool CHUNKED, int PER, int PASSES> __device__ __forceinline__ CacheRow cache_row(const CacheRowsArgs& a) {
+  const uint32_t heads = a.H, sets = (uint32_t)a.S * heads, in = threadIdx.x / (QT_THREADS / PER);
+  uint32_t set, t;
+  if (CHUNKED) {
+    const uint32_t chunk = blockIdx.x / sets;
+    set = blockIdx.x - chunk * sets;
+    t = chunk * (PER * PASSES) + in;
+  } else {
+    const uint32_t at = blockIdx.x * PER + in;
+    set = at / (uint32_t)a.n_rows;
+    t = set < sets ? at - set * a.n_rows : a.n_rows;
+    set = min(set, sets - 1);
+  }
+  const uint32_t s = set / heads;
+  return {(int)s, (int)(set - s * heads), (int)t};
 }
 // Rows that the head holds; none where that is no length.
 __device__ __forceinline__ int cache_len(const CacheRowsArgs& a, const CacheRow r) {
@@ -19,52 +36,81 @@ __device__ __forceinline__ int cache_len(const CacheRowsArgs& a, const CacheRow 
   return n < 0 || n > a.token_stride ? 0 : n;
 }
 
-template <typename T, int D, int BITS>
+template <typename T, int D, int BITS, bool CHUNKED, int PASSES>
 __global__ __launch_bounds__(QT_THREADS) void k_cache_write(const CacheRowsArgs a) {
-  constexpr int LPR = D / QT_COLS, BYTES = D * BITS / 8;
-  const uint32_t at = blockIdx.x * (QT_THREADS / LPR) + threadIdx.x / LPR;
+  constexpr int LPR = D / QT_COLS, BYTES = D * BITS / 8, PER = QT_THREADS / LPR;
   const int part = threadIdx.x % LPR, which = blockIdx.y;
-  if (at >= (uint32_t)a.S * a.H * a.n_rows) return;             // all lanes of a row together, here and below
-  const CacheRow r = cache_row(a, at);
+  const CacheRow r = cache_row<CHUNKED, PER, PASSES>(a);
   const int m = a.count ? a.count[(size_t)r.s * a.len_stride + r.h] : a.n_rows;
-  if (m > a.n_rows || r.t >= m) return;
-  const int j = cache_len(a, r) - m + r.t;
-  if (j < 0) return;
-  float x[QT_COLS];
-  load16((const T*)a.x[which] + r.s * a.stride[which][0] + r.h * a.stride[which][1] + r.t * a.stride[which][2] + part * QT_COLS, x);
-  uint32_t w[QT_COLS * BITS / 32];
-  uint16_t scale, zero;
-  encode16<LPR, BITS>(x, w, scale, zero);
-  const size_t row = (size_t)r.s * a.sample_rows + (size_t)r.h * a.token_stride + j;
+  if (m < 0 || m > a.n_rows || r.t >= m) return;                // all lanes of a row together, here and below
+  const int before = cache_len(a, r) - m;
+  const T* from = (const T*)a.x[which] + r.s * a.stride[which][0] + r.h * a.stride[which][1] + part * QT_COLS;
+  const size_t head = (size_t)r.s * a.sample_rows + (size_t)r.h * a.token_stride;
   const CodeRows& c = a.rows[which];
-  store_codes16<BITS>((uint8_t*)c.codes + row * BYTES + part * (BYTES / LPR), w);
-  if (part == 0) { ((uint16_t*)c.scale)[row] = scale; ((uint16_t*)c.zero)[row] = zero; }
+  float x[PASSES][QT_COLS];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) load16(from + min(r.t + p * PER, m - 1) * a.stride[which][2], x[p]);
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int t = r.t + p * PER, j = before + t;
+    uint32_t w[QT_COLS * BITS / 32];
+    uint16_t scale, zero;
+    encode16<LPR, BITS>(x[p], w, scale, zero);
+    if (t >= m || j < 0) continue;
+    const size_t row = head + j;
+    store_codes16<BITS>((uint8_t*)c.codes + row * BYTES + part * (BYTES / LPR), w);
+    if (part == 0) { ((uint16_t*)c.scale)[row] = scale; ((uint16_t*)c.zero)[row] = zero; }
+  }
 }
 
-template <typename T, int D, int BITS>
+template <typename T, int D, int BITS, bool CHUNKED, int PASSES>
 __global__ __launch_bounds__(QT_THREADS) void k_cache_read(const CacheRowsArgs a) {
-  constexpr int LPR = D / QT_COLS, BYTES = D * BITS / 8;
-  const uint32_t at = blockIdx.x * (QT_THREADS / LPR) + threadIdx.x / LPR;
+  constexpr int LPR = D / QT_COLS, BYTES = D * BITS / 8, PER = QT_THREADS / LPR;
   const int part = threadIdx.x % LPR, which = blockIdx.y;
-  if (at >= (uint32_t)a.S * a.H * a.n_rows) return;
-  const CacheRow r = cache_row(a, at);
-  const int j = a.count ? a.count[at] : r.t;
-  if (j < 0 || j >= cache_len(a, r)) return;
-  const size_t row = (size_t)r.s * a.sample_rows + (size_t)r.h * a.token_stride + j;
+  const CacheRow r = cache_row<CHUNKED, PER, PASSES>(a);
+  if (r.t >= a.n_rows) return;
+  const int n = cache_len(a, r);
+  if (n == 0) return;
+  const int32_t* list = a.count ? a.count + ((size_t)r.s * a.H + r.h) * a.n_rows : nullptr;
+  const size_t head = (size_t)r.s * a.sample_rows + (size_t)r.h * a.token_stride;
   const CodeRows& c = a.rows[which];
-  uint32_t w[QT_COLS * BITS / 32];
-  load_codes16<BITS>(c.codes + row * BYTES + part * (BYTES / LPR), w);
-  float x[QT_COLS];
-  decode16<BITS>(w, c.scale[row], c.zero[row], x);
-  store16((T*)a.x[which] + r.s * a.stride[which][0] + r.h * a.stride[which][1] + r.t * a.stride[which][2] + part * QT_COLS, x);
+  T* to = (T*)a.x[which] + r.s * a.stride[which][0] + r.h * a.stride[which][1] + part * QT_COLS;
+  int j[PASSES];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int t = r.t + p * PER;
+    j[p] = t >= a.n_rows ? -1 : list ? list[t] : t;
+  }
+  uint32_t w[PASSES][QT_COLS * BITS / 32];
+  uint16_t scale[PASSES], zero[PASSES];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const size_t row = head + min(max(j[p], 0), n - 1);
+    load_codes16<BITS>(c.codes + row * BYTES + part * (BYTES / LPR), w[p]);
+    scale[p] = c.scale[row]; zero[p] = c.zero[row];
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (j[p] < 0 || j[p] >= n) continue;
+    float x[QT_COLS];
+    decode16<BITS>(w[p], scale[p], zero[p], x);
+    store16(to + (r.t + p * PER) * a.stride[which][2], x);
+  }
 }
 
 template <typename T, int D, int BITS>
 static void cache_rows(const CacheRowsArgs& a, const bool write, hipStream_t st) {
-  constexpr uint32_t rows = QT_THREADS * QT_COLS / D;
-  const dim3 grid(((uint32_t)a.S * a.H * a.n_rows + rows - 1) / rows, 2), threads(QT_THREADS);
-  if (write) hipLaunchKernelGGL((k_cache_write<T, D, BITS>), grid, threads, 0, st, a);
-  else hipLaunchKernelGGL((k_cache_read<T, D, BITS>), grid, threads, 0, st, a);
+  constexpr uint32_t PER = QT_THREADS * QT_COLS / D, PASSES = 2;
+  const uint32_t sets = (uint32_t)a.S * a.H, rows = a.n_rows;
+  const bool chunked = rows >= PER * PASSES;                    // (a head's last chunk may be nearly empty)
+  const dim3 grid(chunked ? sets * ((rows + PER * PASSES - 1) / (PER * PASSES)) : (sets * rows + PER - 1) / PER, 2), threads(QT_THREADS);
+  if (write) {
+    if (chunked) hipLaunchKernelGGL((k_cache_write<T, D, BITS, true, PASSES>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_cache_write<T, D, BITS, false, 1>), grid, threads, 0, st, a);
+  } else {
+    if (chunked) hipLaunchKernelGGL((k_cache_read<T, D, BITS, true, PASSES>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_cache_read<T, D, BITS, false, 1>), grid, threads, 0, st, a);
+  }
 }
 
 template <typename T>

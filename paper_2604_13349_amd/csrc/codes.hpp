@@ -6,6 +6,7 @@
 #pragma once
 #include <hip/hip_fp16.h>
 #include "common.hpp"
+#include "wave_ops.hpp"
 
 namespace obf {
 
@@ -40,40 +41,63 @@ __device__ __forceinline__ void store16(float* __restrict__ p, const float (&x)[
   for (int i = 0; i < 4; ++i) ((float4*)p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
 }
 
+// Smallest and largest of the LPR neighbouring lanes of a row, in all of them.
+template <int LPR> __device__ __forceinline__ void row_range(float& lo, float& hi) {
+  static_assert(LPR == 4 || LPR == 8, "lanes of a row");
+  const auto meet = [&](const uint32_t l, const uint32_t h) { lo = fminf(lo, __uint_as_float(l)); hi = fmaxf(hi, __uint_as_float(h)); };
+  meet(OBF_DPP_MOV(__float_as_uint(lo), 0xB1), OBF_DPP_MOV(__float_as_uint(hi), 0xB1));                        // lane ^ 1
+  meet(OBF_DPP_MOV(__float_as_uint(lo), 0x4E), OBF_DPP_MOV(__float_as_uint(hi), 0x4E));                        // lane ^ 2
+  if (LPR == 8) meet(OBF_DPP_MOV(__float_as_uint(lo), 0x141), OBF_DPP_MOV(__float_as_uint(hi), 0x141));        // the other four of eight
+}
+
 // Codes of the 16 columns x of a row that LPR neighbouring lanes share, scale and zero as half-precision bits (the same in all of them).
 template <int LPR, int BITS>
 __device__ __forceinline__ void encode16(const float (&x)[QT_COLS], uint32_t (&w)[QT_COLS * BITS / 32], uint16_t& scale, uint16_t& zero) {
   float lo = x[0], hi = x[0];
 #pragma unroll
   for (int i = 1; i < QT_COLS; ++i) { lo = fminf(lo, x[i]); hi = fmaxf(hi, x[i]); }
-#pragma unroll
-  for (int off = LPR / 2; off > 0; off >>= 1) { lo = fminf(lo, __shfl_xor(lo, off)); hi = fmaxf(hi, __shfl_xor(hi, off)); }
+  row_range<LPR>(lo, hi);
   constexpr float L = (float)((1 << BITS) - 1);
   const __half zh = __float2half_rn(lo), sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), L));
   const float z = __half2float(zh), s = __half2float(sh);
-  uint32_t q[QT_COLS];
+  float q[QT_COLS];
   if (s > 0.f && s < INFINITY && fabsf(z) < INFINITY) {
-    // The correctly rounded quotient from the row's reciprocal (Markstein): with r = RN(1/s), s of eleven significant bits, a quotient
-    // within an ulp becomes the correctly rounded one by one residual step; the first step only brings it there.
+    // Nearly always the product with the reciprocal decides: r and the product are off by 2^-24 each, the quotient that is rounded by as much, so that where the product
+    // lies farther than L 2^-22 from the middle between two whole numbers, so does the quotient, on the same side.  (Adding 3 2^22 leaves the nearest whole number.)
     const float r = __frcp_rn(s);
+    float far = 0.f;
 #pragma unroll
     for (int i = 0; i < QT_COLS; ++i) {
-      const float t = __fsub_rn(x[i], z);
-      float y = __fmul_rn(t, r);
-      y = __fmaf_rn(__fmaf_rn(-y, s, t), r, y);
-      y = __fmaf_rn(__fmaf_rn(-y, s, t), r, y);
-      q[i] = (uint32_t)fminf(fmaxf(rintf(y), 0.f), L);
+      const float y = __builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(x[i], z), r), 0.f, L);
+      q[i] = __fsub_rn(__fadd_rn(y, 12582912.f), 12582912.f);
+      far = fmaxf(far, fabsf(__fsub_rn(y, q[i])));
+    }
+    if (__any(!(far < 0.5f - L * 0x1p-22f))) {
+      // The correctly rounded quotient from the row's reciprocal (Markstein): with r = RN(1/s), s of eleven significant bits, a quotient
+      // within an ulp becomes the correctly rounded one by one residual step; the first step only brings it there.
+      float c = s;
+      asm volatile("" : "+v"(c));                              // (a branch: the compiler would take both ways and select)
+#pragma unroll
+      for (int i = 0; i < QT_COLS; ++i) {
+        const float t = __fsub_rn(x[i], z);
+        float y = __fmul_rn(t, r);
+        y = __fmaf_rn(__fmaf_rn(-y, c, t), r, y);
+        y = __fmaf_rn(__fmaf_rn(-y, c, t), r, y);
+        q[i] = fminf(fmaxf(rintf(y), 0.f), L);
+      }
     }
   } else {                                                     // a constant row, or values past the half-precision range
 #pragma unroll
-    for (int i = 0; i < QT_COLS; ++i)
-      q[i] = (s > 0.f) ? (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], z), s)), 0.f), L) : 0u;
+    for (int i = 0; i < QT_COLS; ++i) q[i] = (s > 0.f) ? fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], z), s)), 0.f), L) : 0.f;
   }
 #pragma unroll
   for (int k = 0; k < QT_COLS * BITS / 32; ++k) {              // little-endian: the even column of an int4 pair in the low half
     w[k] = 0u;
 #pragma unroll
-    for (int i = 0; i < 32 / BITS; ++i) w[k] |= q[k * (32 / BITS) + i] << (i * BITS);
+    for (int i = 0; i < 4; ++i) {
+      const float byte = BITS == 8 ? q[4 * k + i] : fmaf(q[8 * k + 2 * i + 1], 16.f, q[8 * k + 2 * i]);
+      w[k] = __builtin_amdgcn_cvt_pk_u8_f32(byte, i, w[k]);
+    }
   }
   scale = __half_as_ushort(sh); zero = __half_as_ushort(zh);
 }

@@ -104,9 +104,10 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   AttendKeys& k = a.keys[0];
   k = attend_own(c);
   const long own_rows = (long)a.T * a.g, d = c->head_dim;
-  // bf16, more than 32 rows: the kernel whose rows share the values that it makes of the codes; 17 to 32: two workgroups read the codes (us, as one of 32 rows: 16 x 8
-  // heads of 4000 rows 30 - 33, 4 x 8 of 1000 13 - 15, 16 x 8 of 8192 to 32768 135 - 139).
-  p.tile = c->dtype == OBF_BF16 && own_rows > kAttendFewRows;
+  // bf16, more than 64 rows: the kernel whose rows share the numbers that it makes of the codes; up to there workgroups of 16 rows read the codes as often as they are (us,
+  // many rows and few: 16 x 8 heads of 8192 to 32768 rows, 40 query rows 297 - 187, of 2000 to 8192, 64 rows 93 - 69, 80 rows 93 - 97; 8 heads of 1000, 40 rows 17 - 12.
+  // Workgroups of 32 rows: 16 x 8 heads of 4000, 20 rows 33 for 30, 4 x 8 of 1000 15 for 13).
+  p.tile = c->dtype == OBF_BF16 && own_rows > kCodesManyRows;
   const int tile_rows = p.tile ? kAttendTileRows : kCodesFewRows;
   k.row_tiles = (int)((own_rows + tile_rows - 1) / tile_rows);
   const bool few_seen = k.window > 0 && (k.sink > 0 || !sinks_per_head);

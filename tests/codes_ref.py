@@ -14,7 +14,7 @@ import torch
 
 from tests.attend_ref import HALF, U, visible
 
-FEW = 32
+FEW = 64
 
 
 def quantise(x, bits):

@@ -77,6 +77,8 @@ WRITE = [
     (F32, 64, 8, 1, 5, 3, 4, (0, 4), (0, 3), False),
     (F32, 128, 8, 2, 2, 1, 1, (1, 1), (1, 1), True),
     (F32, 64, 4, 1, 1, 300, 300, (300, 300), (300, 300), False),
+    (BF, 128, 4, 3, 2, 65, 90, (60, 90), (0, 65), True),
+    (BF, 64, 8, 2, 3, 129, 200, (0, 200), (0, 129), False),
 ]
 
 
@@ -116,6 +118,28 @@ def test_write_of_whole_heads_equals_quantize_rows():
         for x, first in ((K, 0), (V, 3)):
             for name, y in zip(NAMES[first:], B.quantize_rows(x, bits)):
                 assert torch.equal(getattr(cache, name).flatten().view(torch.uint8), y.flatten().view(torch.uint8))
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_write_decides_at_and_beside_the_middle_between_two_codes(bits):
+    """Values whose quotient is a whole number and a half, and the numbers next to them, under scales of all sizes: the quotient, rounded, goes to the even code."""
+    B = _b()
+    L, rows, d = (1 << bits) - 1, 4000, 64
+    gen = torch.Generator().manual_seed(13)
+    scale = (torch.rand((rows, 1), generator=gen) + 0.5).half().float() * 2.0 ** torch.randint(-8, 6, (rows, 1), generator=gen)
+    zero = (torch.randn((rows, 1), generator=gen).half().float() * scale * 3).half().float()
+    half = torch.randint(0, L, (rows, d), generator=gen) + 0.5
+    x = zero + scale * half
+    step = torch.randint(-2, 3, (rows, d), generator=gen)
+    for _ in range(2):
+        x = torch.where(step > 0, torch.nextafter(x, torch.tensor(math.inf)), torch.where(step < 0, torch.nextafter(x, torch.tensor(-math.inf)), x))
+        step = step - step.sign()
+    x[:, :1], x[:, 1:2] = zero, zero + scale * L
+    x = x.view(1, 2, rows // 2, d)
+    cache = B.cache_write(B.code_cache(1, 2, rows // 2, d, bits), x.cuda(), x.flip(2).contiguous().cuda())
+    q, s, z = _oracle_codes(x, bits)
+    assert torch.equal(cache.K_codes.cpu(), R.pack(q, bits)) and torch.equal(cache.K_scale.cpu(), s) and torch.equal(cache.K_zero.cpu(), z)
+    assert torch.equal(cache.V_codes.cpu(), R.pack(q, bits).flip(2))
 
 
 def test_write_at_lengths_and_counts_that_are_none():
@@ -237,6 +261,9 @@ CASES = [
     (BF, 128, 2, 2, 17, 1, 300, (100, 300), True, 0, 0),
     (BF, 128, 1, 1, 33, 1, 300, (100, 300), True, 0, 0),
     (BF, 128, 1, 1, 2, 1100, 1300, (1300, 1300), True, 0, 0),
+    (BF, 128, 2, 2, 8, 8, 700, (300, 700), True, 0, 0),
+    (BF, 64, 1, 2, 5, 13, 300, (100, 300), True, 50, 4),
+    (BF, 64, 2, 8, 4, 20, 700, (600, 700), True, 0, 0),
     (BF, 64, 1, 2, 1, 1030, 1200, (1100, 1200), True, 300, 5),
     (F32, 64, 1, 1, 1, 1, 1, (1, 1), True, 0, 0),
     (F32, 64, 2, 2, 2, 1, 333, (1, 333), True, 0, 0),
