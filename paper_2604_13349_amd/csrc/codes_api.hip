@@ -134,10 +134,12 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   if (a.ranges > 1) at += (size_t)a.ranges * a.rows * d * sizeof(float);
   p.part_lse = at;
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
-  // Values made once for all workgroups of a head
-  p.rows = p.tile && k.row_tiles >= 16;
-  p.c.flags = (k.stride + kCodeFlagRows - 1) / kCodeFlagRows;
+  // Numbers made once for all workgroups of a head, where 16 or more of them read a row and the copies stay under 4 GiB (us, by every workgroup and once: 8 heads of 8000
+  // rows, 4, 8, 16 and 32 tiles of query rows 50 - 58, 66 - 72, 110 - 110, 234 - 188; 8 x 8 heads of 4000, 8 and 16 tiles 192 - 205, 353 - 345).
+  const long readers = k.window > 0 && k.window * (long)a.g / kAttendTileRows < k.row_tiles ? k.window * (long)a.g / kAttendTileRows + 1 : k.row_tiles;
   const size_t values = ((size_t)a.S * a.H * k.stride * d * sizeof(uint16_t) + 255) & ~(size_t)255;
+  p.rows = p.tile && readers >= 16 && values <= (size_t)1 << 31;
+  p.c.flags = (k.stride + kCodeFlagRows - 1) / kCodeFlagRows;
   p.rows_k = at;
   if (p.rows) at += values;
   p.rows_v = at;
@@ -182,7 +184,8 @@ obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_c
 
 size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits) {
   if (check_attend(call) != OBF_OK || check_bits(bits) != OBF_OK) return 0;
-  return plan_attend_codes(call, bits, true).total;
+  const size_t with = plan_attend_codes(call, bits, true).total, without = plan_attend_codes(call, bits, false).total;
+  return with > without ? with : without;
 }
 
 obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V, const int32_t* kv_len,

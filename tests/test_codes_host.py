@@ -2,6 +2,7 @@
 import ctypes as C
 import math
 import os
+import random
 
 import pytest
 import torch
@@ -125,6 +126,26 @@ def test_refused_attention(lib):
             if other not in (o, "V", "per_head") and not (other == "K"):
                 assert call(**{o: at[other]}, ws_bytes=256) == 1, (o, other)
                 assert "overlap" in lib.obf_last_error().decode()
+
+
+def test_a_workspace_serves_calls_with_and_without_first_rows_per_head(lib):
+    """The launch is planned by the rows that a query may see, which sink_len changes; refused for its O, a call has had its workspace looked at."""
+    rng = random.Random(5)
+    calls = [(1, 8, 1, 64, 50, 1638, 8, 1501, B.OBF_F32), (7, 2, 4, 128, 1, 5057, 4, 3944, B.OBF_F32), (2, 2, 5, 128, 4, 7974, 4, 7079, B.OBF_BF16),
+             (1, 1, 1, 128, 66, 15457, 4, 8136, B.OBF_BF16)]
+    for _ in range(3000):
+        calls.append((rng.choice([1, 2, 7]), rng.choice([1, 2, 8]), rng.choice([1, 4, 5, 16]), rng.choice([64, 128]), int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(5, 17)),
+                      rng.choice([4, 8]), rng.choice([0, int(2 ** rng.uniform(3, 16))]), rng.choice([B.OBF_BF16, B.OBF_F32])))
+    sizes = set()
+    codes = B._Codes(1 << 50, 1 << 51, 1 << 52)
+    for S, H, g, d, T, rows, bits, window, dtype in calls:
+        c = B._Attend(S, H, g, d, T, rows, dtype, 1, window, rng.choice([0, 0, 4, 3000]), rows, 0, 0)
+        need = lib.obf_attend_codes_workspace_bytes(C.byref(c), bits)
+        sizes.add(need)
+        for sink_len in (None, 1 << 53):
+            rc = lib.obf_attend_codes(C.byref(c), bits, 1 << 40, C.byref(codes), C.byref(codes), None, sink_len, 1 << 40, None, 1 << 60, need, None)
+            assert rc == 1 and "overlap" in lib.obf_last_error().decode(), (rc, S, H, g, d, T, rows, bits, window)
+    assert len(sizes) > 500
 
 
 def test_tensors_must_be_on_a_gpu_and_need_no_gradient():
