@@ -438,7 +438,7 @@ typedef struct {
  *   cache     row (s, h, j) at s * sample_stride + h * token_stride + j (sample_stride 0: n_kv_heads * token_stride)
  *   kv_len    rows per (sample, head), DEVICE int32, entry s * len_stride + h (len_stride 0: n_kv_heads); NULL: kv_len_all in all.
  *             A length below 0 or above token_stride counts as a head without rows.
- * Limits: head_dim 64 or 128; token_stride, n_rows <= 2^24; n_samples*n_kv_heads <= 65535; at most 2^30 cache rows and 2^30 rows in
+ * Limits: head_dim 64 or 128; token_stride, n_rows <= 2^24; n_samples*n_kv_heads <= 65535; at most 2^30 cache rows and 2^29 rows in
  * K; K, V and codes 16-byte aligned, strides of K and V multiples of 16 bytes.  Values must lie in the half-precision range (an
  * infinity or no number among a row's values may spoil that row, and no other).  Outputs may not overlap inputs or one another (what
  * the host can see of it is OBF_ERR_INVALID_ARG). */
@@ -475,7 +475,7 @@ obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_c
  * numbers (fp32 queries as two, 22 bits).  The weights, times the rows' scales, have 11 bits, with fp32 22.  With bf16 and more than 64 query rows
  * (n_queries * group) per KV head V's values enter rounded to half precision, those past its range as the largest ones.
  * Rows at and behind a head's length are not read.  K and V name the codes' arrays, which are inputs.  The workspace holds half-precision copies
- * of the cache's rows where there are 2^11 query rows per KV head or about as many. */
+ * of the cache's rows, up to 4 GiB, where about 2^11 query rows per KV head or more see a row. */
 size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits);
 obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V,
                               const int32_t* kv_len, const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes,

@@ -42,8 +42,8 @@ static obf_status_t check_rows(const obf_cache_rows_t* c) {
     return OBF_ERR_UNSUPPORTED;
   }
   if ((int64_t)c->n_samples * c->n_kv_heads > 65535) { set_error("cache rows: more than 65535 heads in one call"); return OBF_ERR_UNSUPPORTED; }
-  if ((int64_t)c->n_samples * c->n_kv_heads * c->token_stride > ((int64_t)1 << 30) || (int64_t)c->n_samples * c->n_kv_heads * c->n_rows > ((int64_t)1 << 30)) {
-    set_error("cache rows: more than 2^30 rows in one call");
+  if ((int64_t)c->n_samples * c->n_kv_heads * c->token_stride > ((int64_t)1 << 30) || (int64_t)c->n_samples * c->n_kv_heads * c->n_rows > ((int64_t)1 << 29)) {
+    set_error("cache rows: more than 2^30 cache rows or 2^29 rows of K in one call");        // (the latter: a launch has less than 2^32 threads)
     return OBF_ERR_UNSUPPORTED;
   }
   return OBF_OK;

@@ -148,6 +148,18 @@ def test_a_workspace_serves_calls_with_and_without_first_rows_per_head(lib):
     assert len(sizes) > 500
 
 
+@pytest.mark.parametrize("kind", ["write", "read"])
+@pytest.mark.parametrize("samples, heads, rows", [(65535, 1, 8192), (1 << 14, 2, 1 << 14), (1 << 13, 7, 9362), (32, 1, 1 << 24)])
+def test_a_launch_has_fewer_than_2_32_threads(lib, kind, samples, heads, rows):
+    """256 threads for 64 rows of a head at most; a call of 2^29 rows gets past the sizes (to arrays that overlap), one of more is refused for them."""
+    assert samples * heads * -(-rows // 64) * 256 < 1 << 32 and samples * heads * rows <= 1 << 29 < (samples + 1) * heads * (rows + 1)
+    at = {**AT, "K": AT["K.codes"]}
+    rc, msg = _call(lib, kind, _rows(n_samples=samples, n_kv_heads=heads, token_stride=32, kv_len_all=0, n_rows=rows), at)
+    assert rc == 1 and "overlap" in msg
+    rc, msg = _call(lib, kind, _rows(n_samples=min(samples + 1, 65535 // heads), n_kv_heads=heads, token_stride=32, kv_len_all=0, n_rows=min(rows + 1, 1 << 24)), at)
+    assert rc == 2 and "2^29" in msg
+
+
 def test_tensors_must_be_on_a_gpu_and_need_no_gradient():
     u, f = torch.zeros((1, 1, 4, 32), dtype=torch.uint8), torch.zeros((1, 1, 4), dtype=torch.float16)
     with pytest.raises(ValueError, match="GPU"):
