@@ -11,10 +11,15 @@
 // these, and drop what lies 2^-24 below: of sums of codes below 16 in the lowest bits 2^-20 is lost, in the bits above, or of 8-bit codes, 2^-25 (measured).  K's
 // codes therefore stand four bits up, seven instructions for eight codes; V's, behind whose sums the result is rounded to 2^-8, as they come, five for eight.
 // fp32: codes less the one in the middle of the range, beside the value of that one in the place of the zero, so that the two sums are small where the values lie
-// about 0 (3 x 2 heads, 333 queries: 4e-6 of the result's norm off 64 bits otherwise, 1e-6 so).
+// about 0 (3 x 2 heads, 333 queries: 4e-6 of the result's norm off 64 bits with the codes as they are, 2e-7 so, where the same sums in fp32 are 4e-7 off).
 // Q enters as half-precision numbers under a power of two per row, so that its largest lies in [2^14, 2^15): bf16 exactly but for elements 2^-39 of the largest, fp32
 // as two parts of 11 bits.  The weights times s_j enter V's product as half-precision numbers of 11 bits (fp32: two parts): relative to a reference that follows the
 // largest of 2^x_rj |s_j|, so that the largest product lies in [2^7, 2^15] whatever the scales are.  l, sum_j w z_j and O' are single precision.
+//
+// Bound by the codes' bytes where the caches are long: 16 x 8 heads of 8192 to 32768 rows of 128, 4 bits, one query of 4 heads, 70 us and 5 for the join (4.9 TB/s, the
+// vector pipe busy for 0.53 of the time, the matrix pipe for 0.12); 32 x 8 heads of 1000 to 4096, 8 bits, 34 us (5.1 TB/s).  One round of workgroups with a window: 48 x 8
+// heads, 1024 rows each, 17 us, latency and the half-filled last round; 8 heads of 100 to 340 rows 7 us, one chain of loads; fp32, 3 x 2 heads of 333 to 512, 333 queries
+// of 2 heads, d 64, 9 us.  No gain: loads a tile ahead, two query tiles a workgroup, the queries' loads behind the first tile's.
 #include "attend_codes.hpp"
 #include "attend_few.hpp"
 #include "codes.hpp"

@@ -3,9 +3,9 @@
 // The arithmetic is that of the row code (codes.hpp); what these kernels add is the addressing: rows at the strides of a projection's output,
 // a number of them per head, behind what the head holds, and back by row numbers.  16 columns a lane, keys and values in one launch.
 //
-// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 32 (4.4 and 5.3 TB/s), the kept rows of 36 x 8 heads (800 to
-// 1229), 8 bits, in 50 and back in 50, 1229 of 8192 rows by their numbers in 60 (3.8: a row's 64 bytes come as the 128 of its line).  One row a lane, with lengths loaded
-// beside it: 46, 36, 54, 55 and 61; four rows: 40, 33, 52, 54 and 66.  Stores that bypass the caches double the time of the way back.
+// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 30 (4.5 and 5.7 TB/s), the kept rows of 36 x 8 heads (800 to
+// 1229), 8 bits, in 50 and back in 41 to 50 (4.5 and 4.6 or more), 1229 of 8192 rows by their numbers in 61 (4.7 TB/s with the whole lines that rows of
+// 64 bytes are part of).  One row a lane, with lengths loaded beside it: 46, 36, 54, 55 and 61; four rows: 40, 33, 52, 54 and 66.  Stores that bypass the caches double the time of the way back.
 #include "attend_codes.hpp"
 #include "codes.hpp"
 

@@ -135,7 +135,7 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   p.part_lse = at;
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
   // Numbers made once for all workgroups of a head, where 16 or more of them read a row and the copies stay under 4 GiB (us, by every workgroup and once: 8 heads of 8000
-  // rows, 4, 8, 16 and 32 tiles of query rows 50 - 58, 66 - 72, 110 - 110, 234 - 188; 8 x 8 heads of 4000, 8 and 16 tiles 192 - 205, 353 - 345).
+  // rows, 4, 8, 16 and 32 tiles of query rows 49 - 58, 66 - 72, 108 - 108, 236 - 190; 8 x 8 heads of 4000, 8 and 16 tiles 189 - 200, 342 - 332).
   const long readers = k.window > 0 && k.window * (long)a.g / kAttendTileRows < k.row_tiles ? k.window * (long)a.g / kAttendTileRows + 1 : k.row_tiles;
   const size_t values = ((size_t)a.S * a.H * k.stride * d * sizeof(uint16_t) + 255) & ~(size_t)255;
   p.rows = p.tile && readers >= 16 && values <= (size_t)1 << 31;

@@ -5,7 +5,7 @@
 // Both directions are bound by memory: a lane handles 16 consecutive columns, so that a row of 128 is eight lanes and a wave moves
 // eight rows (sixteen at head_dim 64); rows come and go in 16-byte pieces, the codes of a lane in one piece of 16 (int8) or 8 bytes.
 // A lane of 16 columns also pays for the row's minimum, maximum, scale and zero once per 16 values.  366k rows of 128 bf16 values, int8:
-// 25 us to codes and 29 back (5.4 and 4.9 TB/s; 97 and 108 us with a wave per row and a thread per value).
+// 23 us to codes and 27 back (6.1 and 5.2 TB/s; 97 and 108 us with a wave per row and a thread per value).
 #include "codes.hpp"
 
 namespace obf {
