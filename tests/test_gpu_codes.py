@@ -338,6 +338,33 @@ def test_hidden_rows_of_any_numbers_do_not_reach_a_query(dtype, T, window, value
             assert not torch.isfinite(o["O"][:, :, ~clean].float()).all() if (~clean).any() else True
 
 
+@pytest.mark.parametrize("bits,d,window", [(4, 128, 1200), (8, 64, 1200), (4, 64, 300)])
+def test_many_queries_with_a_window_over_a_used_workspace(bits, d, window):
+    """17 tiles of query rows, of which 19 or (window 300) 5 see a row: rows that no query sees, and one that the last two see, have no numbers, the workspace neither."""
+    B = _b()
+    T, g, rows = 1030, 2, 2600
+    Q, K, V = _make(71, BF, d, 1, 2, g, T, rows)
+    kv_len = torch.tensor([[rows, 2403]], dtype=torch.int32)
+    kw = dict(causal=True, window=window, sink=5)
+    k, v = R.quantise(K, bits), R.quantise(V, bits)
+    O, lse, tO, tl = R.attend(Q, k, v, bits, kv_len, **kw)
+    kb, vb = _spoil(k, kv_len, math.nan), _spoil(v, kv_len, math.nan)
+    for h in range(2):
+        n = int(kv_len[0, h])
+        for x in (kb, vb):
+            x[1][0, h, 5:n - T - window + 1] = math.nan
+            x[2][0, h, 5:n - T - window + 1] = math.nan
+        vb[1][0, h, n - 2] = math.nan
+    cache = _cache(kb, vb, bits, d)
+    o = B.attend_codes(Q.cuda(), cache, kv_len=kv_len.cuda(), **kw)
+    o["ws"].fill_(255)
+    o["O"].zero_()
+    o = B.attend_codes(Q.cuda(), cache, kv_len=kv_len.cuda(), out=o, **kw)
+    _check("O", o["O"][:, :, :-2], O[:, :, :-2], tO[:, :, :-2])
+    _check("lse", o["lse"], lse, tl)
+    assert o["O"][:, :, -2:].isnan().all()
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T,rows", [(1, 90), (1, 9000), (40, 90), (40, 9000)])
 def test_visible_rows_without_numbers_reach_the_result(dtype, T, rows):
