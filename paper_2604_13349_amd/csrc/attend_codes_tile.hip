@@ -117,6 +117,18 @@ __global__ __launch_bounds__(CR_THREADS) void k_codes_rows(const AttendCodesArgs
   if (threadIdx.x == 0) args.bad[(size_t)set * args.flags + block] = bad;
 }
 
+// As attend_set, but the tiles of one number of all sets follow one another: where causal heads have many of them, the last and longest of all heads run first and share their
+// compute units with the first ones (us, set after set and tile after tile: 3 x 8 heads of 2139 rows of 64, 32 tiles, 86 - 75, 2 x 8 of 128 92 - 84, 4 x 8 of 1000 to 2000
+// 95 - 80; heads of few tiles lose their second-level cache: 16 x 8 of 600 to 8000 rows, 7 tiles, 465 - 513).  A die's 32 compute units take its workgroups in turn, so that
+// where its sets divide them they move on by one a turn: tiles of one set, of which a head may be longer than the others, would meet on the same ones (138 - 146 - 131).
+constexpr int kDieCU = 32;
+__device__ __forceinline__ int attend_set_by_tile(const int block, const int sets, int& within) {
+  const int round = sets & 7 ? sets & -sets : 8, groups = sets / round, at = block / round;
+  const int group = (at + (kDieCU % groups ? 0 : at / kDieCU)) % groups;
+  within = at / groups;
+  return group * round + (block + group) % round;
+}
+
 template <int D> struct CodeTileShared {
   char rows[4 * AT_KEYS * D * 2];             // K, K, V, V
   float scale[2][AT_KEYS];                    // of K, key_numbers
@@ -132,7 +144,7 @@ __global__ __launch_bounds__(AT_THREADS, D == 64 && (ROWS || BITS == 4) ? 3 : 2)
   const AttendArgs& a = args.a;
   const AttendKeys& k = a.keys[0];
   int within;
-  const int set = attend_set(blockIdx.x, k.samples * a.H, k.row_tiles * k.nsplit, within);
+  const int set = ROWS ? attend_set_by_tile(blockIdx.x, k.samples * a.H, within) : attend_set(blockIdx.x, k.samples * a.H, k.row_tiles * k.nsplit, within);
   const int split = within % k.nsplit, row_tile = k.row_tiles - 1 - within / k.nsplit;
   const int h = set % a.H, s = set / a.H;
   const int set_rows = a.T * a.g, row0 = row_tile * AT_ROWS;
