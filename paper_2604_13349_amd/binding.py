@@ -610,6 +610,18 @@ class _on:
             self.back.__exit__(*exc)
 
 
+def _enqueue(device, call, *args):
+    """call(*args, stream) on the device's current stream (as _on, for calls that need the GPU made the current one for nothing else: 0.3 us less)."""
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        status = call(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            status = call(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status != 0:
+        _check(status)
+
+
 def _forward_only(a, b, c, *more):
     """These calls have no backward pass: what should get a gradient through them is refused, rather than answered without one."""
     if torch.is_grad_enabled() and (a.requires_grad or b.requires_grad or c.requires_grad or more and any(t is not None and t.requires_grad for t in more)):
@@ -827,11 +839,10 @@ def cache_write(cache: CodeCache, K, V, kv_len=None, n_new=None):
     Returns the cache."""
     _forward_only(K, V, K)
     c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), _meta(n_new), None)
-    with _on(cache.device) as stream:
-        if copy_lens:
-            kv_len, n_new = (None if t is None else t.contiguous() for t in (kv_len, n_new))
-        kc, vc = cache._codes()
-        _check(load_library().obf_cache_write(C.byref(c), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(n_new), C.byref(kc), C.byref(vc), stream))
+    if copy_lens:
+        kv_len, n_new = (None if t is None else t.contiguous() for t in (kv_len, n_new))
+    kc, vc = cache._codes()
+    _enqueue(cache.device, load_library().obf_cache_write, C.byref(c), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(n_new), C.byref(kc), C.byref(vc))
     return cache
 
 
@@ -848,11 +859,10 @@ def cache_read(cache: CodeCache, dtype: torch.dtype, kv_len=None, idx=None, out=
         raise ValueError(f"K_out is {K.dtype}, not {dtype}")
     _forward_only(K, V, K)
     c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), None, _meta(idx))
-    with _on(cache.device) as stream:
-        if copy_lens:
-            kv_len = kv_len.contiguous()
-        kc, vc = cache._codes()
-        _check(load_library().obf_cache_read(C.byref(c), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(idx), K.data_ptr(), V.data_ptr(), stream))
+    if copy_lens:
+        kv_len = kv_len.contiguous()
+    kc, vc = cache._codes()
+    _enqueue(cache.device, load_library().obf_cache_read, C.byref(c), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(idx), K.data_ptr(), V.data_ptr())
     return o
 
 
@@ -896,13 +906,12 @@ def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0
     O, lse = o["O"], o["lse"]
     c, need, copy_lens = _attend_codes_plan(cache._layout(), _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
                                             _int("sink", sink))
-    with _on(cache.device) as stream:
-        ws = o["ws"] = _workspace(o.get("ws"), need, cache.device)
-        if copy_lens:
-            kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
-        kc, vc = cache._codes()
-        _check(load_library().obf_attend_codes(C.byref(c), cache.bits, Q.data_ptr(), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(sink_len), O.data_ptr(),
-                                               lse.data_ptr(), ws.data_ptr(), ws.nbytes, stream))
+    ws = o["ws"] = _workspace(o.get("ws"), need, cache.device)
+    if copy_lens:
+        kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
+    kc, vc = cache._codes()
+    _enqueue(cache.device, load_library().obf_attend_codes, C.byref(c), cache.bits, Q.data_ptr(), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(sink_len), O.data_ptr(),
+             lse.data_ptr(), ws.data_ptr(), ws.nbytes)
     return o
 
 
