@@ -96,6 +96,23 @@ static obf_status_t check_rows_apart(const obf_cache_rows_t* c, const CacheRowsA
 
 struct AttendCodesPlan { AttendCodesArgs c; bool tile, rows; int waves; size_t part_O, part_lse, rows_k, rows_v, numbers, bad, total; };
 
+// Ranges of a launch of the kernel of many rows: the least of an estimate, in us.  A workgroup takes its tiles of 64 rows and as long as two more to begin and end, alone on a
+// compute unit `step` a tile, two in 1.5 times that, more one after another; a join 3 and the partial results' way to memory and back.  Of 190 shapes (8 to 128 heads of 700 to
+// 12000 rows, of one length and ragged, 80 to 2000 query rows) it chooses launches that take 1.014 of the time of the best of up to 12 on average, 1.15 at worst.  (As many ranges
+// as give each compute unit two workgroups, none from one a unit on: 1.067 and 1.58; 8 x 8 heads of 4000 to 12000 rows of 64, 500 query rows 236 - 161 us.)
+static long tile_ranges(const long blocks, const long rows, const long out_rows, const int d) {
+  const double step = d == 128 ? 1.42 : 1.06, join = 3.0, partial = out_rows * (double)d * 8 / 6e6;
+  const long tiles = (rows + 63) / 64;
+  long best = 1;
+  double least = 0;
+  for (long r = 1; r <= 64 && (r == 1 || rows >= 100 * r); r = r < 3 ? r + 1 : r % 3 ? r / 2 * 3 : r / 3 * 4) {        // 1 2 3 4 6 8 12 ...
+    const double each = (double)(blocks * r) / kNumCU, load = each <= 1 ? 1.0 : each <= 2 ? 1.5 : 0.83 * (each + 0.3);
+    const double us = load * ((tiles + r - 1) / r + 2) * step + (r > 1 ? join + r * partial : 0.0);
+    if (r == 1 || us < least) { best = r; least = us; }
+  }
+  return best;
+}
+
 static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool sinks_per_head) {
   AttendCodesPlan p;
   AttendArgs& a = p.c.a;
@@ -113,19 +130,29 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   const bool few_seen = k.window > 0 && (k.sink > 0 || !sinks_per_head);
   const long blocks = (long)k.row_tiles * a.S * a.H, seen = few_seen ? (long)k.window + k.sink + tile_rows / a.g + 1 : k.stride;
   const long rows = seen < k.stride ? seen : k.stride;
-  // Ranges where the sets do not fill the chip; none for short caches, and where there is a workgroup per compute unit for caches that are not long: their join would take
-  // longer (us, ranges and none: 256 sets of 1000 to 2048 rows 22 - 18, of 1000 to 4096 in 8 bits 47 - 43, 24 x 20 tiles of many rows 64 - 51).
-  const bool none = rows <= 512 || (p.tile ? blocks >= kNumCU : (blocks >= 128 && rows <= 1024) || (blocks >= kNumCU && rows <= 4096));
-  const int per_cu = p.tile ? 2 : few_codes_per_cu(c->head_dim, c->dtype == OBF_F32, bits);
-  // At least 512 rows a range, 256 where there are few sets; 32 ranges at most, whose join takes as long as what more of them save (us, 8 heads of 32000 rows, 32, 64 and 128
-  // ranges 19 - 24 - 32; of 4000, 8 and 16 ranges 12.7 - 11.4; 64 heads of 2000, 4 and 8 ranges 14.1 - 16.9).
-  const long least = blocks * ((rows + 511) / 512) < kNumCU / 2 ? 256 : 512;
-  const long most = none ? 1 : (rows + least - 1) / least, want = (per_cu * kNumCU + blocks - 1) / blocks;
-  const long ranges = most < want ? most : want;
-  k.nsplit = (int)(p.tile || ranges < 32 ? ranges : 32);
+  long ranges = 1;
   p.waves = 8;
-  // Long ranges are twice as many of four waves, which even out heads of different lengths (16 x 8 heads of 8192 to 32768 rows: 84 us for 87).
-  if (!p.tile && k.nsplit > 1 && rows >= 4096L * k.nsplit) { p.waves = 4; k.nsplit *= 2; }
+  if (p.tile) {
+    ranges = tile_ranges(blocks, rows, a.rows, (int)d);
+  } else {
+    // Few rows: how many ranges of how many waves was measured over 425 shapes (8 to 640 heads of 40 to 32000 rows, of one length and ragged, all types, 1 to 88 tiles of
+    // query rows), each with up to 14 launches; these rules take 1.014 of the best launch's time on average, 1.17 at worst.  us, otherwise and so:
+    //   a join takes 3 us: none for short caches (8 heads of 600 rows 10.8 - 7.9, 64 of 1000 11.9 - 10.7);
+    //   few sets: a wave with one or two tiles and a join of 16 ranges ends before long ranges do (8 heads of 1500 rows, four of eight waves 12.7 - 9.7);
+    //   long caches: as many small workgroups as even out heads of different lengths (136 of 5000 to 20000 rows, 2 of eight waves and 8 of four 82.9 - 65; 72 of them,
+    //   four of eight waves and 16 of four 45.2 - 35.8); 128 and 256 heads of one length lose by it (8 bits, 9000 rows: 59.9 - 61.4, 105.7 - 110);
+    //   more than 32 ranges take longer to join than they save (8 heads of 32000 rows, 32, 64 and 128 ranges 19 - 24 - 32);
+    //   four waves where eight would have nothing to do (8 heads of 256 rows 6.9 - 6.4, 512 of 100 9.2 - 7.6), and where registers leave room for 12 a compute unit and there
+    //   is work for them (fp32, d 128, 24 heads of 400 rows, 1332 query rows 65.8 - 37.0).
+    const bool wide = few_codes_per_cu(c->head_dim, c->dtype == OBF_F32, bits) == 2;
+    if (rows > (wide && blocks > 32 ? 1536 : wide || blocks > 32 ? 1024 : 768)) {
+      const long most = rows > 16384 ? 32 : 16, want = rows <= 4096 ? (blocks <= 32 ? 16 * blocks : kNumCU) : blocks <= 16 ? 512 : wide ? 1536 : 768;
+      while (2 * ranges * blocks <= want && ranges < most) ranges *= 2;
+    }
+    const bool four = ranges > 1 ? (rows <= 4096 ? blocks <= 32 : blocks > 16) : rows <= 256 || (!wide && blocks >= 384);
+    p.waves = four ? 4 : 8;
+  }
+  k.nsplit = (int)ranges;
   k.split0 = 0;
   a.ranges = k.nsplit;
   k.blocks = (int)(blocks * k.nsplit);
