@@ -34,7 +34,7 @@ constexpr int kCodeFlagRows = 64;
 // Workgroups of eight waves of the kernel of few rows that a compute unit holds.
 constexpr int few_codes_per_cu(const int d, const bool f32, const int bits) { return d == 64 || (bits == 4 && !f32) ? 2 : 1; }
 constexpr int kCodesFewRows = 16;        // its query rows per workgroup
-constexpr int kCodesManyRows = 64;       // query rows per KV head up to which bf16 calls take it
+constexpr int kCodesManyRows = 64;       // query rows per KV head up to which all bf16 calls take it
 obf_status_t launch_attend_codes_few(const AttendCodesArgs& c, int waves, int d, int dtype, int bits, hipStream_t st);
 obf_status_t launch_attend_codes_tile(const AttendCodesArgs& c, int d, int bits, hipStream_t st);          // bf16, tiles of kAttendTileRows; with c.rows_k: over those rows, which it writes
 

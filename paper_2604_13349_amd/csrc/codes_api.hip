@@ -121,15 +121,19 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   AttendKeys& k = a.keys[0];
   k = attend_own(c);
   const long own_rows = (long)a.T * a.g, d = c->head_dim;
-  // bf16, more than 64 rows: the kernel whose rows share the numbers that it makes of the codes; up to there workgroups of 16 rows read the codes as often as they are (us,
-  // many rows and few: 16 x 8 heads of 8192 to 32768 rows, 40 query rows 297 - 187, of 2000 to 8192, 64 rows 93 - 69, 80 rows 93 - 97; 8 heads of 1000, 40 rows 17 - 12.
-  // Workgroups of 32 rows: 16 x 8 heads of 4000, 20 rows 33 for 30, 4 x 8 of 1000 15 for 13).
-  p.tile = c->dtype == OBF_BF16 && own_rows > kCodesManyRows;
-  const int tile_rows = p.tile ? kAttendTileRows : kCodesFewRows;
-  k.row_tiles = (int)((own_rows + tile_rows - 1) / tile_rows);
   const bool few_seen = k.window > 0 && (k.sink > 0 || !sinks_per_head);
-  const long blocks = (long)k.row_tiles * a.S * a.H, seen = few_seen ? (long)k.window + k.sink + tile_rows / a.g + 1 : k.stride;
-  const long rows = seen < k.stride ? seen : k.stride;
+  const auto tiles_of = [&](const int tile_rows) { return (own_rows + tile_rows - 1) / tile_rows; };
+  const auto seen_by = [&](const int tile_rows) { const long seen = (long)k.window + k.sink + tile_rows / a.g + 1; return few_seen && seen < k.stride ? seen : (long)k.stride; };
+  // bf16 calls of more than 64 rows may take the kernel whose rows share the numbers that it makes of the codes; workgroups of 16 rows read the codes as often as they are,
+  // and so are the faster ones for 64 rows at any length and for more where their tiles are not many times what the chip holds, the fewer the longer the caches are (us, many
+  // rows and few: 16 x 8 heads of 8192 to 32768 rows, 40 query rows 297 - 187, of 2000 to 8192, 64 rows 93 - 69, 80 rows 93 - 97; 8 heads of 300 to 600 rows, 96 to 512 query
+  // rows 14 to 20 - 7 to 9, 1000 rows 16.4 - 11.1; 16 heads of 300, 1000 rows (1008 tiles) 16.8 - 19.5; of 4000, 256 rows (256 tiles) 31.5 - 27.5, 64 heads 71 - 80; 8 heads
+  // of 12000, 160 rows (80 tiles) 37.8 - 33.2, 256 rows 38.2 - 40.3).  Workgroups of 32 rows: 16 x 8 heads of 4000, 20 rows 33 for 30, 4 x 8 of 1000 15 for 13.
+  const long few_tiles = tiles_of(kCodesFewRows) * a.S * a.H, few_rows = seen_by(kCodesFewRows);
+  p.tile = c->dtype == OBF_BF16 && own_rows > kCodesManyRows && few_tiles > (few_rows <= 2560 ? 768 : few_rows <= 6144 ? 256 : 96);
+  const int tile_rows = p.tile ? kAttendTileRows : kCodesFewRows;
+  k.row_tiles = (int)tiles_of(tile_rows);
+  const long blocks = (long)k.row_tiles * a.S * a.H, rows = seen_by(tile_rows);
   long ranges = 1;
   p.waves = 8;
   if (p.tile) {
@@ -152,6 +156,9 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
     const bool four = ranges > 1 ? (rows <= 4096 ? blocks <= 32 : blocks > 16) : rows <= 256 || (!wide && blocks >= 384);
     p.waves = four ? 4 : 8;
   }
+  // At most 2^16 rows a range, where the partial results stay under 256 MB: a lane adds up a range's terms in single precision (2^24 rows of equal weights, 2^19 a range: lse
+  // 7e-5 off).
+  while (rows > ranges << 16 && 2 * ranges * a.rows * d * (long)sizeof(float) <= 1L << 28) ranges *= 2;
   k.nsplit = (int)ranges;
   k.split0 = 0;
   a.ranges = k.nsplit;

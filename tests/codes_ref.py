@@ -7,7 +7,7 @@ dx = (d + 8) u sum_c |q_c| (|s| c + |z|) / sqrt(d), a weight by a factor of 1 + 
               2^-24), times codes up to L; with bf16, sums of V's codes drop what lies 2^-20 below a largest product
   many rows   queries with 2^-39 of the largest element, their sum with 2^-33 of it and 2^-25 beside one of up to 2^8 times 2^14 (2^-24 of the largest element, for
               values up to |zero| + 2^(bits - 1) |scale|); V's values rounded to half precision, 2^-11 of the value and 2^-25, weights with 2^-11 and 2^-32 of the largest
-The result is then rounded once to its type."""
+bf16 calls of more than 64 rows take one or the other by their sizes: the larger of both bounds.  The result is then rounded once to its type."""
 import math
 
 import torch
@@ -44,7 +44,7 @@ def attend(Q, K, V, bits, kv_len, causal=True, window=0, sink=0, sink_len=None):
     S, Hq, T, d = Q.shape
     H, R = K[0].shape[1], K[0].shape[2]
     g, L, f32 = Hq // H, float((1 << bits) - 1), Q.dtype == torch.float32
-    many = not f32 and g * T > FEW
+    kernels = ["few", "many"] if not f32 and g * T > FEW else ["few"]
     O = torch.zeros((S, Hq, T, d), dtype=torch.float64)
     lse = torch.full((S, Hq, T), -math.inf, dtype=torch.float64)
     tol_O, tol_lse = torch.zeros_like(O), torch.zeros_like(lse)
@@ -64,24 +64,25 @@ def attend(Q, K, V, bits, kv_len, causal=True, window=0, sink=0, sink_len=None):
                 c = torch.logsumexp(x, dim=1)
                 w = torch.exp(x - c[:, None])
                 qa = q.abs()
-                dx = (d + 8) * U * (qa @ k_abs.t())
-                if many:
-                    middle = values(torch.full_like(K[0][s, h, at][:, :1], 1 << (bits - 1)), K[1][s, h, at].abs(), K[2][s, h, at].abs())[:, 0]
-                    dx = dx + (2.0 ** -39 * d + 2.0 ** -24) * qa.amax(dim=1)[:, None] * middle
-                    dx = dx + (d + 8) * U * qa.sum(dim=1)[:, None] * middle
-                    p_eps, spare = 2.0 ** -11, 2.0 ** -32 * w.amax(dim=1)[:, None] * v.abs().sum(dim=0)
-                    off = w @ (2.0 ** -11 * v.abs() + 2.0 ** -25)
-                else:
-                    codes = values(K[0][s, h, at], K[1][s, h, at].abs(), torch.zeros_like(K[2][s, h, at]))
-                    dx = dx + (2.0 ** -22 if f32 else 0.0) * (qa @ codes.t()) + 2.0 ** -39 * qa.amax(dim=1)[:, None] * codes.sum(dim=1)
-                    p_eps = 2.0 ** -22 if f32 else 2.0 ** -11 + 2.0 ** -20
-                    vs = V[1][s, h, at].double().abs().clamp(min=2.0 ** -24)
-                    spare, off = 2.0 ** -32 * L * at.numel() * (w * vs).amax(dim=1)[:, None], 0.0
-                dx = (dx.amax(dim=1) / math.sqrt(d))[:, None]
-                e = 2 * dx + (at.numel() + 16) * U
                 row = slice(h * g, (h + 1) * g)
                 O[s, row, t] = w @ v
-                tol_O[s, row, t] = (w @ v).abs() * HALF[Q.dtype] * 1.01 + (w @ v_abs) * (e + p_eps) + off + spare
+                for kernel in kernels:
+                    dx = (d + 8) * U * (qa @ k_abs.t())
+                    if kernel == "many":
+                        middle = values(torch.full_like(K[0][s, h, at][:, :1], 1 << (bits - 1)), K[1][s, h, at].abs(), K[2][s, h, at].abs())[:, 0]
+                        dx = dx + (2.0 ** -39 * d + 2.0 ** -24) * qa.amax(dim=1)[:, None] * middle
+                        dx = dx + (d + 8) * U * qa.sum(dim=1)[:, None] * middle
+                        p_eps, spare = 2.0 ** -11, 2.0 ** -32 * w.amax(dim=1)[:, None] * v.abs().sum(dim=0)
+                        off = w @ (2.0 ** -11 * v.abs() + 2.0 ** -25)
+                    else:
+                        codes = values(K[0][s, h, at], K[1][s, h, at].abs(), torch.zeros_like(K[2][s, h, at]))
+                        dx = dx + (2.0 ** -22 if f32 else 0.0) * (qa @ codes.t()) + 2.0 ** -39 * qa.amax(dim=1)[:, None] * codes.sum(dim=1)
+                        p_eps = 2.0 ** -22 if f32 else 2.0 ** -11 + 2.0 ** -20
+                        vs = V[1][s, h, at].double().abs().clamp(min=2.0 ** -24)
+                        spare, off = 2.0 ** -32 * L * at.numel() * (w * vs).amax(dim=1)[:, None], 0.0
+                    dx = (dx.amax(dim=1) / math.sqrt(d))[:, None]
+                    e = 2 * dx + (at.numel() + 16) * U
+                    tol_O[s, row, t] = torch.maximum(tol_O[s, row, t], (w @ v).abs() * HALF[Q.dtype] * 1.01 + (w @ v_abs) * (e + p_eps) + off + spare)
+                    tol_lse[s, row, t] = torch.maximum(tol_lse[s, row, t], (dx + (at.numel() + 16) * U).amax(dim=1) + 4 * U * c.abs())
                 lse[s, row, t] = c
-                tol_lse[s, row, t] = (dx + (at.numel() + 16) * U).amax(dim=1) + 4 * U * c.abs()
     return O, lse, tol_O, tol_lse
