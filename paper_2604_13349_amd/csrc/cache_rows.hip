@@ -3,9 +3,9 @@
 // The arithmetic is that of the row code (codes.hpp); what these kernels add is the addressing: rows at the strides of a projection's output,
 // a number of them per head, behind what the head holds, and back by row numbers.  16 columns a lane, keys and values in one launch.
 //
-// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 30 (4.5 and 5.7 TB/s), the kept rows of 36 x 8 heads (800 to
-// 1229), 8 bits, in 50 and back in 41 to 50 (4.5 and 4.6 or more), 1229 of 8192 rows by their numbers in 61 (4.7 TB/s with the whole lines that rows of
-// 64 bytes are part of).  One row a lane, with lengths loaded beside it: 46, 36, 54, 55 and 61; four rows: 40, 33, 52, 54 and 66.  Stores that bypass the caches double the time of the way back.
+// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 29 (4.5 and 5.9 TB/s), the kept rows of 36 x 8 heads (800 to
+// 1229), 8 bits, in 50 and back in 47 (4.5 and 4.8), 1229 of 8192 rows by their numbers in 52 (5.5 with the whole lines that rows of 64 bytes are part of).
+// One row a lane: 42, 35, 52, 56 and 63; four rows: 40, 32, 52, 44 and 52.  Stores that bypass the caches double the time of the way back.
 #include "attend_codes.hpp"
 #include "codes.hpp"
 
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(QT_THREADS) void k_cache_read(const CacheRowsArgs a
   const int32_t* list = a.count ? a.count + ((size_t)r.s * a.H + r.h) * a.n_rows : nullptr;
   const size_t head = (size_t)r.s * a.sample_rows + (size_t)r.h * a.token_stride;
   const CodeRows& c = a.rows[which];
-  T* to = (T*)a.x[which] + r.s * a.stride[which][0] + r.h * a.stride[which][1] + part * QT_COLS;
+  T* to = (T*)a.x[which] + r.s * a.stride[which][0] + r.h * a.stride[which][1];
   int j[PASSES];
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(QT_THREADS) void k_cache_read(const CacheRowsArgs a
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const size_t row = head + min(max(j[p], 0), n - 1);
-    load_codes16<BITS>(c.codes + row * BYTES + part * (BYTES / LPR), w[p]);
+    load_codes_part<D, BITS>(c.codes + row * BYTES, part, w[p]);
     scale[p] = c.scale[row]; zero[p] = c.zero[row];
   }
 #pragma unroll
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(QT_THREADS) void k_cache_read(const CacheRowsArgs a
     if (j[p] < 0 || j[p] >= n) continue;
     float x[QT_COLS];
     decode16<BITS>(w[p], scale[p], zero[p], x);
-    store16(to + (r.t + p * PER) * a.stride[which][2], x);
+    store_part<D>(to + (r.t + p * PER) * a.stride[which][2], part, x);
   }
 }
 

@@ -3,9 +3,9 @@
 // numbers, zero = fp16(min x), scale = fp16((max x - min x) / L), L = 2^bits - 1, q = clamp(rint((x - zero) / scale), 0, L).
 //
 // Both directions are bound by memory: a lane handles 16 consecutive columns, so that a row of 128 is eight lanes and a wave moves
-// eight rows (sixteen at head_dim 64); rows come and go in 16-byte pieces, the codes of a lane in one piece of 16 (int8) or 8 bytes.
+// eight rows (sixteen at head_dim 64); rows come and go in 16-byte pieces, the codes of a lane in one piece of 16 (int8) or 8 bytes, back in two of half that.
 // A lane of 16 columns also pays for the row's minimum, maximum, scale and zero once per 16 values.  366k rows of 128 bf16 values, int8:
-// 23 us to codes and 27 back (6.1 and 5.2 TB/s; 97 and 108 us with a wave per row and a thread per value).
+// 23 us to codes and 24 back (6.1 and 5.9 TB/s; 97 and 108 us with a wave per row and a thread per value).
 #include "codes.hpp"
 
 namespace obf {
@@ -34,10 +34,10 @@ __global__ __launch_bounds__(QT_THREADS) void k_dequant_rows(const uint8_t* __re
   const int part = threadIdx.x % LPR;
   if (row >= n_rows) return;
   uint32_t w[QT_COLS * BITS / 32];
-  load_codes16<BITS>(codes + row * (D * BITS / 8) + part * (QT_COLS * BITS / 8), w);
+  load_codes_part<D, BITS>(codes + row * (D * BITS / 8), part, w);
   float x[QT_COLS];
   decode16<BITS>(w, scale[row], zero[row], x);
-  store16(X + row * D + part * QT_COLS, x);
+  store_part<D>(X + row * D, part, x);
 }
 
 // Pieces of 16 and 8 bytes need their arrays aligned so.  A caller's arrays usually are (rows of an allocation are); one that starts
