@@ -60,29 +60,15 @@ __device__ __forceinline__ void encode16(const float (&x)[QT_COLS], uint32_t (&w
   const float z = __half2float(zh), s = __half2float(sh);
   float q[QT_COLS];
   if (s > 0.f && s < INFINITY && fabsf(z) < INFINITY) {
-    // Nearly always the product with the reciprocal decides: r and the product are off by 2^-24 each, the quotient that is rounded by as much, so that where the product
-    // lies farther than L 2^-22 from the middle between two whole numbers, so does the quotient, on the same side.  (Adding 3 2^22 leaves the nearest whole number.)
+    // The correctly rounded quotient t / s from r = RN(1 / s), in one step: y = RN(t r) is off by less than 2 ulp, t - y s is exact, since s has 11 significant bits, and
+    // y + (t - y s) r is off by 2^-23 ulp.  From the middle between two floats t / s keeps 2^-12 ulp at least: it is a fraction over an integer below 2^11, and none itself,
+    // since an odd number of 25 bits does not divide one of 24.  (The product alone where that decides, which ties of bf16 rows make
+    // rarer than it looks, and two steps elsewhere: 38.5 us for 37.7 to 4 bits, int4 rows 22.6 for 21.3.)
     const float r = __frcp_rn(s);
-    float far = 0.f;
 #pragma unroll
     for (int i = 0; i < QT_COLS; ++i) {
-      const float y = __builtin_amdgcn_fmed3f(__fmul_rn(__fsub_rn(x[i], z), r), 0.f, L);
-      q[i] = __fsub_rn(__fadd_rn(y, 12582912.f), 12582912.f);
-      far = fmaxf(far, fabsf(__fsub_rn(y, q[i])));
-    }
-    if (__any(!(far < 0.5f - L * 0x1p-22f))) {
-      // The correctly rounded quotient from the row's reciprocal (Markstein): with r = RN(1/s), s of eleven significant bits, a quotient
-      // within an ulp becomes the correctly rounded one by one residual step; the first step only brings it there.
-      float c = s;
-      asm volatile("" : "+v"(c));                              // (a branch: the compiler would take both ways and select)
-#pragma unroll
-      for (int i = 0; i < QT_COLS; ++i) {
-        const float t = __fsub_rn(x[i], z);
-        float y = __fmul_rn(t, r);
-        y = __fmaf_rn(__fmaf_rn(-y, c, t), r, y);
-        y = __fmaf_rn(__fmaf_rn(-y, c, t), r, y);
-        q[i] = fminf(fmaxf(rintf(y), 0.f), L);
-      }
+      const float t = __fsub_rn(x[i], z), y = __fmul_rn(t, r);
+      q[i] = rintf(__builtin_amdgcn_fmed3f(__fmaf_rn(__fmaf_rn(-y, s, t), r, y), 0.f, L));
     }
   } else {                                                     // a constant row, or values past the half-precision range
 #pragma unroll
