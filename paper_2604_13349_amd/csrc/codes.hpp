@@ -62,8 +62,8 @@ __device__ __forceinline__ void encode16(const float (&x)[QT_COLS], uint32_t (&w
   if (s > 0.f && s < INFINITY && fabsf(z) < INFINITY) {
     // The correctly rounded quotient t / s from r = RN(1 / s), in one step: y = RN(t r) is off by less than 2 ulp, t - y s is exact, since s has 11 significant bits, and
     // y + (t - y s) r is off by 2^-23 ulp.  From the middle between two floats t / s keeps 2^-12 ulp at least: it is a fraction over an integer below 2^11, and none itself,
-    // since an odd number of 25 bits does not divide one of 24.  (The product alone where that decides, which ties of bf16 rows make
-    // rarer than it looks, and two steps elsewhere: 38.5 us for 37.7 to 4 bits, int4 rows 22.6 for 21.3.)
+    // since an odd number of 25 bits does not divide one of 24.  (Taking the product alone where it lies far enough from a tie, and two steps
+    // elsewhere, which is often, since bf16 rows have many ties: 38.5 us for 37.7 to 4 bits, int4 rows 22.6 for 21.3.)
     const float r = __frcp_rn(s);
 #pragma unroll
     for (int i = 0; i < QT_COLS; ++i) {
