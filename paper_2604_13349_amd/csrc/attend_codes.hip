@@ -220,7 +220,9 @@ __global__ __launch_bounds__(NW * 64, PER_SIMD) void k_attend_codes_few(const At
     const int base = 32 * i;
     const bool cut = attend_cut(k, span, sink, pmin, pmax, base, 32);
     const float given = __half2float(__ushort_as_half(f.scale)), base_value = __half2float(__ushort_as_half(f.zero));
-    const float scale = given * scale_unit, zero = (PARTS == 2 ? fmaf(given, code_middle(BITS), base_value) : base_value) * zero_unit;
+    // (an infinite number is none: by itself it would hide a key from the queries whose sums have one sign)
+    const float none = 0.f * (given + base_value);
+    const float scale = given * scale_unit, zero = fmaf(PARTS == 2 ? fmaf(given, code_middle(BITS), base_value) : base_value, zero_unit, none);
     const bool flat = __any(of_v && scale == 0.f);
     f32x4 x[2];
 #pragma unroll

@@ -48,10 +48,12 @@ __device__ __forceinline__ void code_numbers(CodeFrag& f, const uint32_t* w, con
   }
 }
 __device__ __forceinline__ _Float16 half_of(const uint16_t x) { union { uint16_t u; _Float16 f; } y; y.u = x; return y.f; }
-// What a logit takes of a row of K: its scale with kTileUnit taken out, and its zero and scale as they are.
+// What a logit takes of a row of K: its scale with kTileUnit taken out, and its zero and scale as they are.  An infinite one makes the first none: by itself it would hide the key
+// from the queries whose sums have one sign.
 constexpr float kTileUnit = 16384.f;          // sum(q) under q's power of two, 2^22 at most, times the middle code is a half-precision number with this taken out
 __device__ __forceinline__ uint2 key_numbers(const uint16_t scale, const uint16_t zero) {
-  return make_uint2(__float_as_uint((float)half_of(scale) * (1.f / kTileUnit)), (uint32_t)scale << 16 | zero);
+  const float s = (float)half_of(scale), z = (float)half_of(zero);
+  return make_uint2(__float_as_uint(fmaf(0.f, s + z, s * (1.f / kTileUnit))), (uint32_t)scale << 16 | zero);
 }
 
 // Eight of V's values, zero + scale * code.

@@ -425,6 +425,79 @@ def test_visible_rows_without_numbers_reach_the_result(dtype, T, rows, crowd):
     _check("O", o["O"][0].cpu()[keep], O[0][keep], tO[0][keep])
 
 
+def _both_signs(Q, H):
+    """Query heads in turn with a positive and a negative sum of their elements (which have both signs)."""
+    sign = torch.where(Q.float().sum(dim=-1, keepdim=True) >= 0, 1.0, -1.0)
+    turn = torch.where(torch.arange(Q.shape[1]) % 2 == 0, 1.0, -1.0)[None, :, None, None]
+    return (Q.float() * sign * turn).to(Q.dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,rows,crowd", [(1, 90, False), (1, 9000, False), (40, 90, False), (40, 90, True), (40, 9000, False), (40, 9000, True)])
+def test_visible_rows_of_infinite_numbers_reach_the_result(dtype, T, rows, crowd):
+    """An infinite scale or zero is no number, whatever the sign of the queries' sums: a key's makes O and lse none, a value's O alone."""
+    bits = 4
+    Q, K, V = _make(25, dtype, 128, 1, 2, 2, T, rows)
+    Q = _both_signs(Q, 2)
+    kv_len = torch.full((1, 2), rows, dtype=torch.int32)
+    k, v = R.quantise(K, bits), R.quantise(V, bits)
+    O, lse, tO, tl = R.attend(Q, k, v, bits, kv_len)
+    for which, number, value in [(w, i, s * math.inf) for w in (0, 1) for i in (1, 2) for s in (1, -1)]:
+        both = [tuple(x.clone() for x in y) for y in (k, v)]
+        both[which][number][0, 0, rows // 3 if T == 1 else 5] = value
+        o = _run(Q, *both, bits, kv_len, crowd=crowd)
+        assert not torch.isfinite(o["O"][0, :2].float()).any(), (which, number, value)
+        if which == 0:
+            assert torch.isnan(o["O"][0, :2]).all() and torch.isnan(o["lse"][0, :2]).all(), (number, value)
+        else:
+            _check("lse", o["lse"], lse, tl)
+        _check("O", o["O"][0, 2:], O[0, 2:], tO[0, 2:])
+        _check("lse", o["lse"][0, 2:], lse[0, 2:], tl[0, 2:])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,window,crowd", [(13, 5, False), (70, 11, True), (150, 64, False), (150, 64, True)])
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_row_of_infinite_numbers_reaches_all_that_see_it_and_nobody_else(dtype, T, window, crowd, which):
+    n = T + 30
+    Q, K, V = _make(26, dtype, 64, 1, 2, 2, T, n)
+    Q = _both_signs(Q, 2)
+    kv_len = torch.full((1, 2), n, dtype=torch.int32)
+    kw = dict(causal=True, window=window, sink=2)
+    k, v = R.quantise(K, 8), R.quantise(V, 8)
+    O, lse, tO, tl = R.attend(Q, k, v, 8, kv_len, **kw)
+    for where, number, value in [(w, i, s * math.inf) for w in (n - 2, n - T // 2, 1) for i in (1, 2) for s in (1, -1)]:
+        both = [tuple(x.clone() for x in y) for y in (k, v)]
+        both[which][number][:, :, where] = value
+        sees = torch.tensor([where in attend_ref.visible(n, T, t, True, window, 2) for t in range(T)])
+        assert sees.any()
+        o = _run(Q, *both, 8, kv_len, crowd=crowd, **kw)
+        _check("O", o["O"][:, :, ~sees], O[:, :, ~sees], tO[:, :, ~sees])
+        _check("lse", o["lse"][:, :, ~sees], lse[:, :, ~sees], tl[:, :, ~sees])
+        assert not torch.isfinite(o["O"][:, :, sees].float()).any(), (where, number, value)
+        if which == 0:
+            assert torch.isnan(o["lse"][:, :, sees]).all(), (where, number, value)
+        else:
+            _check("lse", o["lse"], lse, tl)
+
+
+@pytest.mark.parametrize("dtype,T", [(BF, 1), (F32, 2), (BF, 300)])
+def test_keys_written_from_below_the_half_precision_range(dtype, T):
+    """A key with an element of -1e5 has a finite scale and a zero of -inf: the queries that see it get no number, a window that hides it their results."""
+    B = _b()
+    rows = 400
+    Q, K, V = _make(27, dtype, 128, 1, 2, 2, T, rows)
+    Q = _both_signs(Q, 2)
+    K[0, 0, 3, 7] = -1e5
+    kv_len = torch.full((1, 2), rows, dtype=torch.int32)
+    cache = B.cache_write(B.code_cache(1, 2, rows, 128, 4), K.cuda(), V.cuda())
+    assert cache.K_zero[0, 0, 3] == -math.inf and torch.isfinite(cache.K_scale).all()
+    o = B.attend_codes(Q.cuda(), cache, kv_len=kv_len.cuda())
+    assert torch.isnan(o["O"][0, :2]).all() and torch.isnan(o["lse"][0, :2]).all() and torch.isfinite(o["O"][0, 2:].float()).all()
+    o = B.attend_codes(Q.cuda(), cache, kv_len=kv_len.cuda(), window=90)
+    assert torch.isfinite(o["O"].float()).all() and torch.isfinite(o["lse"]).all()
+
+
 @pytest.mark.parametrize("dtype,T", [(BF, 1), (BF, 2), (BF, 60), (F32, 1), (F32, 20)])
 @pytest.mark.parametrize("bits", [4, 8])
 def test_scales_of_all_sizes_in_one_head(dtype, T, bits):
