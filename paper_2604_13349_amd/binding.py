@@ -622,10 +622,12 @@ def _enqueue(device, call, *args):
         _check(status)
 
 
-def _forward_only(a, b, c, *more):
+def _forward_only(*tensors):
     """These calls have no backward pass: what should get a gradient through them is refused, rather than answered without one."""
-    if torch.is_grad_enabled() and (a.requires_grad or b.requires_grad or c.requires_grad or more and any(t is not None and t.requires_grad for t in more)):
-        raise ValueError("forward only: no gradient reaches a tensor that requires one (call under torch.no_grad(), or detach it)")
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("forward only: no gradient reaches a tensor that requires one (call under torch.no_grad(), or detach it)")
 
 
 def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
@@ -799,6 +801,11 @@ class CodeCache:
                 _Codes(self.V_codes.data_ptr(), self.V_scale.data_ptr(), self.V_zero.data_ptr()))
 
 
+def _numbers(cache):
+    """The tensors of a cache that may require a gradient."""
+    return () if cache is None else (cache.K_scale, cache.K_zero, cache.V_scale, cache.V_zero)
+
+
 def code_cache(samples: int, heads: int, rows: int, d: int, bits: int = 4, device="cuda") -> CodeCache:
     """An empty cache held in codes: room for `rows` rows per head."""
     both = [[torch.zeros((samples, heads, rows, d * bits // 8), dtype=torch.uint8, device=device)] +
@@ -836,8 +843,8 @@ def _rows_plan(cache, K, V, kv_len, per_head, idx):
 def cache_write(cache: CodeCache, K, V, kv_len=None, n_new=None):
     """obf_cache_write: K, V [S,H,T,d] (any strides of 16 bytes, last dimension contiguous) become the newest rows of the cache's heads.  kv_len int32 [S,H]:
     rows per head with the new ones (None: the cache is full then); n_new int32 [S,H]: how many of the T rows are a head's (None: all), the first of them.
-    Returns the cache."""
-    _forward_only(K, V, K)
+    Forward only, as attend.  Returns the cache."""
+    _forward_only(K, V, *_numbers(cache))
     c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), _meta(n_new), None)
     if copy_lens:
         kv_len, n_new = (None if t is None else t.contiguous() for t in (kv_len, n_new))
@@ -848,7 +855,8 @@ def cache_write(cache: CodeCache, K, V, kv_len=None, n_new=None):
 
 def cache_read(cache: CodeCache, dtype: torch.dtype, kv_len=None, idx=None, out=None):
     """obf_cache_read: rows idx int32 [S,H,n] of every head, or (None) all of its rows, as dtype.  out: a dict whose K_out, V_out [S,H,n,d] are filled; where a
-    head has no such row they stay as they are.  Without it they are made, with zeros in such places.  Returns the dict."""
+    head has no such row they stay as they are.  Without it they are made, with zeros in such places.  Forward only, as attend.
+    Returns the dict."""
     o = out if out is not None else {}
     S, H, rows = cache.shape
     for name in ("K_out", "V_out"):
@@ -857,7 +865,7 @@ def cache_read(cache: CodeCache, dtype: torch.dtype, kv_len=None, idx=None, out=
     K, V = o["K_out"], o["V_out"]
     if K.dtype != dtype:
         raise ValueError(f"K_out is {K.dtype}, not {dtype}")
-    _forward_only(K, V, K)
+    _forward_only(K, V, *_numbers(cache))
     c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), None, _meta(idx))
     if copy_lens:
         kv_len = kv_len.contiguous()
@@ -896,14 +904,15 @@ def _attend_codes_plan(cache, Q, O, lse, kv_len, sink_len, causal, window, sink)
 
 
 def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0, sink_len=None, out=None):
-    """obf_attend_codes: attend, over a cache held in codes, without accumulated weights.  Returns a dict as attend does: O [S,H*g,T,d], lse [S,H*g,T], ws."""
-    _forward_only(Q, Q, Q)
+    """obf_attend_codes: attend, over a cache held in codes, without accumulated weights.  Returns a dict as attend does: O [S,H*g,T,d], lse [S,H*g,T], ws.
+    Forward only: queries, outputs or a cache whose scale or zero requires a gradient are refused while gradients are recorded."""
     o = out if out is not None else {}
     if "O" not in o:
         o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
     if "lse" not in o:
         o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
     O, lse = o["O"], o["lse"]
+    _forward_only(Q, O, lse, *_numbers(cache))
     c, need, copy_lens = _attend_codes_plan(cache._layout(), _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
                                             _int("sink", sink))
     ws = o["ws"] = _workspace(o.get("ws"), need, cache.device)

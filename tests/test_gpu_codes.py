@@ -813,3 +813,27 @@ def test_binding_refuses_tensors_that_do_not_match():
         with pytest.raises(B.ObfError):
             f()
             pytest.fail(f"call {i} was taken")
+
+
+def test_a_cache_that_requires_a_gradient_is_refused():
+    """While gradients are recorded; the flag may be set after the cache was made, and on any of its four numbers."""
+    B = _b()
+    Q, K, V = (x.cuda() for x in _make(28, BF, 64, 1, 2, 1, 3, 3))
+    cache = B.cache_write(B.code_cache(1, 2, 8, 64, 4), K, V, kv_len=torch.full((1, 2), 3, dtype=torch.int32, device="cuda"))
+    parts = [getattr(cache, n) for n in NAMES]
+    calls = (lambda c: B.attend_codes(Q, c), lambda c: B.cache_read(c, BF), lambda c: B.cache_write(c, K, V))
+    for i in (1, 2, 4, 5):
+        mine = [x.clone() for x in parts]
+        own = B.CodeCache(*mine, d=64, bits=4)
+        for call in calls:
+            call(own)
+        mine[i].requires_grad_()
+        for c in (own, B.CodeCache(*mine, d=64, bits=4)):
+            for call in calls:
+                with pytest.raises(ValueError, match="gradient"):
+                    call(c)
+                with torch.no_grad():
+                    call(c)
+    for out in ({"O": torch.zeros_like(Q).requires_grad_()}, {"lse": torch.zeros(Q.shape[:3], device="cuda", requires_grad=True)}):
+        with pytest.raises(ValueError, match="gradient"):
+            B.attend_codes(Q, cache, out=out)
