@@ -8,6 +8,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libobf_relay.so"
@@ -623,11 +624,15 @@ def _enqueue(device, call, *args):
 
 
 def _forward_only(*tensors):
-    """These calls have no backward pass: what should get a gradient through them is refused, rather than answered without one."""
+    """These calls have no backward pass, nor a forward-mode one: what should get a gradient through them, or carries a tangent, is refused, rather than answered without one."""
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
                 raise ValueError("forward only: no gradient reaches a tensor that requires one (call under torch.no_grad(), or detach it)")
+    if getattr(forward_ad, "_current_level", 0) >= 0:          # (-1: no level is open, no tensor has a tangent)
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("forward only: a tangent would be dropped (hand over the primal of torch.autograd.forward_ad.unpack_dual)")
 
 
 def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
@@ -673,7 +678,7 @@ def attend(Q, K, V, kv_len=None, causal=True, window=0, sink=0, sink_len=None, m
     apart) with kv_len int32 [S,H] rows per head (None: all).  sink_len int32 [S,H]: first rows that stay visible behind a window, per head, in place of
     `sink`, which then says about how many they are, if that is known (for the launch alone).  mass float32 [S,H,rows], in place: accumulated attention weight.
     out: a dict returned by an earlier call of the same shape, whose buffers and workspace are used again.  Returns it: O [S,H*g,T,d], lse [S,H*g,T], ws.
-    Forward only: tensors that require a gradient are refused while gradients are recorded."""
+    Forward only: tensors that require a gradient are refused while gradients are recorded, tensors with a tangent always."""
     return _attend_run(Q, K, V, kv_len, sink_len, causal, window, sink, mass, out)
 
 
@@ -905,7 +910,7 @@ def _attend_codes_plan(cache, Q, O, lse, kv_len, sink_len, causal, window, sink)
 
 def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0, sink_len=None, out=None):
     """obf_attend_codes: attend, over a cache held in codes, without accumulated weights.  Returns a dict as attend does: O [S,H*g,T,d], lse [S,H*g,T], ws.
-    Forward only: queries, outputs or a cache whose scale or zero requires a gradient are refused while gradients are recorded."""
+    Forward only: queries, outputs or a cache whose scale or zero requires a gradient are refused while gradients are recorded, tangents always."""
     o = out if out is not None else {}
     if "O" not in o:
         o["O"] = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)

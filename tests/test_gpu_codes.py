@@ -837,3 +837,21 @@ def test_a_cache_that_requires_a_gradient_is_refused():
     for out in ({"O": torch.zeros_like(Q).requires_grad_()}, {"lse": torch.zeros(Q.shape[:3], device="cuda", requires_grad=True)}):
         with pytest.raises(ValueError, match="gradient"):
             B.attend_codes(Q, cache, out=out)
+
+
+def test_tangents_are_refused():
+    """Forward-mode tangents would be dropped: every forward-only call refuses them."""
+    import torch.autograd.forward_ad as fwd
+    B = _b()
+    Q, K, V = (x.cuda() for x in _make(29, BF, 64, 1, 2, 1, 3, 3))
+    cache = B.cache_write(B.code_cache(1, 2, 3, 64, 4), K, V)
+    mass = torch.zeros((1, 2, 3), device="cuda")
+    with fwd.dual_level():
+        B.attend_codes(Q, cache)
+        B.attend(Q, K, V)
+        q, k = (fwd.make_dual(x, torch.ones_like(x)) for x in (Q, K))
+        own = B.CodeCache(cache.K_codes, fwd.make_dual(cache.K_scale, torch.ones_like(cache.K_scale)), cache.K_zero, cache.V_codes, cache.V_scale, cache.V_zero, d=64, bits=4)
+        for call in (lambda: B.attend_codes(q, cache), lambda: B.attend_codes(Q, own), lambda: B.cache_read(own, BF), lambda: B.cache_write(cache, k, V), lambda: B.attend(q, K, V),
+                     lambda: B.attend(Q, k, V), lambda: B.evict(k, V, mass, budget=2)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
