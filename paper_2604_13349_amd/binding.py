@@ -766,12 +766,26 @@ def evict(K, V, mass, budget: int, kv_len=None, recent: int = 0, sink: int = 0, 
     return o
 
 
+_CODES = ("K_codes", "K_scale", "K_zero", "V_codes", "V_scale", "V_zero")
+
+
+def _kept(i):
+    return property(lambda self: self._kept[i].detach(), doc=f"A view of {_CODES[i]}.")
+
+
 class CodeCache:
     """A cache held in codes of 4 or 8 bits (obf_codes_t): K_codes, V_codes uint8 [S,H,rows,d*bits/8], K_scale, K_zero, V_scale, V_zero float16 [S,H,rows];
     samples any whole number of rows apart, the same in all six, the heads of a sample contiguous (a layer of [S,L,H,...] tensors is a cache as it lies).  Rows
-    are what quantize_rows makes of them.  Shapes, strides and devices are checked here, once: the tensors keep them."""
+    are what quantize_rows makes of them.  Shapes, strides and devices are checked here, once, and views of the tensors kept: attributes are read-only, and what
+    happens to the layout of a tensor later (resize_, set_, transpose_), its own or one that an attribute gave, changes nothing here."""
 
-    __slots__ = ("K_codes", "K_scale", "K_zero", "V_codes", "V_scale", "V_zero", "d", "bits", "shape", "between", "device")
+    __slots__ = ("_kept", "_numbers", "_layout")
+    K_codes, K_scale, K_zero, V_codes, V_scale, V_zero = map(_kept, range(6))
+    shape = property(lambda self: self._layout[0], doc="(samples, heads, rows)")
+    between = property(lambda self: self._layout[1], doc="rows between samples")
+    d = property(lambda self: self._layout[2])
+    bits = property(lambda self: self._layout[3])
+    device = property(lambda self: self._layout[4])
 
     def __init__(self, K_codes, K_scale, K_zero, V_codes, V_scale, V_zero, d: int, bits: int):
         d, bits = _int("d", d), _int("bits", bits)
@@ -795,20 +809,13 @@ class CodeCache:
             if between is not None and apart != between:
                 raise ValueError(f"{name} must have the row strides of K_codes")
             between = apart
-        self.K_codes, self.K_scale, self.K_zero, self.V_codes, self.V_scale, self.V_zero = K_codes, K_scale, K_zero, V_codes, V_scale, V_zero
-        self.d, self.bits, self.shape, self.between, self.device = d, bits, (S, H, rows), between, K_codes.device
-
-    def _layout(self):
-        return self.shape, self.between, self.d, self.bits, self.device
+        self._kept = tuple([t.detach() for t in (K_codes, K_scale, K_zero, V_codes, V_scale, V_zero)])
+        self._numbers = K_scale, K_zero, V_scale, V_zero               # as given: they may require a gradient, now or later
+        self._layout = (S, H, rows), between, d, bits, K_codes.device
 
     def _codes(self):
-        return (_Codes(self.K_codes.data_ptr(), self.K_scale.data_ptr(), self.K_zero.data_ptr()),
-                _Codes(self.V_codes.data_ptr(), self.V_scale.data_ptr(), self.V_zero.data_ptr()))
-
-
-def _numbers(cache):
-    """The tensors of a cache that may require a gradient."""
-    return () if cache is None else (cache.K_scale, cache.K_zero, cache.V_scale, cache.V_zero)
+        at = [t.data_ptr() for t in self._kept]
+        return _Codes(*at[:3]), _Codes(*at[3:])
 
 
 def code_cache(samples: int, heads: int, rows: int, d: int, bits: int = 4, device="cuda") -> CodeCache:
@@ -849,12 +856,12 @@ def cache_write(cache: CodeCache, K, V, kv_len=None, n_new=None):
     """obf_cache_write: K, V [S,H,T,d] (any strides of 16 bytes, last dimension contiguous) become the newest rows of the cache's heads.  kv_len int32 [S,H]:
     rows per head with the new ones (None: the cache is full then); n_new int32 [S,H]: how many of the T rows are a head's (None: all), the first of them.
     Forward only, as attend.  Returns the cache."""
-    _forward_only(K, V, *_numbers(cache))
-    c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), _meta(n_new), None)
+    _forward_only(K, V, *getattr(cache, "_numbers", ()))
+    c, copy_lens = _rows_plan(cache._layout, _meta(K), _meta(V), _meta(kv_len), _meta(n_new), None)
     if copy_lens:
         kv_len, n_new = (None if t is None else t.contiguous() for t in (kv_len, n_new))
     kc, vc = cache._codes()
-    _enqueue(cache.device, load_library().obf_cache_write, C.byref(c), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(n_new), C.byref(kc), C.byref(vc))
+    _enqueue(cache._layout[4], load_library().obf_cache_write, C.byref(c), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(n_new), C.byref(kc), C.byref(vc))
     return cache
 
 
@@ -863,19 +870,19 @@ def cache_read(cache: CodeCache, dtype: torch.dtype, kv_len=None, idx=None, out=
     head has no such row they stay as they are.  Without it they are made, with zeros in such places.  Forward only, as attend.
     Returns the dict."""
     o = out if out is not None else {}
-    S, H, rows = cache.shape
+    (S, H, rows), _, d, _, device = cache._layout
     for name in ("K_out", "V_out"):
         if name not in o:
-            o[name] = torch.zeros((S, H, rows if idx is None else idx.shape[-1], cache.d), dtype=dtype, device=cache.device)
+            o[name] = torch.zeros((S, H, rows if idx is None else idx.shape[-1], d), dtype=dtype, device=device)
     K, V = o["K_out"], o["V_out"]
     if K.dtype != dtype:
         raise ValueError(f"K_out is {K.dtype}, not {dtype}")
-    _forward_only(K, V, *_numbers(cache))
-    c, copy_lens = _rows_plan(cache._layout(), _meta(K), _meta(V), _meta(kv_len), None, _meta(idx))
+    _forward_only(K, V, *getattr(cache, "_numbers", ()))
+    c, copy_lens = _rows_plan(cache._layout, _meta(K), _meta(V), _meta(kv_len), None, _meta(idx))
     if copy_lens:
         kv_len = kv_len.contiguous()
     kc, vc = cache._codes()
-    _enqueue(cache.device, load_library().obf_cache_read, C.byref(c), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(idx), K.data_ptr(), V.data_ptr())
+    _enqueue(cache._layout[4], load_library().obf_cache_read, C.byref(c), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(idx), K.data_ptr(), V.data_ptr())
     return o
 
 
@@ -917,14 +924,14 @@ def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0
     if "lse" not in o:
         o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
     O, lse = o["O"], o["lse"]
-    _forward_only(Q, O, lse, *_numbers(cache))
-    c, need, copy_lens = _attend_codes_plan(cache._layout(), _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
+    _forward_only(Q, O, lse, *getattr(cache, "_numbers", ()))
+    c, need, copy_lens = _attend_codes_plan(cache._layout, _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
                                             _int("sink", sink))
-    ws = o["ws"] = _workspace(o.get("ws"), need, cache.device)
+    ws = o["ws"] = _workspace(o.get("ws"), need, cache._layout[4])
     if copy_lens:
         kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
     kc, vc = cache._codes()
-    _enqueue(cache.device, load_library().obf_attend_codes, C.byref(c), cache.bits, Q.data_ptr(), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(sink_len), O.data_ptr(),
+    _enqueue(cache._layout[4], load_library().obf_attend_codes, C.byref(c), cache._layout[3], Q.data_ptr(), C.byref(kc), C.byref(vc), _addr(kv_len), _addr(sink_len), O.data_ptr(),
              lse.data_ptr(), ws.data_ptr(), ws.nbytes)
     return o
 

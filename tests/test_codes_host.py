@@ -171,6 +171,15 @@ def test_tensors_must_be_on_a_gpu_and_need_no_gradient():
             call()
 
 
+def test_a_cache_keeps_its_tensors_and_its_layout():
+    """Both are checked where the cache is made, and go to the GPU as they were then."""
+    cache = object.__new__(B.CodeCache)
+    for name in ("K_codes", "K_scale", "K_zero", "V_codes", "V_scale", "V_zero", "d", "bits", "shape", "between", "device"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, 8)
+            pytest.fail(f"{name} was set")
+
+
 def test_definition_on_known_answers():
     """The code's values by hand; over exact codes the attention is that of the values."""
     q, s, z = R.quantise(torch.tensor([[1.0, 2.0, 8.5, 16.0]]), 4)

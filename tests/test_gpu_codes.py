@@ -855,3 +855,25 @@ def test_tangents_are_refused():
                      lambda: B.attend(Q, k, V), lambda: B.evict(k, V, mass, budget=2)):
             with pytest.raises(ValueError, match="tangent"):
                 call()
+
+
+def test_a_cache_whose_tensors_change_their_layout():
+    """resize_, set_ and the like, of the tensors that the cache was made of and of those that its attributes give: the calls go on with the memory that was checked."""
+    B = _b()
+    Q, K, V = (x.cuda() for x in _make(30, BF, 64, 2, 2, 1, 3, 40))
+    made = B.cache_write(B.code_cache(2, 2, 40, 64, 4), K, V)
+    want, rows = B.attend_codes(Q, made), B.cache_read(made, BF)
+    changes = [lambda t: t.resize_((1,) + tuple(t.shape[1:])), lambda t: t.resize_((5,) + tuple(t.shape[1:])), lambda t: t.set_(torch.zeros_like(t[:1, :1, :1])),
+               lambda t: t.transpose_(1, 2), lambda t: t.resize_(0)]
+    for change in changes:
+        for i, name in enumerate(NAMES):
+            parts = [getattr(made, n).clone() for n in NAMES]
+            cache = B.CodeCache(*parts, d=64, bits=4)
+            change(parts[i])
+            change(getattr(cache, name))
+            assert getattr(cache, name).shape == getattr(made, name).shape and cache.shape == (2, 2, 40)
+            o, r = B.attend_codes(Q, cache), B.cache_read(cache, BF)
+            assert torch.equal(o["O"], want["O"]) and torch.equal(o["lse"], want["lse"])
+            assert torch.equal(r["K_out"], rows["K_out"]) and torch.equal(r["V_out"], rows["V_out"])
+            B.cache_write(cache, V, K)
+            assert torch.equal(cache.K_codes, made.V_codes) and torch.equal(cache.V_zero, made.K_zero)
