@@ -862,6 +862,7 @@ def cache_write(cache: CodeCache, K, V, kv_len=None, n_new=None):
         kv_len, n_new = (None if t is None else t.contiguous() for t in (kv_len, n_new))
     kc, vc = cache._codes()
     _enqueue(cache._layout[4], load_library().obf_cache_write, C.byref(c), K.data_ptr(), V.data_ptr(), _addr(kv_len), _addr(n_new), C.byref(kc), C.byref(vc))
+    torch.autograd.graph.increment_version(cache._kept)           # (autograd may have kept one of them for a backward pass)
     return cache
 
 

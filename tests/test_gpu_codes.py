@@ -877,3 +877,22 @@ def test_a_cache_whose_tensors_change_their_layout():
             assert torch.equal(r["K_out"], rows["K_out"]) and torch.equal(r["V_out"], rows["V_out"])
             B.cache_write(cache, V, K)
             assert torch.equal(cache.K_codes, made.V_codes) and torch.equal(cache.V_zero, made.K_zero)
+
+
+def test_a_write_counts_as_a_change_of_the_caches_tensors():
+    """What autograd kept of a cache for its backward pass is not the cache any more once rows were written into it."""
+    B = _b()
+    _, K, V = (x.cuda() for x in _make(31, BF, 64, 1, 2, 1, 1, 4))
+    cache = B.cache_write(B.code_cache(1, 2, 8, 64, 8), K, V, kv_len=torch.full((1, 2), 4, dtype=torch.int32, device="cuda"))
+    w = torch.ones((1, 2, 8), dtype=torch.float16, device="cuda", requires_grad=True)
+    before = [getattr(cache, n)._version for n in NAMES]
+    kept = (cache.V_scale * w).sum()
+    B.attend_codes(K, cache)
+    B.cache_read(cache, BF)
+    assert [getattr(cache, n)._version for n in NAMES] == before
+    B.cache_write(cache, K, V)
+    assert all(getattr(cache, n)._version > b for n, b in zip(NAMES, before))
+    with pytest.raises(RuntimeError, match="inplace"):
+        kept.backward()
+    with torch.inference_mode():
+        B.cache_write(cache, K, V)
