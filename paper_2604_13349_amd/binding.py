@@ -483,6 +483,13 @@ def _int(name: str, v) -> int:
     return v
 
 
+def _sizes(**sizes):
+    """Sizes of tensors that the C side takes as int32: an expanded tensor may have larger ones."""
+    for name, v in sizes.items():
+        if v >= 1 << 31:
+            raise ValueError(f"{name} {v} is out of range")
+
+
 def _meta(t: Optional[torch.Tensor]):
     """What a call is checked and laid out by; never a tensor's address."""
     return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
@@ -535,6 +542,12 @@ def _row_strides(name: str, m, d: int):
     return [stride[i] if shape[i] > 1 else d * max(1, shape[2]) for i in range(3)]
 
 
+def _lens_layout(S: int, H: int, metas):
+    """(entries between samples, 0: heads of all samples contiguous, or one sample; whether the lengths have to be made contiguous) of int32 [S, H] tensors."""
+    copy = any(H > 1 and m[1][1] != 1 or S > 1 and not H <= m[1][0] < 1 << 31 for m in metas) or len({m[1][0] for m in metas if S > 1}) > 1
+    return (metas[0][1][0] if metas and S > 1 and not copy else 0), copy
+
+
 @functools.lru_cache(maxsize=1024)
 def _attend_plan(Q, K, V, O, lse, mass, kv_len, sink_len, prefix_K, prefix_V, prefix_len, causal, window, sink):
     """The descriptor of an attention call and what goes with it, from the tensors' metadata, which is checked: (obf_attend_t, bytes of workspace, rows of the
@@ -559,12 +572,12 @@ def _attend_plan(Q, K, V, O, lse, mass, kv_len, sink_len, prefix_K, prefix_V, pr
         _want("mass", mass, (S, H, rows), torch.float32, contiguous=False)
         if H > 1 and mass[1][1] != rows or rows > 1 and mass[1][2] != 1 or S > 1 and mass[1][0] != between:
             raise ValueError("mass must have the row strides of K")
-    lens = [m for m in (kv_len, sink_len) if m is not None]
     _want("kv_len", kv_len, (S, H), torch.int32, contiguous=False)
     _want("sink_len", sink_len, (S, H), torch.int32, contiguous=False)
-    copy_lens = any(H > 1 and m[1][1] != 1 or S > 1 and m[1][0] < H for m in lens) or len({m[1][0] for m in lens if S > 1}) > 1
+    len_stride, copy_lens = _lens_layout(S, H, [m for m in (kv_len, sink_len) if m is not None])
+    _sizes(samples=S, heads=H, query_heads=Hq, queries=T, rows=rows)
     c = _Attend(S, H, Hq // H, d, T, rows, OBF_F32 if dtype == torch.float32 else OBF_BF16, int(bool(causal)), int(window), int(sink), rows,
-                lens[0][1][0] if lens and S > 1 and not copy_lens else 0, between)
+                len_stride, between)
     c.q_stride = (C.c_int64 * 3)(*_row_strides("Q", Q, d))
     if O is not None:
         _want("O", O, Q[0], dtype, contiguous=False)
@@ -825,12 +838,6 @@ def code_cache(samples: int, heads: int, rows: int, d: int, bits: int = 4, devic
     return CodeCache(*both[0], *both[1], d=d, bits=bits)
 
 
-def _lens_layout(S: int, H: int, metas):
-    """(entries between samples, 0: heads of all samples contiguous, or one sample; whether the lengths have to be made contiguous) of int32 [S, H] tensors."""
-    copy = any(H > 1 and m[1][1] != 1 or S > 1 and m[1][0] < H for m in metas) or len({m[1][0] for m in metas if S > 1}) > 1
-    return (metas[0][1][0] if metas and S > 1 and not copy else 0), copy
-
-
 @functools.lru_cache(maxsize=1024)
 def _rows_plan(cache, K, V, kv_len, per_head, idx):
     """The descriptor of a cache_write (per_head: n_new) or cache_read (idx) from the tensors' metadata, which is checked: (obf_cache_rows_t, whether the
@@ -846,6 +853,7 @@ def _rows_plan(cache, K, V, kv_len, per_head, idx):
     _want("n_new", per_head, (S, H), torch.int32, contiguous=False)
     _want("idx", idx, K[0][:3], torch.int32)
     len_stride, copy_lens = _lens_layout(S, H, [m for m in (kv_len, per_head) if m is not None])
+    _sizes(samples=S, heads=H, rows=rows, rows_of_K=K[0][2])
     c = _CacheRows(S, H, d, bits, OBF_F32 if K[2] == torch.float32 else OBF_BF16, K[0][2], rows, rows, len_stride, between)
     c.k_stride = (C.c_int64 * 3)(*_row_strides("K", K, d))
     c.v_stride = (C.c_int64 * 3)(*_row_strides("V", V, d))
@@ -903,6 +911,7 @@ def _attend_codes_plan(cache, Q, O, lse, kv_len, sink_len, causal, window, sink)
     _want("O", O, Q[0], Q[2], contiguous=False)
     _want("lse", lse, Q[0][:3], torch.float32)
     len_stride, copy_lens = _lens_layout(S, H, [m for m in (kv_len, sink_len) if m is not None])
+    _sizes(samples=S, heads=H, query_heads=Q[0][1], queries=Q[0][2], rows=rows)
     c = _Attend(S, H, Q[0][1] // H, d, Q[0][2], rows, OBF_F32 if Q[2] == torch.float32 else OBF_BF16, int(causal), window, sink, rows, len_stride, between)
     c.q_stride = (C.c_int64 * 3)(*_row_strides("Q", Q, d))
     so = _row_strides("O", O, d)

@@ -180,6 +180,32 @@ def test_a_cache_keeps_its_tensors_and_its_layout():
             pytest.fail(f"{name} was set")
 
 
+def test_sizes_and_strides_past_32_bits(lib):
+    """The C side takes them as int32: lengths that lie further apart are copied, an expanded tensor of more rows is refused.  By the plans, which go by metadata alone."""
+    dev = torch.device("cuda", 0)
+    cache, far = ((2, 3, 40), 120, 128, 4, dev), 1 << 32
+
+    def meta(shape, stride, dtype):
+        return torch.Size(shape), stride, dtype, dev
+
+    Q, lse = meta((2, 3, 1, 128), (384, 128, 128, 1), torch.bfloat16), meta((2, 3, 1), (3, 1, 1), torch.float32)
+    K = meta((2, 3, 40, 128), (15360, 5120, 128, 1), torch.bfloat16)
+    for apart, stride, copy in ((3, 3, False), (7, 7, False), ((1 << 31) - 1, (1 << 31) - 1, False), (1 << 31, 0, True), (far + 3, 0, True)):
+        n = meta((2, 3), (apart, 1), torch.int32)
+        for c, *_, copied in (B._attend_codes_plan(cache, Q, Q, lse, n, n, True, 0, 0), B._rows_plan(cache, K, K, n, n, None),
+                              B._attend_plan(Q, K, K, Q, lse, None, n, n, None, None, None, True, 0, 0)):
+            assert (c.len_stride, copied) == (stride, copy)
+    one = meta((2, 3, far + 5, 128), (384, 128, 0, 1), torch.bfloat16)
+    with pytest.raises(ValueError, match="out of range"):
+        B._rows_plan(cache, one, one, None, None, None)
+    for wide in (((2, 3, far + 40), 3 * (far + 40), 128, 4, dev), ((far + 2, 3, 40), 120, 128, 4, dev)):
+        k = meta(wide[0][:2] + (1, 128), (384, 128, 128, 1), torch.bfloat16)
+        with pytest.raises(ValueError, match="out of range"):
+            B._rows_plan(wide, k, k, None, None, None)
+        with pytest.raises(ValueError, match="out of range"):
+            B._attend_codes_plan(wide, k, k, meta(wide[0][:2] + (1,), (3, 1, 1), torch.float32), None, None, True, 0, 0)
+
+
 def test_definition_on_known_answers():
     """The code's values by hand; over exact codes the attention is that of the values."""
     q, s, z = R.quantise(torch.tensor([[1.0, 2.0, 8.5, 16.0]]), 4)
