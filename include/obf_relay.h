@@ -477,8 +477,10 @@ obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_c
  * Rows at and behind a head's length are not read, and no number of a row that a query does not see reaches its result; a visible
  * row whose scale or zero is infinite or no number makes, in K, O and lse of the queries that see it no number, in V their O alone
  * (no number or infinite).  K and V name the codes' arrays, which are inputs.  The workspace holds half-precision copies
- * of the cache's rows, up to 4 GiB, where about 2^11 query rows per KV head or more see a row. */
+ * of the cache's rows, up to 4 GiB, where about 2^11 query rows per KV head or more see a row; one with less than these bytes, but
+ * the `least`, serves the call too, which then takes longer. */
 size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits);
+size_t obf_attend_codes_workspace_least(const obf_attend_t* call, int32_t bits);
 obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V,
                               const int32_t* kv_len, const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes,
                               void* stream);

@@ -154,6 +154,8 @@ def load_library():
     lib.obf_cache_read.argtypes = [rp, cp, cp, vp, vp, vp, vp, vp]
     lib.obf_attend_codes_workspace_bytes.restype = sz
     lib.obf_attend_codes_workspace_bytes.argtypes = [ap, i32]
+    lib.obf_attend_codes_workspace_least.restype = sz
+    lib.obf_attend_codes_workspace_least.argtypes = [ap, i32]
     lib.obf_attend_codes.restype = C.c_int
     lib.obf_attend_codes.argtypes = [ap, i32, vp, cp, cp, vp, vp, vp, vp, vp, sz, vp]
     lib.obf_profile_enable.restype = C.c_int
@@ -648,10 +650,15 @@ def _forward_only(*tensors):
                 raise ValueError("forward only: a tangent would be dropped (hand over the primal of torch.autograd.forward_ad.unpack_dual)")
 
 
-def _workspace(ws: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
-    """ws, if it holds `need` bytes of its own on the device, or a new one."""
+def _workspace(ws: Optional[torch.Tensor], need: int, device, least: Optional[int] = None) -> torch.Tensor:
+    """ws, if it holds `need` bytes of its own on the device, or a new one; one of `least` bytes where the memory for it is not there."""
     if ws is None or ws.nbytes < need or ws.device != device or not ws.is_contiguous():
-        return torch.empty(need, dtype=torch.uint8, device=device)
+        try:
+            return torch.empty(need, dtype=torch.uint8, device=device)
+        except torch.OutOfMemoryError:
+            if least is None or least >= need:
+                raise
+        return torch.empty(least, dtype=torch.uint8, device=device)
     return ws
 
 
@@ -897,7 +904,7 @@ def cache_read(cache: CodeCache, dtype: torch.dtype, kv_len=None, idx=None, out=
 
 @functools.lru_cache(maxsize=1024)
 def _attend_codes_plan(cache, Q, O, lse, kv_len, sink_len, causal, window, sink):
-    """As _attend_plan: (obf_attend_t, bytes of workspace, whether the lengths have to be made contiguous)."""
+    """As _attend_plan: (obf_attend_t, bytes of workspace, the least of them, whether the lengths have to be made contiguous)."""
     (S, H, rows), between, d, bits, device = cache
     for name, m in (("Q", Q), ("O", O), ("lse", lse), ("kv_len", kv_len), ("sink_len", sink_len)):
         if m is not None and m[3] != device:
@@ -919,10 +926,10 @@ def _attend_codes_plan(cache, Q, O, lse, kv_len, sink_len, causal, window, sink)
         raise ValueError("O: rows must not overlap")
     c.o_stride = (C.c_int64 * 3)(*so)
     lib = load_library()
-    need = int(lib.obf_attend_codes_workspace_bytes(C.byref(c), bits))
+    need, least = int(lib.obf_attend_codes_workspace_bytes(C.byref(c), bits)), int(lib.obf_attend_codes_workspace_least(C.byref(c), bits))
     if need == 0:
         raise ObfError(2, lib.obf_last_error().decode())
-    return c, need, copy_lens
+    return c, need, least, copy_lens
 
 
 def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0, sink_len=None, out=None):
@@ -935,9 +942,9 @@ def attend_codes(Q, cache: CodeCache, kv_len=None, causal=True, window=0, sink=0
         o["lse"] = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
     O, lse = o["O"], o["lse"]
     _forward_only(Q, O, lse, *getattr(cache, "_numbers", ()))
-    c, need, copy_lens = _attend_codes_plan(cache._layout, _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
+    c, need, least, copy_lens = _attend_codes_plan(cache._layout, _meta(Q), _meta(O), _meta(lse), _meta(kv_len), _meta(sink_len), bool(causal), _int("window", window),
                                             _int("sink", sink))
-    ws = o["ws"] = _workspace(o.get("ws"), need, cache._layout[4])
+    ws = o["ws"] = _workspace(o.get("ws"), need, cache._layout[4], least)
     if copy_lens:
         kv_len, sink_len = (None if t is None else t.contiguous() for t in (kv_len, sink_len))
     kc, vc = cache._codes()

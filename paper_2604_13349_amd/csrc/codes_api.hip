@@ -94,7 +94,7 @@ static obf_status_t check_rows_apart(const obf_cache_rows_t* c, const CacheRowsA
   return check_apart(outs, 2, ins, 8);
 }
 
-struct AttendCodesPlan { AttendCodesArgs c; bool tile, rows; int waves; size_t part_O, part_lse, rows_k, rows_v, numbers, bad, total; };
+struct AttendCodesPlan { AttendCodesArgs c; bool tile, rows; int waves; size_t part_O, part_lse, least, rows_k, rows_v, numbers, bad, total; };      // least: without the rows' numbers
 
 // Ranges of a launch of the kernel of many rows: the least of an estimate, in us.  A workgroup takes its tiles of 64 rows and as long as two more to begin and end, alone on a
 // compute unit `step` a tile, two in 1.5 times that, more one after another; a join 3 and the partial results' way to memory and back.  Of 190 shapes (8 to 128 heads of 700 to
@@ -168,6 +168,7 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   if (a.ranges > 1) at += (size_t)a.ranges * a.rows * d * sizeof(float);
   p.part_lse = at;
   if (a.ranges > 1) at += ((size_t)a.ranges * a.rows * sizeof(float) + 255) & ~(size_t)255;
+  p.least = at ? at : 256;
   // Numbers made once for all workgroups of a head, where 16 or more of them read a row and the copies stay under 4 GiB (us, by every workgroup and once: 8 heads of 8000
   // rows, 4, 8, 16 and 32 tiles of query rows 49 - 58, 66 - 72, 108 - 108, 236 - 190; 8 x 8 heads of 4000, 8 and 16 tiles 189 - 200, 342 - 332).
   const long readers = k.window > 0 && k.window * (long)a.g / kAttendTileRows < k.row_tiles ? k.window * (long)a.g / kAttendTileRows + 1 : k.row_tiles;
@@ -182,7 +183,7 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   if (p.rows) at += ((size_t)a.S * a.H * k.stride * sizeof(uint2) + 255) & ~(size_t)255;
   p.bad = at;
   if (p.rows) at += ((size_t)a.S * a.H * p.c.flags + 255) & ~(size_t)255;
-  p.total = at ? at : 256;
+  p.total = p.rows ? at : p.least;
   return p;
 }
 
@@ -222,6 +223,12 @@ size_t obf_attend_codes_workspace_bytes(const obf_attend_t* call, int32_t bits) 
   return with > without ? with : without;
 }
 
+size_t obf_attend_codes_workspace_least(const obf_attend_t* call, int32_t bits) {
+  if (check_attend(call) != OBF_OK || check_bits(bits) != OBF_OK) return 0;
+  const size_t with = plan_attend_codes(call, bits, true).least, without = plan_attend_codes(call, bits, false).least;
+  return with > without ? with : without;
+}
+
 obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void* Q, const obf_codes_t* K, const obf_codes_t* V, const int32_t* kv_len,
                               const int32_t* sink_len, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
   OBF_TRY(check_attend(call));
@@ -229,6 +236,7 @@ obf_status_t obf_attend_codes(const obf_attend_t* call, int32_t bits, const void
   OBF_TRY(check_aligned("Q", Q)); OBF_TRY(check_aligned("O", O));
   OBF_TRY(check_codes("K", K)); OBF_TRY(check_codes("V", V));
   AttendCodesPlan p = plan_attend_codes(call, bits, sink_len != nullptr);
+  if (ws_bytes < p.total) { p.rows = false; p.total = p.least; }
   OBF_TRY(check_attend_ws(p.total, ws, ws_bytes));
   AttendArgs& a = p.c.a;
   a.Q = Q; a.O = O; a.lse = lse;

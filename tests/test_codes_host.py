@@ -148,6 +148,24 @@ def test_a_workspace_serves_calls_with_and_without_first_rows_per_head(lib):
     assert len(sizes) > 500
 
 
+def test_the_least_workspace(lib):
+    """A call that would like copies of the rows takes a workspace without them, and none that is smaller; one that needs none asks for the same bytes both times."""
+    codes = B._Codes(1 << 50, 1 << 51, 1 << 52)
+    for S, H, g, d, T, rows, window, copies in ((1, 2, 4, 128, 1, 40000, 0, False), (1, 8, 4, 128, 4096, 13517, 0, True), (3, 8, 5, 64, 500, 2139, 0, True), (1, 2, 2, 128, 3000, 5000, 2048, True),
+                                                (1, 2, 2, 128, 3000, 5000, 64, False)):
+        for bits in (4, 8):
+            c = B._Attend(S, H, g, d, T, rows, B.OBF_BF16, 1, window, 0, rows, 0, 0)
+            need, least = lib.obf_attend_codes_workspace_bytes(C.byref(c), bits), lib.obf_attend_codes_workspace_least(C.byref(c), bits)
+            assert (need - least >= 4 * S * H * rows * d) if copies else need == least
+            for sink_len in (None, 1 << 53):
+                for size, status, word in ((need, 1, "overlap"), (least, 1, "overlap"), (need - 1, 1, "overlap") if copies else (need, 1, "overlap")):
+                    rc = lib.obf_attend_codes(C.byref(c), bits, 1 << 40, C.byref(codes), C.byref(codes), None, sink_len, 1 << 40, None, 1 << 60, size, None)
+                    assert rc == status and word in lib.obf_last_error().decode()
+                small = min(255, least - 1)
+                assert lib.obf_attend_codes(C.byref(c), bits, 1 << 40, C.byref(codes), C.byref(codes), None, sink_len, 1 << 41, None, 1 << 60, small, None) == 3
+    assert lib.obf_attend_codes_workspace_least(C.byref(c), 5) == 0
+
+
 @pytest.mark.parametrize("kind", ["write", "read"])
 @pytest.mark.parametrize("samples, heads, rows", [(65535, 1, 8192), (1 << 14, 2, 1 << 14), (1 << 13, 7, 9362), (32, 1, 1 << 24)])
 def test_a_launch_has_fewer_than_2_32_threads(lib, kind, samples, heads, rows):

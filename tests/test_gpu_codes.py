@@ -632,6 +632,48 @@ def test_repeated_calls_and_a_used_workspace_change_no_bit(T, rows):
     assert torch.equal(again["O"], first[0]) and torch.equal(again["lse"], first[1])
 
 
+@pytest.mark.parametrize("S,H,g,d,T,rows,window", [(1, 2, 2, 128, 1100, 1500, 0), (2, 2, 4, 64, 600, 1300, 0), (1, 1, 8, 128, 300, 7000, 0), (1, 2, 2, 64, 1500, 2600, 1200)])
+def test_a_workspace_without_room_for_copies(S, H, g, d, T, rows, window, monkeypatch):
+    """Prompts that go over copies of the rows go without them where the memory is not there, and write nothing behind the least workspace."""
+    B = _b()
+    Q, K, V = _make(33, BF, d, S, H, g, T, rows)
+    kv_len = _lens(9, S, H, T, rows)
+    k, v = R.quantise(K, 4), R.quantise(V, 4)
+    cache = _cache(k, v, 4, d)
+    kw = dict(window=window, sink=3)
+    if S * H * -(-g * T // 16) <= 768:                        # (by the kernel of many rows: among samples without any)
+        more = 768 // (H * (g * T // 16)) + 1
+        Q, kv_len = torch.cat([Q, Q[:1].expand(more, -1, -1, -1)]), torch.cat([kv_len, torch.zeros((more, H), dtype=torch.int32)])
+        k, v = (tuple(torch.cat([x, x[:1].expand((more,) + tuple(x.shape[1:]))]) for x in y) for y in (k, v))
+        cache = _cache(k, v, 4, d)
+    full = B.attend_codes(Q.cuda(), cache, kv_len=kv_len.cuda(), **kw)
+    empty = torch.empty
+
+    def short(*size, **more):
+        if more.get("dtype") == torch.uint8 and size[0] == full["ws"].nbytes:
+            raise torch.OutOfMemoryError("no room")
+        return empty(*size, **more)
+
+    monkeypatch.setattr(torch, "empty", short)
+    o = B.attend_codes(Q.cuda(), cache, kv_len=kv_len.cuda(), **kw)
+    monkeypatch.undo()
+    c, need, least, _ = B._attend_codes_plan(cache._layout, B._meta(Q.cuda()), B._meta(o["O"]), B._meta(o["lse"]), B._meta(kv_len.cuda()), None, True, window, 3)
+    assert o["ws"].nbytes == least < need == full["ws"].nbytes and need - least >= 4 * Q.shape[0] * H * rows * d
+    want, lse, tO, tl = R.attend(Q[:S], *(tuple(x[:S] for x in y) for y in (k, v)), 4, kv_len[:S], **kw)
+    for x in (full, o):
+        _check("O", x["O"][:S], want, tO)
+        _check("lse", x["lse"][:S], lse, tl)
+    # the same by the C side, over a workspace with something behind it
+    import ctypes as C
+    ws = torch.full((least + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    kc, vc = cache._codes()
+    qd, nd, O, l = Q.cuda(), kv_len.cuda(), torch.zeros_like(o["O"]), torch.zeros_like(o["lse"])
+    rc = B.load_library().obf_attend_codes(C.byref(c), 4, qd.data_ptr(), C.byref(kc), C.byref(vc), nd.data_ptr(), None, O.data_ptr(), l.data_ptr(), ws.data_ptr(), least,
+                                           torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == 0 and torch.equal(O, o["O"]) and torch.equal(l, o["lse"]) and (ws[least:] == 0x5A).all()
+
+
 @pytest.mark.parametrize("T,rows,window", [(1, 600, 400), (3, 5000, 400), (100, 1600, 400), (100, 7000, 0)])
 def test_captured_steps_replay(T, rows, window):
     """Lengths grow, rows are written, read back and attended over in one graph; two graphs with a cache and a workspace each, replayed in turn with eager work between."""
