@@ -472,8 +472,9 @@ obf_status_t obf_cache_read(const obf_cache_rows_t* call, const obf_codes_t* K_c
 
 /* obf_attend over a cache held in codes (without accumulated weights); call->dtype is that of Q and O.  A row stands for zero + scale * q,
  * unrounded; sums and statistics are single precision, the codes, and the queries under a power of two per row, enter the products as half-precision
- * numbers (fp32 queries as two, 22 bits).  The weights, times the rows' scales, have 11 bits, with fp32 22.  Where bf16 query rows are many
- * (more than 64, n_queries * group, per KV head, and by the sizes of the call) V's values enter rounded to half precision, those past its range as the largest ones.
+ * numbers (fp32 queries as two, within 2^-23 of an element).  The weights, times the rows' scales, have 11 bits, with fp32 they are within 2^-23; sums over
+ * 4-bit values of a bf16 call may drop what lies 2^-20 below a largest term.  Where bf16 query rows are many (more than 64, n_queries * group, per KV head,
+ * and by the sizes of the call) V's values enter rounded to half precision, those past its range as the largest ones.
  * Rows at and behind a head's length are not read, and no number of a row that a query does not see reaches its result; a visible
  * row whose scale or zero is infinite or no number makes, in K, O and lse of the queries that see it no number, in V their O alone
  * (no number or infinite).  K and V name the codes' arrays, which are inputs.  The workspace holds half-precision copies

@@ -1,4 +1,4 @@
-// Attention over a cache held in codes of 4 or 8 bits, few query rows per KV head (and any number of fp32 rows).
+// Attention over a cache held in codes of 4 or 8 bits, few query rows per KV head; and any number of them over short caches, and of fp32 rows.
 //
 //   x_rj = (s_j q_r . c_j + z_j sum_c q_rc) / sqrt(d),  O_r = sum_j w_rj (s_j c_j + z_j),  w_rj = exp(x_rj - lse_r) over the visible rows j
 //
@@ -13,13 +13,17 @@
 // fp32: codes less the one in the middle of the range, beside the value of that one in the place of the zero, so that the two sums are small where the values lie
 // about 0 (3 x 2 heads, 333 queries: 4e-6 of the result's norm off 64 bits with the codes as they are, 2e-7 so, where the same sums in fp32 are 4e-7 off).
 // Q enters as half-precision numbers under a power of two per row, so that its largest lies in [2^14, 2^15): bf16 exactly but for elements 2^-39 of the largest, fp32
-// as two parts of 11 bits.  The weights times s_j enter V's product as half-precision numbers of 11 bits (fp32: two parts): relative to a reference that follows the
-// largest of 2^x_rj |s_j|, so that the largest product lies in [2^7, 2^15] whatever the scales are.  l, sum_j w z_j and O' are single precision.
+// as two parts, rounded, which three numbers in four are exactly and the others within 2^-23.  The weights times s_j enter V's product as half-precision numbers of 11 bits, behind
+// which the result is rounded to 8 (fp32: two parts): relative to a reference that follows the largest of 2^x_rj |s_j|, so that the largest product lies in [2^7, 2^15] whatever
+// the scales are.  l, sum_j w z_j and O' are single precision.  A part more was measured: bf16 weights of 22 bits take 16 x 8 heads of 16000 rows from 52.7 to 54.3 us, 32 heads'
+// 40 queries over 2 x 8 of 4000 from 24.4 to 26.2, and leave the result as far off, 1.6e-3 of its norm; fp32 of 33 bits 324 to 374 (2000 queries of 32 heads over 8 of 4000 rows),
+// 104 to 111 (one query, 16 x 8 of 16000, 8 bits), and the result 1.1e-7 off where it is 1.2e-7 (heads of two rows), 2.8e-7 where it is 3.1e-7 (512 rows).
 //
-// Bound by the codes' bytes where the caches are long: 16 x 8 heads of 8192 to 32768 rows of 128, 4 bits, one query of 4 heads, 70 us and 5 for the join (4.9 TB/s, the
-// vector pipe busy for 0.53 of the time, the matrix pipe for 0.12); 32 x 8 heads of 1000 to 4096, 8 bits, 34 us (5.1 TB/s).  One round of workgroups with a window: 48 x 8
-// heads, 1024 rows each, 17 us, latency and the half-filled last round; 8 heads of 100 to 340 rows 7 us, one chain of loads; fp32, 3 x 2 heads of 333 to 512, 333 queries
-// of 2 heads, d 64, 9 us.  No gain: loads a tile ahead, two query tiles a workgroup, the queries' loads behind the first tile's.
+// Bound by the codes' bytes where the caches are long: 16 x 8 heads of 8192 to 32768 rows of 128, 4 bits, one query of 4 heads, 69 to 72 us and 5 for the join (5.0 to 5.2 TB/s, the
+// vector pipe busy for 0.52 of the time, the matrix pipe for 0.12); 32 x 8 heads of 1000 to 4096, 8 bits, 34 us (5.1 TB/s).  With a window of 1024, 48 x 8 heads, 17 to 18 us: all
+// 384 workgroups run at once, one on some compute units and two on the others, whose waves take four or five of a head's 33 or 34 tiles; 8 heads of 100 to 340 rows 7 us, one chain
+// of loads; fp32, 3 x 2 heads of 333 to 512, 333 queries of 2 heads, d 64, 8 to 9 us, 8 heads of 4000 rows of 128, 2000 queries of 32 heads, which read the codes for every 16 query
+// rows, 385 to 392 (0.25 PFLOP/s).  No gain: loads a tile ahead, two query tiles a workgroup, the queries' loads behind the first tile's.
 #include "attend_codes.hpp"
 #include "attend_few.hpp"
 #include "codes.hpp"

@@ -14,10 +14,11 @@
 //
 // Every workgroup of a head makes the numbers anew.  Where there are many (ROWS), a kernel of its own makes them once, and the tiles come straight to LDS.
 //
-// Bound by power with long prompts: 4096 queries of 32 heads over 8 heads of 13517 rows of 128, 4 bits, 780 to 820 us (0.96 PFLOP/s, the matrix pipe busy for 0.49 and the vector
-// pipe for 0.56 of the time, together 0.84, at 1.9 GHz) and 18 for the rows' numbers (73 MB, 4.0 TB/s).  By the longest heads where their lengths differ: 500 queries of 40 heads
-// over 3 x 8 heads of 700 to 2139 rows of 64, 8 bits, 47 to 53 us, one wave a SIMD on average, and 6 to 8 for the numbers.  No gain: the logits a tile ahead of the weights
-// (815 - 810 us; 32 row tiles over 8 heads of 8000 rows 192 - 212); two groups of waves on alternate tiles, joined in LDS (829 - 864; 59 - 60; 192 - 163).
+// Bound by power with long prompts: 4096 queries of 32 heads over 8 heads of 13517 rows of 128, 4 bits, 789 us at best and 841 on average of 30 in a row (0.92 to 0.98 PFLOP/s, the
+// matrix pipe busy for 0.48 and the vector pipe for 0.55 of the time, together 0.83, at 1.8 to 1.9 GHz) and 18 for the rows' numbers (73 MB, 4.0 TB/s); with a window of 1024, 2000
+// queries of 32 heads over 4 x 8 heads of 4000 to 6000 rows, 4 bits, 202 to 220 us (0.61 to 0.67 PFLOP/s of visible pairs) and 16 for the numbers.  By the longest heads where their
+// lengths differ: 500 queries of 40 heads over 3 x 8 heads of 700 to 2139 rows of 64, 8 bits, 51 us, one wave a SIMD on average, and 8 for the numbers.  No gain: the logits a tile
+// ahead of the weights (815 - 810 us; 32 row tiles over 8 heads of 8000 rows 192 - 212); two groups of waves on alternate tiles, joined in LDS (829 - 864; 59 - 60; 192 - 163).
 #include "attend_codes.hpp"
 #include "attend_tile.hpp"
 

@@ -3,8 +3,9 @@
 // The arithmetic is that of the row code (codes.hpp); what these kernels add is the addressing: rows at the strides of a projection's output,
 // a number of them per head, behind what the head holds, and back by row numbers.  16 columns a lane, keys and values in one launch.
 //
-// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 29 (4.5 and 5.9 TB/s), the kept rows of 36 x 8 heads (800 to
-// 1229), 8 bits, in 50 and back in 47 (4.5 and 4.8), 1229 of 8192 rows by their numbers in 52 (5.5 with the whole lines that rows of 64 bytes are part of).
+// Bound by memory: 4 x 8 heads of 8192 rows as a projection leaves them, 4 bits, in 38 us and back in 29 (4.5 and 5.8 TB/s), the kept rows of 36 x 8 heads (800 to
+// 1229), 8 bits, in 50 and back in 41 (4.5 and 5.5), 1229 of 8192 rows by their numbers in 52 (5.5 with the whole lines that rows of 64 bytes are part of); fp32 rows, 4 x 8 heads of
+// 8192 to 4 bits, in 78 and back in 71 (3.9 and 4.3).
 // One row a lane: 42, 35, 52, 56 and 63; four rows: 40, 32, 52, 44 and 52.  Stores that bypass the caches double the time of the way back.
 #include "attend_codes.hpp"
 #include "codes.hpp"

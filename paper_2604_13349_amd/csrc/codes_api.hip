@@ -98,8 +98,9 @@ struct AttendCodesPlan { AttendCodesArgs c; bool tile, rows; int waves; size_t p
 
 // Ranges of a launch of the kernel of many rows: the least of an estimate, in us.  A workgroup takes its tiles of 64 rows and as long as two more to begin and end, alone on a
 // compute unit `step` a tile, two in 1.5 times that, more one after another; a join 3 and the partial results' way to memory and back.  Of 190 shapes (8 to 128 heads of 700 to
-// 12000 rows, of one length and ragged, 80 to 2000 query rows) it chooses launches that take 1.014 of the time of the best of up to 12 on average, 1.15 at worst.  (As many ranges
-// as give each compute unit two workgroups, none from one a unit on: 1.067 and 1.58; 8 x 8 heads of 4000 to 12000 rows of 64, 500 query rows 236 - 161 us.)
+// 12000 rows, of one length and ragged, 80 to 2000 query rows) it chooses launches that take 1.014 of the time of the best of up to 12 on average, 1.15 at worst
+// (profiles/codes_launches.txt).  (As many ranges as give each compute unit two workgroups, none from one a unit on: 1.067 and 1.58; 8 x 8 heads of 4000 to 12000 rows of 64, 500
+// query rows 236 - 161 us.)
 static long tile_ranges(const long blocks, const long rows, const long out_rows, const int d) {
   const double step = d == 128 ? 1.42 : 1.06, join = 3.0, partial = out_rows * (double)d * 8 / 6e6;
   const long tiles = (rows + 63) / 64;
@@ -139,8 +140,8 @@ static AttendCodesPlan plan_attend_codes(const obf_attend_t* c, int bits, bool s
   if (p.tile) {
     ranges = tile_ranges(blocks, rows, a.rows, (int)d);
   } else {
-    // Few rows: how many ranges of how many waves was measured over 425 shapes (8 to 640 heads of 40 to 32000 rows, of one length and ragged, all types, 1 to 88 tiles of
-    // query rows), each with up to 14 launches; these rules take 1.014 of the best launch's time on average, 1.17 at worst.  us, otherwise and so:
+    // Few rows: how many ranges of how many waves was measured over 559 shapes (2 to 640 heads of 40 to 32000 rows, of one length and ragged, all types, 1 to 175 tiles of
+    // query rows), each with up to 14 launches (profiles/codes_launches.txt); these rules take 1.012 of the best launch's time on average, 1.17 at worst.  us, otherwise and so:
     //   a join takes 3 us: none for short caches (8 heads of 600 rows 10.8 - 7.9, 64 of 1000 11.9 - 10.7);
     //   few sets: a wave with one or two tiles and a join of 16 ranges ends before long ranges do (8 heads of 1500 rows, four of eight waves 12.7 - 9.7);
     //   long caches: as many small workgroups as even out heads of different lengths (136 of 5000 to 20000 rows, 2 of eight waves and 8 of four 82.9 - 65; 72 of them,

@@ -2,7 +2,7 @@
 
 Bounds, as in attend_ref (u = 2^-24), with a row's two numbers taken apart, since the kernels sum scale times codes and zeros separately: a logit is off by at most
 dx = (d + 8) u sum_c |q_c| (|s| c + |z|) / sqrt(d), a weight by a factor of 1 + 2 dx + (n + 16) u.  Beside that
-  few rows    fp32 queries enter as two parts of 11 bits (2^-22 of an element), every element with 2^-25 beside a largest of 2^14 or more (2^-39 of it); weights
+  few rows    fp32 queries enter as two parts of 11 bits (taken as 2^-22 of an element; 2^-23 at most), every element with 2^-25 beside a largest of 2^14 or more (2^-39 of it); weights
               times scale with 2^-11 (bf16) or 2^-22 (fp32) and 2^-25 beside a largest of 2^7 or more (2^-32 of the largest, in which a scale of 0 counts as
               2^-24), times codes up to L; with bf16, sums of V's codes drop what lies 2^-20 below a largest product
   many rows   queries with 2^-39 of the largest element, their sum with 2^-33 of it and 2^-25 beside one of up to 2^8 times 2^14 (2^-24 of the largest element, for
