@@ -481,6 +481,31 @@ def test_a_row_of_infinite_numbers_reaches_all_that_see_it_and_nobody_else(dtype
             _check("lse", o["lse"], lse, tl)
 
 
+@pytest.mark.parametrize("which,number", [(0, 1), (0, 2), (1, 1), (1, 2)])
+def test_infinite_numbers_among_copies_of_the_rows(which, number):
+    """17 tiles of query rows, of which 19 see a row: the rows' numbers are made once; all but the last queries see one that has none."""
+    T, rows, window, where = 1030, 2600, 1200, 1380
+    Q, K, V = _make(34, BF, 64, 1, 2, 2, T, rows)
+    Q = _both_signs(Q, 2)
+    kv_len = torch.full((1, 2), rows, dtype=torch.int32)
+    kw = dict(causal=True, window=window)
+    k, v = R.quantise(K, 4), R.quantise(V, 4)
+    O, lse, tO, tl = R.attend(Q, k, v, 4, kv_len, **kw)
+    sees = rows - T + torch.arange(T) - window < where
+    assert 0 < (~sees).sum() < 30
+    for value in (math.inf, -math.inf):
+        both = [tuple(x.clone() for x in y) for y in (k, v)]
+        both[which][number][:, :, where] = value
+        o = _run(Q, *both, 4, kv_len, crowd=True, **kw)
+        _check("O", o["O"][:, :, ~sees], O[:, :, ~sees], tO[:, :, ~sees])
+        _check("lse", o["lse"][:, :, ~sees], lse[:, :, ~sees], tl[:, :, ~sees])
+        assert not torch.isfinite(o["O"][:, :, sees].float()).any()
+        if which == 0:
+            assert torch.isnan(o["lse"][:, :, sees]).all()
+        else:
+            _check("lse", o["lse"], lse, tl)
+
+
 @pytest.mark.parametrize("dtype,T", [(BF, 1), (F32, 2), (BF, 300)])
 def test_keys_written_from_below_the_half_precision_range(dtype, T):
     """A key with an element of -1e5 has a finite scale and a zero of -inf: the queries that see it get no number, a window that hides it their results."""
